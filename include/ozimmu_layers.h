@@ -1,0 +1,73 @@
+/*
+ * ozimmu layers -- the feed-forward layer of a language model on MI355X (gfx950): a linear layer with its epilogue, its
+ * gradients, the AdamW step that uses them, and a mixture-of-experts layer for the few tokens of a serving step.
+ *
+ * Conventions, those of ozimmu.h where they apply
+ *   - Matrices hold one token, or one output feature of a weight, per row; the entries of a row are contiguous and rows
+ *     are `ld` entries apart (ld >= the entries of a row).  As column-major matrices they are the transposes: one column
+ *     a token.
+ *   - All matrix, state and workspace pointers are DEVICE pointers owned by the caller, aligned to their element (a
+ *     workspace to 256 bytes).  The library allocates nothing and keeps nothing from one call to the next.  Pointers marked [host]
+ *     are host pointers.
+ *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  Calls are asynchronous on that stream, record
+ *     into HIP graphs (kernels only) and return one of the OZIMMU_* status codes; nothing throws or aborts.
+ *   - Outputs must not overlap inputs or each other unless an entry point says so.
+ *   - Sums, activations and statistics are formed in 32 bits; what is written in 16 bits is rounded to nearest once.
+ *     Results are deterministic (no atomics on floating-point values; the order of every sum is fixed by the sizes).
+ *   - NaN and infinities go where the formulas take them; no entry point looks for them.
+ *   - Sizes of 0 are accepted: no tokens or no output features write nothing, n_in = 0 gives products of 0.
+ */
+#ifndef OZIMMU_LAYERS_H
+#define OZIMMU_LAYERS_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "ozimmu.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* element types */
+#define OZIMMU_BF16 0
+#define OZIMMU_F16 1
+#define OZIMMU_F32 2
+#define OZIMMU_E4M3 3 /* 8 bits, AdamW's states only */
+
+/* activations */
+#define OZIMMU_ACT_NONE 0
+#define OZIMMU_ACT_RELU 1
+#define OZIMMU_ACT_GELU 2      /* z Phi(z), Phi the normal distribution function */
+#define OZIMMU_ACT_GELU_TANH 3 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define OZIMMU_ACT_SILU 4      /* z / (1 + exp(-z)) */
+
+/*
+ * y = act(x w^T + bias) + residual
+ *   x [tokens, n_in], w [n_out, n_in], bias [n_out], residual, pre and y [tokens, n_out], all of `type` (BF16, F16, F32).
+ *   bias, residual and pre may be NULL.  pre receives x w^T + bias, which ozimmu_linear_grad takes.
+ *   residual may be y itself (same pointer and ld).
+ * Workspace: ozimmu_linear_workspace_bytes (partial sums where the contraction is divided among work-groups; it may be
+ * 0, then NULL is accepted).
+ */
+size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type);
+int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int ldx, const void *w, int ldw, const void *bias,
+                  const void *residual, int ldr, int activation, void *pre, int ldpre, void *y, int ldy, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of ozimmu_linear.  With dz = dy * act'(pre), rounded to `type` for the products (one rounding, to the
+ * type the matrix cores take; the bias gradient is summed from the unrounded values):
+ *   dx = dz w   [tokens, n_in],   dw = dz^T x   [n_out, n_in],   db = the sum of dz over the tokens   [n_out]
+ * (the gradient of the residual is dy itself).  dx, dw and db may each be NULL and are then not formed; pre may be NULL for
+ * OZIMMU_ACT_NONE; x may be NULL without dw, w without dx.  act'(0) = 0 for OZIMMU_ACT_RELU.
+ */
+size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation);
+int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const void *w,
+                       int ldw, const void *pre, int ldpre, int activation, void *dx, int lddx, void *dw, int lddw, void *db,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

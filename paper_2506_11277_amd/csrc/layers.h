@@ -1,0 +1,29 @@
+// Host-side declarations of the feed-forward operators: what ozimmu_layers.h's entry points call, per element type.
+#pragma once
+#include "layers_dev.h"
+
+namespace oz {
+
+inline size_t element_bytes(int type) { return type == OZIMMU_F32 ? 4 : 2; }
+
+ProductPlan plan_product(int np, int nq, int nk, int type);
+inline size_t product_partial_bytes(int np, int nq, const ProductPlan &p)
+{
+    return p.splits > 1 ? (size_t)p.splits * nq * ((np + 7) / 8 * 8) * 4 : 0;
+}
+hipError_t launch_product_bf16(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_product_f16(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_product_f32(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+
+// dz = dy * act'(pre) and the sums of its columns (grad.hip)
+constexpr int kGradRows = 64;              // tokens a work-group sums
+struct GradInput {
+    const void *dy, *pre;                  // pre may be null (no activation)
+    void *dz;                              // null: only the sums
+    void *db;                              // null: no sums
+    float *sums;                           // [ceil(tokens / kGradRows)][n_out]
+    int lddy, ldpre, lddz, tokens, n_out, act, wide;
+};
+hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st);
+
+}  // namespace oz

@@ -1,0 +1,182 @@
+// What the feed-forward operators (ozimmu_layers.h) share: element types, matrix instructions, activations, and the
+// epilogue of a product.  HIP only.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/ozimmu_layers.h"
+#include "gemm_dev.h"
+
+namespace oz {
+
+typedef __bf16 bf16;
+typedef _Float16 f16;
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
+
+// 16 bytes of elements: what a lane feeds to the matrix instructions per half of a step of 128 bytes of k.
+template <class T>
+struct Chunk {
+    static constexpr int E = 16 / (int)sizeof(T);
+    typedef T V __attribute__((ext_vector_type(E)));
+};
+
+// c += p q over the k of one chunk per lane.  Operands of 16 bits: one 16x16x32 instruction, lane l holds row l % 16 and
+// k 8 (l / 16) ... + 7.  32 bits: four 16x16x4 instructions, lane l's element i standing for k 4 (l / 16) + i; which k an
+// instruction takes does not matter as long as both operands agree.  Sums in 32 bits.
+// Result: lane l, register i = entry (4 (l / 16) + i, l % 16) of the 16 x 16 block, rows from p, columns from q.
+__device__ __forceinline__ v4f mma(v4u p, v4u q, v4f c, bf16)
+{
+    typedef Chunk<bf16>::V V;
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, p), __builtin_bit_cast(V, q), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(v4u p, v4u q, v4f c, f16)
+{
+    typedef Chunk<f16>::V V;
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, p), __builtin_bit_cast(V, q), c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(v4u p, v4u q, v4f c, float)
+{
+    const v4f a = __builtin_bit_cast(v4f, p), b = __builtin_bit_cast(v4f, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+}
+
+// 16 bytes from an address that is aligned to the element only, `n` elements of them there (the others 0)
+template <class T>
+__device__ __forceinline__ v4u load_chunk(const T *p, int n)
+{
+    constexpr int E = Chunk<T>::E;
+    union { v4u v; T e[E]; } r;
+    if (n >= E) {
+        __builtin_memcpy(&r.v, p, 16);
+    } else {
+        r.v = v4u{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < n) r.e[i] = p[i];
+    }
+    return r.v;
+}
+
+// Activations, in 32 bits.  (ACT_GELU: z Phi(z) = z (1 + erf(z / sqrt 2)) / 2.  ACT_GELU_TANH with
+// (1 + tanh u) / 2 = 1 / (1 + exp(-2u)).)
+__device__ __forceinline__ float activate(int act, float z)
+{
+    switch (act) {
+        case OZIMMU_ACT_RELU: return z < 0.0f ? 0.0f : z;               // (a NaN stays one)
+        case OZIMMU_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+        case OZIMMU_ACT_GELU_TANH: {
+            const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
+            return z / (1.0f + expf(-2.0f * u));
+        }
+        case OZIMMU_ACT_SILU: return z / (1.0f + expf(-z));
+    }
+    return z;
+}
+
+// ... and their slopes
+__device__ __forceinline__ float activation_slope(int act, float z)
+{
+    switch (act) {
+        case OZIMMU_ACT_RELU: return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+        case OZIMMU_ACT_GELU:
+            return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+        case OZIMMU_ACT_GELU_TANH: {
+            const float u = 0.79788456080286536f * (z + 0.044715f * z * z * z);
+            const float s = 1.0f / (1.0f + expf(-2.0f * u));
+            return s + z * 2.0f * s * (1.0f - s) * 0.79788456080286536f * (1.0f + 0.134145f * z * z);
+        }
+        case OZIMMU_ACT_SILU: {
+            const float s = 1.0f / (1.0f + expf(-z));
+            return s * (1.0f + z * (1.0f - s));
+        }
+    }
+    return 1.0f;
+}
+
+// What happens to the sums of a product: y = act(sum + bias) + residual, `pre` = sum + bias.  Entry (q, p) of the result
+// stands at out[q * ldo + p]: p runs along the contiguous side.
+struct Epilogue {
+    const void *bias, *residual;          // may be null
+    void *pre, *out;                      // pre may be null
+    int ldr, ldpre, ldo;
+    int np, nq;
+    int act;
+    int wide;                             // every row of 8 entries that starts at a multiple of 8 is aligned to its size, up to 16 bytes
+};
+
+template <class T, int N>
+__device__ __forceinline__ void load_row(const T *p, float (&v)[N])
+{
+    typedef T V __attribute__((ext_vector_type(N)));
+    const V x = *(const V *)p;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (float)x[i];
+}
+template <class T, int N>
+__device__ __forceinline__ void store_row(T *p, const float (&v)[N])
+{
+    typedef T V __attribute__((ext_vector_type(N)));
+    V x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (T)v[i];
+    *(V *)p = x;
+}
+
+// N = 8 (p a multiple of 8) entries of row q
+template <class T>
+__device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, float (&v)[8])
+{
+    if (e.wide && p + 8 <= e.np) {
+        float t[8];
+        if (e.bias) {
+            load_row((const T *)e.bias + p, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        if (e.pre) store_row((T *)e.pre + (size_t)q * e.ldpre + p, v);
+        if (e.act)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(e.act, v[i]);
+        if (e.residual) {
+            load_row((const T *)e.residual + (size_t)q * e.ldr + p, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        }
+        store_row((T *)e.out + (size_t)q * e.ldo + p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (p + i >= e.np) continue;
+            float x = v[i];
+            if (e.bias) x += (float)((const T *)e.bias)[p + i];
+            if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)x;
+            x = activate(e.act, x);
+            if (e.residual) x += (float)((const T *)e.residual)[(size_t)q * e.ldr + p + i];
+            ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)x;
+        }
+    }
+}
+
+// ---- launchers, one set per element type (layers_bf16.hip, layers_f16.hip, layers_f32.hip)
+
+// D[q][p] = sum over k of P Q.  An operand's rows (p or q) are contiguous along k (`k_rows`), or its entries of one k are
+// contiguous along p or q.
+struct Product {
+    const void *P, *Q;
+    int ldp, ldq;
+    bool p_k_rows, q_k_rows;
+    int nk;
+    Epilogue e;
+};
+
+struct ProductPlan {
+    int tile;                // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+    int splits, steps;       // the contraction in `splits` parts of `steps` steps of 128 bytes
+    bool direct;             // copied to LDS without registers
+};
+
+}  // namespace oz
