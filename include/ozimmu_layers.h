@@ -67,6 +67,54 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
                        int ldw, const void *pre, int ldpre, int activation, void *dx, int lddx, void *dw, int lddw, void *db,
                        void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * One AdamW step, in place, over `tensors` tensors of `list` [host, read before the call returns]:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = (1 - lr weight_decay) p - lr / (1 - beta1^step)  m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in 32 bits, every operation rounded by itself.  step counts from 1.
+ *   grads [host]  the gradients' pointers, or NULL: those of the list.
+ *   state_type OZIMMU_F32: m and v are floats.  OZIMMU_E4M3: blocks of 256 consecutive values (the last one of a tensor may
+ *     be shorter) hold m and sqrt(v) as m[i] * m_scale[i / 256] and v[i] * v_scale[i / 256], m[i] and v[i] e4m3 (a sign bit,
+ *     4 of exponent, 3 of mantissa, largest value 448, 0x7f a NaN) and the scales float, 1/448 of the block's largest finite
+ *     magnitude.  A value between two codes goes to the upper one with the probability of its distance from the
+ *     lower, by 32-bit words that depend on the value's place, step and seed only; sqrt(v) > 0 does not become 0.  A NaN or an infinity makes its own m and v NaN,
+ *     the others of the block stay what they are.  Where a block's
+ *     largest magnitude is below 2^-100, m is held as zeros and sqrt(v) > 0 as the smallest code.
+ *   copy, may be NULL: receives p in 16 bits (copy_type BF16 or F16), the weights of the next forward pass.
+ * Tensors are arrays of `count` contiguous values at any alignment of their type; they must not overlap.
+ */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale; /* OZIMMU_E4M3 only: (count + 255) / 256 of each */
+    void *copy;
+    int64_t count;
+    int param_type, grad_type, state_type, copy_type;
+} ozimmu_adamw_tensor;
+
+int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const void *const *grads, double lr, double beta1, double beta2,
+                 double eps, double weight_decay, long long step, uint32_t seed, void *stream);
+
+/*
+ * A mixture-of-experts layer for the tokens of a serving step, 0 <= tokens <= OZIMMU_MOE_TOKENS:
+ *   logits = x router^T;  the top_k experts of a token are those of its largest logits, ties to the lowest index;
+ *   gate = exp(logit) / the sum of exp(logit) over all experts, or over the chosen ones where `normalise` is not 0;
+ *   y = sum over the chosen experts e of  gate_e w_out[e] (silu(w_in[e][0 ... hidden) x) * (w_in[e][hidden ... 2 hidden) x))
+ *   x, y [tokens, width]; router [experts, width], w_in [experts, 2 hidden, width], w_out [experts, width, hidden] contiguous;
+ *   all of `type`.  chosen [tokens, top_k]: the experts of each token in ascending order; gates: theirs, float.
+ * The products of the hidden layer are rounded to `type` with their gate for the second product (one rounding).  A NaN
+ * logit counts as larger than any number.
+ * 1 <= top_k <= experts <= OZIMMU_MOE_EXPERTS, top_k <= OZIMMU_MOE_TOP_K.
+ */
+#define OZIMMU_MOE_TOKENS 64
+#define OZIMMU_MOE_EXPERTS 512
+#define OZIMMU_MOE_TOP_K 16
+size_t ozimmu_moe_workspace_bytes(int tokens, int width, int hidden, int experts, int top_k, int type);
+int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int type, int normalise, const void *x, int ldx,
+               const void *router, const void *w_in, const void *w_out, int32_t *chosen, float *gates, void *y, int ldy,
+               void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

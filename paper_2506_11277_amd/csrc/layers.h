@@ -6,7 +6,8 @@ namespace oz {
 
 inline size_t element_bytes(int type) { return type == OZIMMU_F32 ? 4 : 2; }
 
-ProductPlan plan_product(int np, int nq, int nk, int type);
+constexpr int kFewTokens = 64;             // columns few_tokens_kernel takes
+ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows);
 inline size_t product_partial_bytes(int np, int nq, const ProductPlan &p)
 {
     return p.splits > 1 ? (size_t)p.splits * nq * ((np + 7) / 8 * 8) * 4 : 0;
@@ -25,5 +26,15 @@ struct GradInput {
     int lddy, ldpre, lddz, tokens, n_out, act, wide;
 };
 hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st);
+
+// a mixture-of-experts layer on a few tokens (moe.hip)
+struct MoeArgs {
+    const void *x, *router, *w_in, *w_out;
+    int *chosen;
+    float *gates;
+    void *h, *y;                           // h: [tokens * top_k] rows of the hidden layer, ldh apart
+    int ldx, ldh, ldy, tokens, width, hidden, experts, top_k, normalise;
+};
+hipError_t launch_moe(const MoeArgs &a, int type, hipStream_t st);
 
 }  // namespace oz

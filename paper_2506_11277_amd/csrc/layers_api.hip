@@ -5,10 +5,18 @@ namespace oz {
 
 // Tile and number of parts of the contraction.  A launch takes as many rounds as its work-groups need on 256 compute
 // units; a round of tiles costs their entries times the steps over the rate that tile reaches where it fills the chip.
-ProductPlan plan_product(int np, int nq, int nk, int type)
+ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows)
 {
     const int ke = type == OZIMMU_F32 ? 32 : 64;
     const int all = (nk + ke - 1) / ke;
+    if (k_rows && nq <= kFewTokens) {
+        // work-groups of 16 features; the contraction is divided where they leave most compute units without one
+        const int groups = (np + 15) / 16;
+        int s = 1;
+        while (s < 16 && groups * s * 2 <= 256 && all / (2 * s) >= 16) s *= 2;
+        const int steps = (all + s - 1) / s;
+        return ProductPlan{kTileFew, steps > 0 ? (all + steps - 1) / steps : 1, steps, false};
+    }
     static const int edge[3] = {256, 128, 64};
     static const double rate[3] = {1.0, 0.8, 0.5};
     ProductPlan best{2, 1, all, false};
@@ -81,8 +89,8 @@ GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int acti
     w.lddz = (n_out + 7) & ~7;
     w.sums = activation == OZIMMU_ACT_NONE ? 0 : padded((size_t)tokens * w.lddz * element_bytes(type));
     w.partial = w.sums + padded((size_t)((tokens + kGradRows - 1) / kGradRows) * n_out * 4);
-    const size_t dx = product_partial_bytes(n_in, tokens, plan_product(n_in, tokens, n_out, type));
-    const size_t dw = product_partial_bytes(n_in, n_out, plan_product(n_in, n_out, tokens, type));
+    const size_t dx = product_partial_bytes(n_in, tokens, plan_product(n_in, tokens, n_out, type, false));
+    const size_t dw = product_partial_bytes(n_in, n_out, plan_product(n_in, n_out, tokens, type, false));
     w.total = w.partial + padded(dx > dw ? dx : dw);
     return w;
 }
@@ -99,7 +107,7 @@ extern "C" {
 size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type)
 {
     if (tokens < 0 || n_in < 0 || n_out < 0 || bad_type(type)) return 0;
-    return product_partial_bytes(n_out, tokens, plan_product(n_out, tokens, n_in, type));
+    return product_partial_bytes(n_out, tokens, plan_product(n_out, tokens, n_in, type, true));
 }
 
 int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int ldx, const void *w, int ldw, const void *bias,
@@ -111,7 +119,7 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     if (bad_rows(tokens, n_in, x, ldx, size) || bad_rows(n_out, n_in, w, ldw, size) || bad_rows(tokens, n_out, y, ldy, size)) return OZIMMU_BAD_ARG;
     if ((uintptr_t)bias % size || (residual && bad_rows(tokens, n_out, residual, ldr, size)) || (pre && bad_rows(tokens, n_out, pre, ldpre, size)))
         return OZIMMU_BAD_ARG;
-    const ProductPlan plan = plan_product(n_out, tokens, n_in, type);
+    const ProductPlan plan = plan_product(n_out, tokens, n_in, type, true);
     if (bad_workspace(workspace, workspace_bytes, product_partial_bytes(n_out, tokens, plan))) return OZIMMU_BAD_ARG;
     Product a{};
     a.P = w;
@@ -178,7 +186,7 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
         a.q_k_rows = true;
         a.nk = n_out;
         a.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, 0};
-        if (launch_product(a, plan_product(n_in, tokens, n_out, type), type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+        if (launch_product(a, plan_product(n_in, tokens, n_out, type, false), type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     }
     if (dw) {
         a.P = x;
@@ -188,9 +196,35 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
         a.q_k_rows = false;
         a.nk = tokens;
         a.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, 0};
-        if (launch_product(a, plan_product(n_in, n_out, tokens, type), type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+        if (launch_product(a, plan_product(n_in, n_out, tokens, type, false), type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     }
     return OZIMMU_OK;
+}
+
+size_t ozimmu_moe_workspace_bytes(int tokens, int width, int hidden, int experts, int top_k, int type)
+{
+    if (tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || hidden < 0 || experts < 1 || experts > OZIMMU_MOE_EXPERTS || top_k < 1 ||
+        top_k > experts || top_k > OZIMMU_MOE_TOP_K || bad_type(type))
+        return 0;
+    return padded((size_t)tokens * top_k * ((hidden + 7) & ~7) * element_bytes(type));
+}
+
+int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int type, int normalise, const void *x, int ldx,
+               const void *router, const void *w_in, const void *w_out, int32_t *chosen, float *gates, void *y, int ldy,
+               void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (bad_type(type) || tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || hidden < 0 || hidden > 0x3fffffff || experts < 1 ||
+        experts > OZIMMU_MOE_EXPERTS || top_k < 1 || top_k > experts || top_k > OZIMMU_MOE_TOP_K)
+        return OZIMMU_BAD_ARG;
+    const size_t size = element_bytes(type);
+    if (bad_rows(tokens, width, x, ldx, size) || bad_rows(tokens, width, y, ldy, size) || bad_rows(experts, width, router, width > 1 ? width : 1, size) ||
+        bad_rows(2 * hidden, width, w_in, width > 1 ? width : 1, size) || bad_rows(width, hidden, w_out, hidden > 1 ? hidden : 1, size))
+        return OZIMMU_BAD_ARG;
+    if (tokens > 0 && (!chosen || !gates || (uintptr_t)chosen % 4 || (uintptr_t)gates % 4)) return OZIMMU_BAD_ARG;
+    if (bad_workspace(workspace, workspace_bytes, ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, type))) return OZIMMU_BAD_ARG;
+    if (tokens == 0) return OZIMMU_OK;
+    const MoeArgs a{x, router, w_in, w_out, chosen, gates, workspace, y, ldx, (hidden + 7) & ~7, ldy, tokens, width, hidden, experts, top_k, normalise != 0};
+    return launch_moe(a, type, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
 }
 
 }  // extern "C"

@@ -173,8 +173,9 @@ struct Product {
     Epilogue e;
 };
 
+enum Tile { kTile256, kTile128, kTile64, kTileFew };      // edge; few_tokens_kernel
 struct ProductPlan {
-    int tile;                // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+    int tile;
     int splits, steps;       // the contraction in `splits` parts of `steps` steps of 128 bytes
     bool direct;             // copied to LDS without registers
 };

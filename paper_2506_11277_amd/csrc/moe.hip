@@ -1,0 +1,251 @@
+// A mixture-of-experts layer for a few tokens.  Bound by memory: the weights of the chosen experts, read once.
+//
+//   moe_route_kernel   a work-group per token: logits of all experts, the chosen ones and their gates
+//   moe_hidden_kernel  a work-group per 16 hidden features of an expert that some token chose: gate and up rows against
+//                      the tokens that chose it, h = gate silu(a) b rounded for the next product
+//   moe_out_kernel     a work-group per 16 output features: their rows of every chosen expert against its tokens' h, all in one
+//                      sum, so nothing is scattered and no atomics change an order
+//
+// Which experts are chosen is known on the device only: the second launch has a work-group for each of the min(experts,
+// tokens * top_k) experts that can be, which finds its expert in a bit map of the chosen ones and leaves if there is none.
+#include "layers.h"
+#include "stream_dev.h"
+
+namespace oz {
+namespace {
+
+constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 8;
+constexpr int kWords = OZIMMU_MOE_EXPERTS / 32;
+
+// bit map of the experts that the `n` choices name
+__device__ __forceinline__ void mark_chosen(unsigned *map, const int *chosen, int n)
+{
+    for (int i = threadIdx.x; i < kWords; i += blockDim.x) map[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) atomicOr(&map[chosen[i] >> 5], 1u << (chosen[i] & 31));
+    __syncthreads();
+}
+
+// a > b, a NaN above everything, for a at a later place than b if `later` (ties go to the earlier one)
+__device__ __forceinline__ bool before(float a, float b, bool later)
+{
+    const bool an = a != a, bn = b != b;
+    if (an || bn) return an && (!bn || !later);
+    return later ? a > b : a >= b;
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
+{
+    constexpr int E = Chunk<T>::E;
+    typedef typename Chunk<T>::V V;
+    __shared__ float logits[OZIMMU_MOE_EXPERTS];
+    __shared__ float best[OZIMMU_MOE_EXPERTS];
+    __shared__ unsigned map[kWords];
+    __shared__ float total;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int t = blockIdx.x;
+    const T *x = (const T *)a.x + (size_t)t * a.ldx;
+    for (int i = threadIdx.x; i < kWords; i += blockDim.x) map[i] = 0;
+    // four experts of a wavefront at a time
+    for (int e0 = wave; e0 < a.experts; e0 += 4 * kRouteWaves) {
+        const T *r[4];
+        float s[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = e0 + i * kRouteWaves;
+            r[i] = (const T *)a.router + (size_t)(e < a.experts ? e : e0) * a.width;
+        }
+        for (int k = lane * E; k < a.width; k += 64 * E) {
+            const int n = a.width - k;
+            const V xv = __builtin_bit_cast(V, load_chunk(x + k, n));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const V rv = __builtin_bit_cast(V, load_chunk(r[i] + k, n));
+#pragma unroll
+                for (int c = 0; c < E; ++c) s[i] = __builtin_fmaf((float)xv[c], (float)rv[c], s[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int d = 32; d; d >>= 1) s[i] += __shfl_xor(s[i], d);
+            if (lane == 0 && e0 + i * kRouteWaves < a.experts) logits[e0 + i * kRouteWaves] = s[i];
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
+        const float l = logits[e];
+        int rank = 0;
+        for (int o = 0; o < a.experts; ++o) rank += o != e && before(logits[o], l, o > e);
+        if (rank < a.top_k) atomicOr(&map[e >> 5], 1u << (e & 31));
+        best[e] = l;
+    }
+    __syncthreads();
+    // the largest logit and the sum of the exponentials, by one wavefront
+    if (wave == 0) {
+        float top = -__builtin_inff();
+        for (int e = lane; e < a.experts; e += 64) top = fmaxf(top, best[e]);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        float sum = 0.0f;
+        for (int e = lane; e < a.experts; e += 64) {
+            const float x = expf(best[e] - top);
+            best[e] = x;
+            if (!a.normalise || (map[e >> 5] >> (e & 31) & 1)) sum += x;
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) total = sum;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
+        if (!(map[e >> 5] >> (e & 31) & 1)) continue;
+        int place = __popc(map[e >> 5] & ((1u << (e & 31)) - 1));
+        for (int i = 0; i < e >> 5; ++i) place += __popc(map[i]);
+        a.chosen[t * a.top_k + place] = e;
+        a.gates[t * a.top_k + place] = best[e] / total;
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a)
+{
+    constexpr int KE = 8 * Chunk<T>::E;
+    __shared__ unsigned map[kWords];
+    __shared__ int choices[OZIMMU_MOE_TOKENS];                 // of the tokens that chose this expert: token * top_k + place
+    __shared__ int count;
+    __shared__ __attribute__((aligned(16))) float sums[kHiddenWaves][2][16 * kStreamLd];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int all = a.tokens * a.top_k;
+    mark_chosen(map, a.chosen, all);
+    int expert = -1;
+    for (int i = 0, left = blockIdx.y; i < kWords; ++i) {      // the blockIdx.y-th bit that is set
+        unsigned m = map[i];
+        const int n = __popc(m);
+        if (left >= n) {
+            left -= n;
+            continue;
+        }
+        for (; left > 0; --left) m &= m - 1;
+        expert = i * 32 + __builtin_ctz(m);
+        break;
+    }
+    if (expert < 0) return;
+    if (wave == 0) {                                           // its tokens in their order: a lane each
+        int mine = -1;
+        if (lane < a.tokens)
+            for (int i = 0; i < a.top_k; ++i)
+                if (a.chosen[lane * a.top_k + i] == expert) mine = lane * a.top_k + i;
+        const unsigned long long who = __ballot(mine >= 0);
+        if (mine >= 0) choices[__popcll(who & ((1ull << lane) - 1))] = mine;
+        if (lane == 0) count = __popcll(who);
+    }
+    __syncthreads();
+    const int f0 = blockIdx.x * 16, row = f0 + (lane & 15) < a.hidden ? f0 + (lane & 15) : a.hidden - 1;
+    const T *const base = (const T *)a.w_in + (size_t)expert * 2 * a.hidden * a.width;
+    const T *const w[2] = {base + (size_t)row * a.width, base + ((size_t)a.hidden + row) * a.width};
+    const int steps = (a.width + KE - 1) / KE;
+    for (int c0 = 0; c0 < count; c0 += 16) {
+        const bool on[1] = {c0 + (lane & 15) < count};
+        const T *const x[1] = {(const T *)a.x + (size_t)(choices[on[0] ? c0 + (lane & 15) : 0] / a.top_k) * a.ldx};
+        v4f acc[2][1] = {{v4f{0, 0, 0, 0}}, {v4f{0, 0, 0, 0}}};
+        stream_products<T, 2, 1, 4>(acc, w, x, on, wave, steps, kHiddenWaves, a.width, lane);
+        put_sums(sums[wave][0], acc[0][0], lane);
+        put_sums(sums[wave][1], acc[1][0], lane);
+        __syncthreads();
+        const int i = threadIdx.x;                             // 16 tokens x 16 features
+        const int q = i >> 4, f = i & 15;
+        if (i < 256 && c0 + q < count && f0 + f < a.hidden) {
+            float g = 0.0f, u = 0.0f;
+#pragma unroll
+            for (int s = 0; s < kHiddenWaves; ++s) {
+                g += sums[s][0][q * kStreamLd + f];
+                u += sums[s][1][q * kStreamLd + f];
+            }
+            const int choice = choices[c0 + q];
+            ((T *)a.h)[(size_t)choice * a.ldh + f0 + f] = (T)(a.gates[choice] * activate(OZIMMU_ACT_SILU, g) * u);
+        }
+        __syncthreads();
+    }
+}
+
+template <class T, int NX>
+__global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
+{
+    constexpr int KE = 8 * Chunk<T>::E;
+    __shared__ unsigned map[kWords];
+    __shared__ int chosen[OZIMMU_MOE_TOKENS * OZIMMU_MOE_TOP_K];
+    __shared__ __attribute__((aligned(16))) float sums[kOutWaves][NX][16 * kStreamLd];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int all = a.tokens * a.top_k;
+    for (int i = threadIdx.x; i < all; i += blockDim.x) chosen[i] = a.chosen[i];
+    mark_chosen(map, a.chosen, all);
+    const int p0 = blockIdx.x * 16, row = p0 + (lane & 15) < a.width ? p0 + (lane & 15) : a.width - 1;
+    v4f acc[1][NX];
+#pragma unroll
+    for (int j = 0; j < NX; ++j) acc[0][j] = v4f{0, 0, 0, 0};
+    // the steps of all chosen experts, one after the other, are dealt to the wavefronts in turn
+    const int steps = (a.hidden + KE - 1) / KE;
+    int first = wave;
+    for (int i = 0; i < kWords; ++i)
+        for (unsigned m = map[i]; m; m &= m - 1) {
+            const int expert = i * 32 + __builtin_ctz(m);
+            if (first < steps) {
+                const T *const w[1] = {(const T *)a.w_out + ((size_t)expert * a.width + row) * a.hidden};
+                const T *x[NX];
+                bool on[NX];
+#pragma unroll
+                for (int j = 0; j < NX; ++j) {
+                    const int t = 16 * j + (lane & 15);
+                    int choice = -1;
+                    if (t < a.tokens)
+                        for (int c = 0; c < a.top_k; ++c)
+                            if (chosen[t * a.top_k + c] == expert) choice = t * a.top_k + c;
+                    on[j] = choice >= 0;
+                    x[j] = (const T *)a.h + (size_t)(on[j] ? choice : 0) * a.ldh;
+                }
+                stream_products<T, 1, NX, NX == 1 ? 4 : 2>(acc, w, x, on, first, steps, kOutWaves, a.hidden, lane);
+            }
+            // where this wavefront goes on in the next expert's steps
+            first = ((first - steps) % kOutWaves + kOutWaves) % kOutWaves;
+        }
+#pragma unroll
+    for (int j = 0; j < NX; ++j) put_sums(sums[wave][j], acc[0][j], lane);
+    __syncthreads();
+    for (int i = threadIdx.x; i < NX * 256; i += 64 * kOutWaves) {
+        const int q = i >> 4, p = i & 15;
+        if (q >= a.tokens || p0 + p >= a.width) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kOutWaves; ++s) v += sums[s][q >> 4][(q & 15) * kStreamLd + p];
+        ((T *)a.y)[(size_t)q * a.ldy + p0 + p] = (T)v;
+    }
+}
+
+template <class T>
+hipError_t launch(const MoeArgs &a, hipStream_t st)
+{
+    moe_route_kernel<T><<<a.tokens, 64 * kRouteWaves, 0, st>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    const int can = a.tokens * a.top_k < a.experts ? a.tokens * a.top_k : a.experts;
+    if (a.hidden > 0) {
+        moe_hidden_kernel<T><<<dim3((a.hidden + 15) / 16, can), 64 * kHiddenWaves, 0, st>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    const int groups = (a.width + 15) / 16;
+    if (groups == 0) return hipSuccess;
+    if (a.tokens <= 16) moe_out_kernel<T, 1><<<groups, 64 * kOutWaves, 0, st>>>(a);
+    else if (a.tokens <= 32) moe_out_kernel<T, 2><<<groups, 64 * kOutWaves, 0, st>>>(a);
+    else moe_out_kernel<T, 4><<<groups, 64 * kOutWaves, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_moe(const MoeArgs &a, int type, hipStream_t st)
+{
+    return type == OZIMMU_BF16 ? launch<bf16>(a, st) : type == OZIMMU_F16 ? launch<f16>(a, st) : launch<float>(a, st);
+}
+
+}  // namespace oz

@@ -17,7 +17,7 @@
 // behind k is read from a chunk of zeros.  Otherwise 16 bytes a lane are loaded at any alignment, and written to LDS behind the
 // products.  Rows behind the operand's last are read as the last and not stored.
 #pragma once
-#include "layers_dev.h"
+#include "few_dev.h"
 
 namespace oz {
 
@@ -318,15 +318,7 @@ hipError_t launch_product_shape(const Product &a, const ProductPlan &plan, float
     static std::atomic<unsigned long long> done{0};
     if (hipError_t e = allow_dynamic_lds((const void *)kernel, S::kLds, done)) return e;
     kernel<<<dim3((unsigned)blocks, plan.splits), S::kThreads, S::kLds, st>>>(a, plan.splits > 1 ? partial : nullptr, plan.steps, tiles_p, tiles_q);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (plan.splits > 1) {
-        const size_t threads = (size_t)a.e.nq * ((a.e.np + 7) / 8);
-        const size_t groups = (threads + 255) / 256;
-        if (groups > 0x7fffffff) return hipErrorInvalidValue;
-        product_join_kernel<T><<<(unsigned)groups, 256, 0, st>>>(a.e, partial, plan.splits);
-        return hipGetLastError();
-    }
-    return hipSuccess;
+    return hipGetLastError();
 }
 
 template <class T, bool PK, bool QK>
@@ -343,11 +335,27 @@ hipError_t launch_product_order(const Product &a, const ProductPlan &plan, float
 }
 
 template <class T>
-hipError_t launch_product_type(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
+hipError_t launch_product_tiles(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
     if (a.p_k_rows && a.q_k_rows) return launch_product_order<T, true, true>(a, plan, partial, st);
     if (a.q_k_rows) return launch_product_order<T, false, true>(a, plan, partial, st);
     return launch_product_order<T, false, false>(a, plan, partial, st);
+}
+
+template <class T>
+hipError_t launch_join(const Product &a, const ProductPlan &plan, const float *partial, hipStream_t st)
+{
+    const size_t threads = (size_t)a.e.nq * ((a.e.np + 7) / 8), groups = (threads + 255) / 256;
+    if (groups > 0x7fffffff) return hipErrorInvalidValue;
+    product_join_kernel<T><<<(unsigned)groups, 256, 0, st>>>(a.e, partial, plan.splits);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_product_type(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
+{
+    if (hipError_t e = plan.tile == kTileFew ? launch_few_tokens<T>(a, plan, partial, st) : launch_product_tiles<T>(a, plan, partial, st)) return e;
+    return plan.splits > 1 ? launch_join<T>(a, plan, partial, st) : hipSuccess;
 }
 
 }  // namespace oz

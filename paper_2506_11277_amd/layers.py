@@ -14,6 +14,8 @@ BF16, F16, F32, E4M3 = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 
+BLOCK = 256          # values that share a scale where AdamW's moments are held in 8 bits
+
 _TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 
 _c = ctypes
@@ -23,7 +25,18 @@ _SIGNATURES = {
     "ozimmu_linear": (_int, [_int] * 4 + [_ptr, _int, _ptr, _int, _ptr, _ptr, _int, _int, _ptr, _int, _ptr, _int, _ptr, _size, _ptr]),
     "ozimmu_linear_grad_workspace_bytes": (_size, [_int] * 5),
     "ozimmu_linear_grad": (_int, [_int] * 4 + [_ptr, _int] * 4 + [_int] + [_ptr, _int] * 2 + [_ptr, _ptr, _size, _ptr]),
+    "ozimmu_moe_workspace_bytes": (_size, [_int] * 6),
+    "ozimmu_moe": (_int, [_int] * 7 + [_ptr, _int] + [_ptr] * 6 + [_int, _ptr, _size, _ptr]),
 }
+
+
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", _ptr), ("grad", _ptr), ("m", _ptr), ("v", _ptr), ("m_scale", _ptr), ("v_scale", _ptr), ("copy", _ptr),
+                ("count", _c.c_int64), ("param_type", _int), ("grad_type", _int), ("state_type", _int), ("copy_type", _int)]
+
+
+_SIGNATURES["ozimmu_adamw"] = (_int, [_int, _c.POINTER(_AdamWTensor), _c.POINTER(_ptr)] + [_c.c_double] * 5 +
+                               [_c.c_longlong, _c.c_uint32, _ptr])
 
 _lib = None
 
@@ -145,3 +158,118 @@ def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=
     if rc != OK:
         raise OzimmuError(rc, "linear_grad")
     return dx, dw, db
+
+
+def adamw_state(params, bits=32):
+    """Moments of new parameters for AdamW: (m, v, m_scale, v_scale), lists with a tensor per parameter.  bits=32: float32,
+    the scales None; bits=8: float8_e4m3fn values of m and of the root of v, one float32 scale of each per BLOCK values."""
+    if bits not in (8, 32):
+        raise ValueError("bits: 8 or 32 expected")
+    kind = torch.float32 if bits == 32 else torch.float8_e4m3fn
+
+    def zeros():
+        return [torch.zeros(p.numel(), dtype=torch.float32 if bits == 32 else torch.uint8, device=p.device).view(kind).view(p.shape) for p in params]
+
+    def scales():
+        return None if bits == 32 else [torch.zeros(-(-p.numel() // BLOCK), dtype=torch.float32, device=p.device) for p in params]
+
+    return zeros(), zeros(), scales(), scales()
+
+
+class AdamW:
+    """AdamW over many tensors at once: a plan for parameters and moments that stay where they are.
+
+    params: float32, bfloat16 or float16; m, v and their scales as adamw_state gives them (float32 moments, or float8_e4m3fn
+    ones with scales); copies: None, or a bfloat16 or float16 tensor per parameter that receives it with every step.
+    The plan holds the tensors; one that is replaced or resized needs a new plan."""
+
+    def __init__(self, params, m, v, m_scale=None, v_scale=None, copies=None):
+        n = len(params)
+        given = [params, m, v] + [x for x in (m_scale, v_scale, copies) if x is not None]
+        if any(len(x) != n for x in given):
+            raise ValueError("AdamW: lists of one length expected")
+        self._held = given
+        self._list = (_AdamWTensor * n)()
+        self._shapes = [p.shape for p in params]
+        self._device = params[0].device if n else None
+        for i, (t, p) in enumerate(zip(self._list, params)):
+            kind = _type_of(p, f"params[{i}]")
+            eight = m[i].dtype == torch.float8_e4m3fn
+            expected = torch.float8_e4m3fn if eight else torch.float32
+            for x, what, dtypes in ((p, "params", (p.dtype,)), (m[i], "m", (expected,)), (v[i], "v", (expected,)),
+                                    (None if copies is None else copies[i], "copies", (torch.bfloat16, torch.float16))):
+                if x is not None and (x.dtype not in dtypes or x.shape != p.shape or x.device != self._device or not x.is_contiguous()):
+                    raise ValueError(f"{what}[{i}]: contiguous {list(p.shape)} of {dtypes[0]} on {self._device} expected")
+            t.param, t.m, t.v, t.count, t.param_type, t.grad_type = p.data_ptr(), m[i].data_ptr(), v[i].data_ptr(), p.numel(), kind, -1
+            t.state_type = E4M3 if eight else F32
+            if eight:
+                for x, what in ((m_scale, "m_scale"), (v_scale, "v_scale")):
+                    if x is None or x[i].dtype != torch.float32 or x[i].numel() != -(-p.numel() // BLOCK) or x[i].device != self._device or not x[i].is_contiguous():
+                        raise ValueError(f"{what}[{i}]: contiguous [{-(-p.numel() // BLOCK)}] of float32 on {self._device} expected")
+                t.m_scale, t.v_scale = m_scale[i].data_ptr(), v_scale[i].data_ptr()
+            if copies is not None:
+                t.copy, t.copy_type = copies[i].data_ptr(), _TYPES[copies[i].dtype]
+        self._grad_types = None
+        self._pointers = _ptr * n
+
+    def step(self, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, seed=0):
+        """One step with the gradients `grads`, contiguous tensors of the parameters' shapes; `step` counts from 1; `seed`
+        makes the random words that 8-bit moments are rounded with.  Asynchronous on the current stream."""
+        kinds = [g.dtype for g in grads]
+        if [g.shape for g in grads] != self._shapes or any([g.device != self._device or not g.is_contiguous() for g in grads]):
+            raise ValueError("grads: contiguous tensors of the parameters' shapes and device expected")
+        if kinds != self._grad_types:
+            for t, kind in zip(self._list, kinds):
+                if kind not in _TYPES:
+                    raise ValueError("grads: bfloat16, float16 or float32 expected")
+                t.grad_type = _TYPES[kind]
+            self._grad_types = kinds
+        pointers = self._pointers(*[g.data_ptr() for g in grads])
+        rc = (_lib or lib()).ozimmu_adamw(len(self._list), self._list, pointers, lr, beta1, beta2, eps, weight_decay, step,
+                                          seed & 0xffffffff, ozimmu._stream())
+        if rc != OK:
+            raise OzimmuError(rc, "adamw")
+
+
+MOE_TOKENS, MOE_EXPERTS, MOE_TOP_K = 64, 512, 16       # at most
+
+
+def moe_workspace_bytes(tokens, width, hidden, experts, top_k, dtype):
+    return lib().ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, _TYPES[dtype])
+
+
+def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, gates=None, workspace=None):
+    """A mixture-of-experts layer on at most MOE_TOKENS tokens; returns (y, chosen, gates).
+
+    x [tokens, width], router [experts, width], w_in [experts, 2 * hidden, width] (gate rows, then up rows), w_out [experts,
+    width, hidden], the weights contiguous.  Every token takes the top_k experts of its largest logits x @ router.T
+    (ties to the lowest index) with the softmax over all experts, or over the chosen ones (normalise), as their gates.
+    chosen [tokens, top_k], int32, lists them in ascending order, gates, float32, has theirs."""
+    kind = _type_of(x, "x")
+    if x.dim() != 2 or router.dim() != 2 or w_in.dim() != 3 or w_out.dim() != 3:
+        raise ValueError("x and router: matrices, w_in and w_out: three dimensions expected")
+    tokens, width = x.shape
+    experts, hidden = router.shape[0], w_out.shape[2]
+    for w, shape, what in ((router, (experts, width), "router"), (w_in, (experts, 2 * hidden, width), "w_in"),
+                           (w_out, (experts, width, hidden), "w_out")):
+        if w.shape != shape or w.dtype != x.dtype or w.device != x.device or not w.is_contiguous():
+            raise ValueError(f"{what}: contiguous {list(shape)} of {x.dtype} on {x.device} expected")
+    ldx = _ld(x, tokens, width, x, "x")
+    if out is None:
+        out = torch.empty((tokens, width), dtype=x.dtype, device=x.device)
+    ldy = _ld(out, tokens, width, x, "out")
+    if chosen is None:
+        chosen = torch.empty((tokens, top_k), dtype=torch.int32, device=x.device)
+    if gates is None:
+        gates = torch.empty((tokens, top_k), dtype=torch.float32, device=x.device)
+    for t, dtype, what in ((chosen, torch.int32, "chosen"), (gates, torch.float32, "gates")):
+        if t.shape != (tokens, top_k) or t.dtype != dtype or t.device != x.device or not t.is_contiguous():
+            raise ValueError(f"{what}: contiguous [{tokens}, {top_k}] of {dtype} on {x.device} expected")
+    L = _lib or lib()
+    keep, ws, nbytes = _workspace(workspace, L.ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, kind)
+                                  if workspace is None else 0, x.device)
+    rc = L.ozimmu_moe(tokens, width, hidden, experts, top_k, kind, int(normalise), x.data_ptr(), ldx, router.data_ptr(), w_in.data_ptr(),
+                      w_out.data_ptr(), chosen.data_ptr(), gates.data_ptr(), out.data_ptr(), ldy, ws, nbytes, ozimmu._stream())
+    if rc != OK:
+        raise OzimmuError(rc, "moe")
+    return out, chosen, gates
