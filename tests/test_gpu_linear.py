@@ -1,0 +1,220 @@
+"""ozimmu_linear and ozimmu_linear_grad against plain 64-bit forms, componentwise within the error of 32-bit sums and one rounding."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2506_11277_amd import layers
+from tests.layers_reference import ROUND, TYPES, U32, act, guarded, product_bound, rounded, slope, sum_bound, untouched, within
+
+# one token ... many, sizes that fit tiles, that miss them by one, and that fit nothing; contractions of nothing, of less than
+# a step, and long enough to be divided among work-groups
+SHAPES = [(1, 1, 1), (1, 1024, 4096), (1, 8192, 33), (2, 0, 40), (7, 64, 16), (16, 65, 15), (17, 2048, 64), (33, 1000, 130), (48, 8192, 260),
+          (64, 127, 129), (65, 128, 128), (128, 128, 128), (129, 63, 257), (200, 4100, 72), (257, 256, 255), (300, 1000, 256),
+          (512, 384, 500), (1531, 1001, 777), (1300, 72, 1288), (2300, 520, 2200)]
+ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+def operands(tokens, n_in, n_out, kind, extra, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    dtype = TYPES[kind]
+
+    def normal(rows, cols, std=1.0):
+        return guarded(rows, cols, cols + extra, dtype, torch.randn(rows, cols, device="cuda", generator=gen).mul_(std))
+
+    x, w = normal(tokens, n_in), normal(n_out, n_in, max(1, n_in) ** -0.5)
+    bias = torch.randn(n_out, device="cuda", generator=gen).to(dtype)
+    return x[0], w[0], bias, normal(tokens, n_out)[0], normal(tokens, n_out)[0]
+
+
+def check_linear(x, w, bias, residual, name, y, pre):
+    dtype = x.dtype
+    X, W = x.double(), w.double()
+    z = torch.matmul(X, W.t()) + (0 if bias is None else bias.double())
+    zb = product_bound(X, W) + 2 * U32 * ((0 if bias is None else bias.double().abs()) + z.abs())
+    if pre is not None:
+        within(pre, z, zb + rounded(z, dtype) + ROUND[dtype] * zb, "pre")
+    a = act(name, z)
+    # the slope of every activation is below 1.13; evaluated in 32 bits, whose exponential is off by a few units times its argument
+    ab = 1.2 * zb + 16 * U32 * (a.abs() + z.abs() * (1 + z.abs()).clamp_max(8))
+    Y = a if residual is None else a + residual.double()
+    ab = ab + 2 * U32 * Y.abs()
+    within(y, Y, ab + rounded(Y, dtype) + ROUND[dtype] * ab, "y")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("extra", [0, 8, 3])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_linear(shape, kind, extra):
+    tokens, n_in, n_out = shape
+    x, w, bias, residual, _ = operands(tokens, n_in, n_out, kind, extra, 100 + n_in)
+    name = ACTS[(tokens + n_out + extra) % 5]
+    (y, ybuf), (pre, pbuf) = (guarded(tokens, n_out, n_out + extra, x.dtype) for _ in range(2))
+    print(shape, kind, extra, name, flush=True)
+    assert layers.linear(x, w, bias, residual, layers.ACTIVATIONS[name], pre=pre, out=y) is y
+    torch.cuda.synchronize()
+    check_linear(x, w, bias, residual, name, y, pre)
+    assert untouched(y, ybuf) and untouched(pre, pbuf)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(3, 200, 100), (300, 200, 100)])
+@pytest.mark.parametrize("name", ACTS)
+def test_linear_without_the_optional_parts_and_in_place(shape, kind, name):
+    x, w, bias, residual, _ = operands(*shape, kind, 0, 7)
+    check_linear(x, w, None, None, name, layers.linear(x, w, activation=layers.ACTIVATIONS[name]), None)
+    stream = residual.clone()
+    y = layers.linear(x, w, bias, stream, layers.ACTIVATIONS[name], out=stream)      # added to in place
+    check_linear(x, w, bias, residual, name, y, None)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("extra", [0, 8, 3])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_linear_grad(shape, kind, extra):
+    tokens, n_in, n_out = shape
+    x, w, bias, dy, z = operands(tokens, n_in, n_out, kind, extra, 200 + n_in)
+    name = ACTS[(tokens + n_out + extra) % 5]
+    dtype, u = x.dtype, ROUND[x.dtype]
+    out = [guarded(tokens, n_in, n_in + extra, dtype), guarded(n_out, n_in, n_in + extra, dtype)]
+    print(shape, kind, extra, name, flush=True)
+    dx, dw, db = layers.linear_grad(dy, x, w, None if name == "none" else z, layers.ACTIVATIONS[name], dx=out[0][0], dw=out[1][0])
+    torch.cuda.synchronize()
+    Z, G = z.double(), dy.double()
+    dz = G * slope(name, Z)
+    # the slope in 32 bits, then one rounding of dz for the products
+    sb = (0 if name in ("none", "relu") else 32 * U32 * G.abs() * (1 + Z.abs()) ** 2)
+    zb = sb + (0 if name == "none" else rounded(dz, dtype))
+    X, W = x.double(), w.double()
+    for got, P, Q, PB, what in ((dx, dz, W.t(), zb, "dx"), (dw, dz.t(), X.t(), zb.t() if torch.is_tensor(zb) else zb, "dw")):
+        want = torch.matmul(P, Q.t())
+        bound = product_bound(P, Q, 2 * U32) + (torch.matmul(PB, Q.abs().t()) if torch.is_tensor(PB) else 0)
+        within(got, want, bound + rounded(want, dtype) + u * bound, what)
+    want = dz.sum(0)
+    bound = dz.abs().sum(0) * sum_bound(tokens) + (sb.sum(0) if torch.is_tensor(sb) else 0)
+    within(db, want, bound + rounded(want, dtype) + u * bound, "db")
+    assert untouched(dx, out[0][1]) and untouched(dw, out[1][1])
+
+
+@pytest.mark.parametrize("name", ACTS)
+def test_linear_grad_against_differences(name):
+    # sum(y * dy) changes by <gradient, direction> h: central differences of the 64-bit form along random directions
+    tokens, n_in, n_out = 37, 45, 29
+    x, w, bias, dy, _ = operands(tokens, n_in, n_out, "f32", 0, 5)
+    pre = torch.empty(tokens, n_out, device="cuda")
+    layers.linear(x, w, bias, None, layers.ACTIVATIONS[name], pre=pre)
+    dx, dw, db = layers.linear_grad(dy, x, w, pre, layers.ACTIVATIONS[name])
+
+    def loss(X, W, B):
+        return float((act(name, torch.matmul(X, W.t()) + B) * dy.double()).sum())
+
+    at, h = (x.double(), w.double(), bias.double()), 1e-6
+    for i, g in enumerate((dx, dw, db)):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(50 + i)
+        d = torch.randn(g.shape, device="cuda", dtype=torch.float64, generator=gen)
+        ends = [loss(*(a + s * h * d if j == i else a for j, a in enumerate(at))) for s in (1, -1)]
+        difference, slope_along = (ends[0] - ends[1]) / (2 * h), float((g.double() * d).sum())
+        # 64-bit sums of about 1e3 differ by 1e-13 times that, over h: 1e-4; relu also bends within h of 0 (none of the 1073 values here is as near)
+        assert abs(difference - slope_along) <= 1e-3 + 1e-5 * float((g.double() * d).abs().sum())
+
+
+def test_linear_grad_forms_what_is_asked_for():
+    x, w, bias, dy, z = operands(130, 70, 90, "bf16", 0, 6)
+    all_ = layers.linear_grad(dy, x, w, z, layers.ACT_GELU)
+    for want in (("dx",), ("dw",), ()):
+        got = layers.linear_grad(dy, x, w, z, layers.ACT_GELU, want=want, bias="dw" not in want)
+        for name, a, b in zip(("dx", "dw", "db"), all_, got):
+            if name in want or (name == "db" and "dw" not in want):
+                assert torch.equal(a, b)
+            else:
+                assert b is None
+
+
+def test_no_tokens():
+    x, w, dy = torch.empty(0, 40, device="cuda"), torch.randn(24, 40, device="cuda"), torch.empty(0, 24, device="cuda")
+    assert layers.linear(x, w).shape == (0, 24)
+    dx, dw, db = layers.linear_grad(dy, x, w)
+    assert dx.shape == (0, 40) and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("tokens", [5, 200])
+def test_infinities_and_nans_stay_in_their_rows(tokens):
+    x, w, bias, residual, _ = operands(tokens, 200, 96, "bf16", 8, 9)
+    want = layers.linear(x, w, bias, residual, layers.ACT_SILU).clone()
+    x[1, 3], x[4, 199] = float("nan"), float("inf")
+    y = layers.linear(x, w, bias, residual, layers.ACT_SILU)
+    assert torch.isnan(y[1]).all() and not torch.isfinite(y[4]).all()
+    keep = [i for i in range(tokens) if i not in (1, 4)]
+    assert torch.equal(y[keep], want[keep])
+
+
+def test_entries_beyond_32_bit_offsets():
+    # a matrix whose rows lie further apart than 2^32 bytes in all
+    ld, rows = (1 << 20) + 8, 2200
+    buf = torch.zeros(rows * ld, dtype=torch.bfloat16, device="cuda")
+    x = buf.view(rows, ld)[:, :136]
+    x.normal_()
+    w = torch.randn(80, 136, device="cuda").bfloat16()
+    y = layers.linear(x, w)
+    check_linear(x, w, None, None, "none", y, None)
+    dx, dw, _ = layers.linear_grad(y, x, w, dx=x.clone())
+    P = y.double()
+    within(dw, torch.matmul(P.t(), x.double()), torch.matmul(P.abs().t(), x.double().abs()) * (sum_bound(rows) + 2.0 ** -8), "dw")
+
+
+def test_other_streams_and_repetition_give_the_same_bits():
+    x, w, bias, residual, dy = operands(300, 2000, 200, "bf16", 0, 11)
+    y = layers.linear(x, w, bias, residual, layers.ACT_GELU)
+    g = layers.linear_grad(dy, x, w, residual, layers.ACT_GELU)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y2 = layers.linear(x, w, bias, residual, layers.ACT_GELU)
+        g2 = layers.linear_grad(dy, x, w, residual, layers.ACT_GELU)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(g, g2))
+
+
+@pytest.mark.parametrize("tokens", [3, 300])
+def test_calls_replay_from_a_captured_graph(tokens):
+    x, w, bias, residual, dy = operands(tokens, 1000, 200, "f16", 0, 12)
+    y, pre = torch.empty_like(residual).contiguous(), torch.empty(tokens, 200, device="cuda", dtype=torch.float16)
+    ws = torch.empty(max(layers.linear_workspace_bytes(tokens, 1000, 200, x.dtype),
+                         layers.linear_grad_workspace_bytes(tokens, 1000, 200, x.dtype, layers.ACT_SILU)) + 256, dtype=torch.uint8, device="cuda")
+    dx, dw, db = torch.empty(tokens, 1000, device="cuda").half(), torch.empty(200, 1000, device="cuda").half(), torch.empty(200, device="cuda").half()
+
+    def both():
+        layers.linear(x, w, bias, residual, layers.ACT_SILU, pre=pre, out=y, workspace=ws)
+        layers.linear_grad(dy, x, w, pre, layers.ACT_SILU, dx=dx, dw=dw, db=db, workspace=ws)
+
+    both()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (y, pre, dx, dw, db)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        for t in (y, pre, dx, dw, db):
+            t.fill_(float("nan"))
+        layers.linear(residual, torch.randn(50, 200, device="cuda").half())      # eager work between the replays
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((y, pre, dx, dw, db), want))
+
+
+def test_the_binding_refuses_operands_that_do_not_fit():
+    x, w = torch.zeros(4, 8, device="cuda"), torch.zeros(6, 8, device="cuda")
+    for call in (lambda: layers.linear(x, w[:, :7]), lambda: layers.linear(x, w.half()), lambda: layers.linear(x.t(), w),
+                 lambda: layers.linear(x, w, bias=torch.zeros(5, device="cuda")), lambda: layers.linear(x, w, residual=x),
+                 lambda: layers.linear(x, w, out=torch.zeros(4, 7, device="cuda")), lambda: layers.linear(x.double(), w.double()),
+                 lambda: layers.linear(x, w.cpu()), lambda: layers.linear_grad(torch.zeros(4, 6, device="cuda"), x, w, None, layers.ACT_RELU),
+                 lambda: layers.linear_grad(torch.zeros(4, 5, device="cuda"), x, w)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(layers.OzimmuError):
+        layers.linear(x, w, activation=17)
