@@ -1,7 +1,7 @@
 // Gradient of the values before the activation, dz = dy * act'(pre), and the bias gradient: the sum of dz over the tokens.
 //
 // Bound by memory: dy and pre are read once, dz is written once; the column sums ride along in registers.  A work-group
-// owns 512 columns of kGradRows tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
+// owns 512 columns of grad_rows() tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
 // work-group of tokens, in a second kernel, always in the same order.
 #include "layers.h"
 
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
     __shared__ float part[4][512];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int c = blockIdx.x * 512 + lane * 8, n = a.n_out - c;
-    const int first = blockIdx.y * kGradRows, last = first + kGradRows < a.tokens ? first + kGradRows : a.tokens;
+    const int first = blockIdx.y * a.rows, last = first + a.rows < a.tokens ? first + a.rows : a.tokens;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (n > 0)
 #pragma unroll 2
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
             if (a.act) {
                 load8((const T *)a.pre + (size_t)r * a.ldpre + c, n, a.wide, z);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= activation_slope(a.act, z[i]);
+                for (int i = 0; i < 8; ++i) d[i] *= activation_slope<T>(a.act, z[i]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += d[i];
@@ -57,26 +57,30 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
 }
 
 template <class T>
-__global__ __launch_bounds__(64) void bias_grad_kernel(const float *sums, int rows, int n, T *db)
+__global__ __launch_bounds__(256) void bias_grad_kernel(const float *sums, int rows, int n, T *db)
 {
-    const int c = blockIdx.x * 64 + threadIdx.x;
-    if (c >= n) return;
+    __shared__ float part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     float s = 0.0f;
-    for (int r = 0; r < rows; ++r) s += sums[(size_t)r * n + c];
-    db[c] = (T)s;
+    if (c < n)
+#pragma unroll 8
+        for (int r = wave; r < rows; r += 4) s += sums[(size_t)r * n + c];
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < n) db[c] = (T)((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
 }
 
 template <class T>
 hipError_t launch(const GradInput &g, hipStream_t st)
 {
-    const int rows = (g.tokens + kGradRows - 1) / kGradRows;
-    if (rows > 65535) return hipErrorInvalidValue;
-    if (rows > 0) {
-        grad_input_kernel<T><<<dim3((g.n_out + 511) / 512, rows), 256, 0, st>>>(g);
+    const int groups = (g.tokens + g.rows - 1) / g.rows;
+    if (groups > 65535) return hipErrorInvalidValue;
+    if (groups > 0) {
+        grad_input_kernel<T><<<dim3((g.n_out + 511) / 512, groups), 256, 0, st>>>(g);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (g.db) {
-        bias_grad_kernel<T><<<(g.n_out + 63) / 64, 64, 0, st>>>(g.sums, rows, g.n_out, (T *)g.db);
+        bias_grad_kernel<T><<<(g.n_out + 63) / 64, 256, 0, st>>>(g.sums, groups, g.n_out, (T *)g.db);
         return hipGetLastError();
     }
     return hipSuccess;

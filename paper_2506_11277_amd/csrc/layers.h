@@ -17,13 +17,22 @@ hipError_t launch_product_f16(const Product &a, const ProductPlan &plan, float *
 hipError_t launch_product_f32(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
 
 // dz = dy * act'(pre) and the sums of its columns (grad.hip)
-constexpr int kGradRows = 64;              // tokens a work-group sums
+// Tokens a work-group sums: 64, fewer where that leaves fewer than 1024 work-groups, at least two a wavefront, more where
+// the grid would grow beyond its limit.
+inline int grad_rows(int tokens, int n_out)
+{
+    const long long strips = (n_out + 511) / 512;
+    int rows = 64;
+    while (rows > 8 && strips * ((tokens + rows - 1) / rows) < 1024) rows /= 2;
+    while ((tokens + rows - 1) / rows > 65535) rows *= 2;
+    return rows;
+}
 struct GradInput {
     const void *dy, *pre;                  // pre may be null (no activation)
     void *dz;                              // null: only the sums
     void *db;                              // null: no sums
-    float *sums;                           // [ceil(tokens / kGradRows)][n_out]
-    int lddy, ldpre, lddz, tokens, n_out, act, wide;
+    float *sums;                           // [ceil(tokens / rows)][n_out]
+    int lddy, ldpre, lddz, tokens, n_out, rows, act, wide;
 };
 hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st);
 

@@ -25,7 +25,7 @@ ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows)
         const double tiles = (double)((np + edge[t] - 1) / edge[t]) * ((nq + edge[t] - 1) / edge[t]);
         for (int s = 1; s <= 16 && (s == 1 || all / s >= 4); s *= 2) {
             const double groups = tiles * s;
-            const double rounds = groups <= 256 ? 1.0 : groups / 256 + 0.5;
+            const double rounds = __builtin_ceil(groups / 256);
             const int steps = (all + s - 1) / s;
             // in units of a step of a 64 x 64 tile; each work-group has a start and an end, a join reads the parts
             const double cost = rounds * (edge[t] / 64) * (edge[t] / 64) / rate[t] * (steps + 4) + (s > 1 ? 24 + (double)np * nq * s / (64 * 64 * 64) : 0);
@@ -88,7 +88,7 @@ GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int acti
     GradWorkspace w{};
     w.lddz = (n_out + 7) & ~7;
     w.sums = activation == OZIMMU_ACT_NONE ? 0 : padded((size_t)tokens * w.lddz * element_bytes(type));
-    w.partial = w.sums + padded((size_t)((tokens + kGradRows - 1) / kGradRows) * n_out * 4);
+    w.partial = w.sums + padded((size_t)((tokens + grad_rows(tokens, n_out) - 1) / grad_rows(tokens, n_out)) * n_out * 4);
     const size_t dx = product_partial_bytes(n_in, tokens, plan_product(n_in, tokens, n_out, type, false));
     const size_t dw = product_partial_bytes(n_in, n_out, plan_product(n_in, n_out, tokens, type, false));
     w.total = w.partial + padded(dx > dw ? dx : dw);
@@ -168,6 +168,7 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
         g.lddz = ws.lddz;
         g.tokens = tokens;
         g.n_out = n_out;
+        g.rows = grad_rows(tokens, n_out);
         g.act = activation;
         g.wide = on16(dy, lddy, size) && (!activation || on16(pre, ldpre, size));
         if (launch_grad_input(g, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;

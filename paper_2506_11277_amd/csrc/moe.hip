@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
                 u += sums[s][1][q * kStreamLd + f];
             }
             const int choice = choices[c0 + q];
-            ((T *)a.h)[(size_t)choice * a.ldh + f0 + f] = (T)(a.gates[choice] * activate(OZIMMU_ACT_SILU, g) * u);
+            ((T *)a.h)[(size_t)choice * a.ldh + f0 + f] = (T)(a.gates[choice] * activate<T>(OZIMMU_ACT_SILU, g) * u);
         }
         __syncthreads();
     }

@@ -23,10 +23,41 @@ namespace oz {
 
 __device__ __attribute__((aligned(16))) const unsigned kZeroChunk[4] = {0, 0, 0, 0};
 
+__device__ __forceinline__ void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // 16 bytes per lane, any global address -> LDS (ldsaddr + lane * 16)
 __device__ __forceinline__ void lds_dma16_any(const void *p, unsigned ldsaddr)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(ldsaddr), "v"(p) : "memory", "m0");
+}
+
+// c += p q as mma(), in place and where the order in the source puts it.  (The builtin lets the register allocator move
+// accumulators about when they take half of all registers: 184 moves in a step of 128 instructions, 758 us instead of 490 for
+// 8192 x 4096 x 8192.)  ACC: c in accumulator registers, else in ordinary ones: not all of the former are used, or the
+// allocator has none to spare.  settle() has to follow before anything else reads c.
+template <bool ACC>
+__device__ __forceinline__ void mma_in_place(v4u p, v4u q, v4f &c, bf16)
+{
+    if constexpr (ACC) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(p), "v"(q));
+    else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(p), "v"(q));
+}
+template <bool ACC>
+__device__ __forceinline__ void mma_in_place(v4u p, v4u q, v4f &c, f16)
+{
+    if constexpr (ACC) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(p), "v"(q));
+    else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(p), "v"(q));
+}
+// the wait states between a matrix instruction and another use of its result, which the compiler does not see through the asm
+template <bool ACC, int N>
+__device__ __forceinline__ void settle(v4f (&c)[N])
+{
+    static_assert(N == 8, "");
+    if constexpr (ACC)
+        asm volatile("s_nop 15\n\ts_nop 15"
+                     : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]), "+a"(c[4]), "+a"(c[5]), "+a"(c[6]), "+a"(c[7]));
+    else
+        asm volatile("s_nop 15\n\ts_nop 15"
+                     : "+v"(c[0]), "+v"(c[1]), "+v"(c[2]), "+v"(c[3]), "+v"(c[4]), "+v"(c[5]), "+v"(c[6]), "+v"(c[7]));
 }
 
 template <class T, int BP, int BQ, int WP, int WQ>
@@ -34,9 +65,11 @@ struct ProductShape {
     static constexpr int kWaves = WP * WQ, kThreads = 64 * kWaves;
     static constexpr int kStage = (BP + BQ) * 128;
     static constexpr int kPW = BP / WP, kQW = BQ / WQ;                  // a wavefront's part of the tile
-    static constexpr int kStripLd = kPW + 4;                            // floats; epilogue strip of 16 q a wavefront
-    static constexpr int kStrip = kWaves * 16 * kStripLd * 4;
-    static constexpr int kLds = 2 * kStage > kStrip ? 2 * kStage : kStrip;
+    static constexpr bool kAlone = kPW == 128 && kQW == 128;            // one wavefront per SIMD
+    static constexpr int kSQ = kQW < 64 ? kQW : 64;                     // epilogue: q of a wavefront's part at a time
+    static constexpr int kSumsLd = kPW + 4, kSums = kSQ * kSumsLd * 4;
+    static constexpr int kLds = 2 * kStage > kWaves * kSums ? 2 * kStage : kWaves * kSums;
+    static_assert(kLds <= kLdsBytes, "LDS");
 };
 
 // One operand of the tile: where its chunks come from and where they go in LDS.
@@ -117,6 +150,13 @@ struct Operand {
         }
     }
 
+    // one of the N copies of a step that lies before nk; from = at(its k)
+    template <int I>
+    __device__ __forceinline__ void copy_one(const T *from, unsigned lds, int wave)
+    {
+        lds_dma16(from, off[I], lds + (I * WAVES + wave) * 1024);
+    }
+
     __device__ __forceinline__ void load(int k0, int wave, int lane)
     {
 #pragma unroll
@@ -138,46 +178,124 @@ struct Operand {
         for (int i = 0; i < N; ++i) *(v4u *)(lds + ((i * WAVES + wave) * 64 + lane) * 16) = reg[i];
     }
 
-    // the operand of rows w0 + 16 f ... + 15 (w0: a wavefront's part, a multiple of 32), half s of the step
-    static __device__ __forceinline__ v4u fragment(const char *lds, int w0, int f, int s, int lane)
+    // Where a lane finds its operands in a stage: fragment() of rows w0 + 16 f ... + 15 (w0: a wavefront's part, a multiple of
+    // 32) and half h of a step is read from `from`, which is reader() behind the operand's place in LDS (a multiple of 1 KB); f
+    // and the swizzle meet in one exclusive or.
+    static __device__ __forceinline__ unsigned reader(int w0, int lane)
     {
         const int r = lane & 15, g = lane >> 4;
+        if constexpr (K_ROWS) return (w0 + r) * 128 + ((g ^ twist(r)) << 4);
+        else if constexpr (sizeof(T) == 2) {
+            const int k = 8 * g + (r >> 2);
+            return k * kRowBytes + (((w0 >> 4) ^ (twist(k) >> 1)) << 5) + (r & 3) * 8;
+        } else return 4 * g * kRowBytes + ((((w0 + r) >> 2) ^ twist(4 * g)) << 4) + (r & 3) * 4;
+    }
+    static __device__ __forceinline__ v4u fragment(unsigned from, int f, int h)
+    {
         if constexpr (K_ROWS) {
-            const int row = w0 + 16 * f + r;
-            return *(const v4u *)(lds + row * 128 + ((((4 * s + g) ^ ((r >> 1) & 7))) << 4));
+            return *(const __attribute__((address_space(3))) v4u *)((from ^ (h << 6)) + f * 2048);
         } else if constexpr (sizeof(T) == 2) {
             typedef short v4s __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) v4s lds_v4s;
-            const int k = 32 * s + 8 * g + (r >> 2);
-            const int unit = ((w0 >> 4) + f) ^ (twist(k) >> 1);
-            const char *p = lds + k * kRowBytes + unit * 32 + (r & 3) * 8;
-            union { v4s h[2]; v4u v; } u;
-            u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)p);
-            u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(p + 4 * kRowBytes));
-            return u.v;
+            const unsigned at = (from ^ (f << 5)) + h * 32 * kRowBytes;
+            const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)at), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s *)(at + 4 * kRowBytes));
+            const v2u a = __builtin_bit_cast(v2u, x), b = __builtin_bit_cast(v2u, y);
+            return v4u{a[0], a[1], b[0], b[1]};
         } else {
-            const int col = w0 + 16 * f + r;
+            const unsigned at = (from ^ (f << 6)) + h * 16 * kRowBytes;
             v4u v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = 16 * s + 4 * g + i;
-                v[i] = *(const unsigned *)(lds + k * kRowBytes + (((col >> 2) ^ twist(k)) << 4) + (col & 3) * 4);
-            }
+            for (int i = 0; i < 4; ++i) v[i] = *(const __attribute__((address_space(3))) unsigned *)(at + i * kRowBytes);
             return v;
         }
     }
 };
+
+// Epilogue of a wavefront's part of the tile: its sums pass through LDS, 64 q of it at a time (a loop over them with the
+// accumulators in registers would have to pick them by number, which puts them in memory), so that a lane has 8
+// entries along p of a row, always of the same columns: its bias is loaded once.
+template <class T, int PW>
+__device__ __forceinline__ void load_bias(const Epilogue &e, int p0, int lane, float (&bias)[8])
+{
+    const int p = p0 + lane % (PW / 8) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+    if (e.bias && e.wide && p + 8 <= e.np) load_row((const T *)e.bias + p, bias);
+}
+
+// rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time
+template <class T, int ACT, int PW, int QW>
+__device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
+{
+    constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, R = QW / ROWS < 4 ? QW / ROWS : 4;
+    static_assert(QW % (ROWS * R) == 0, "");
+    const int col = lane % LANES * 8, p = p0 + col;
+    if (p >= e.np) return;
+    const bool whole = e.wide && p + 8 <= e.np;
+#pragma nounroll
+    for (int s = lane / LANES; s < QW && q0 + s < e.nq; s += R * ROWS) {
+        float v[R][8], res[R][8];
+#pragma unroll
+        for (int y = 0; y < R; ++y)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[y][i] = sums[(s + y * ROWS) * LD + col + i];
+        if (partial) {
+            // (partial sums: rows of np rounded up to 8 floats, so that they are written whole)
+            const int ldn = (e.np + 7) & ~7;
+#pragma unroll
+            for (int y = 0; y < R; ++y)
+                if (q0 + s + y * ROWS < e.nq) store_row(partial + ((size_t)blockIdx.y * e.nq + q0 + s + y * ROWS) * ldn + p, v[y]);
+            continue;
+        }
+        if (!whole) {
+#pragma unroll
+            for (int y = 0; y < R; ++y)
+                if (q0 + s + y * ROWS < e.nq) finish_row<T>(e, q0 + s + y * ROWS, p, v[y]);
+            continue;
+        }
+        if (e.residual)
+#pragma unroll
+            for (int y = 0; y < R; ++y)
+                if (q0 + s + y * ROWS < e.nq) load_row((const T *)e.residual + (size_t)(q0 + s + y * ROWS) * e.ldr + p, res[y]);
+#pragma unroll
+        for (int y = 0; y < R; ++y) {
+            const int q = q0 + s + y * ROWS;
+            if (q >= e.nq) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[y][i] += bias[i];
+            if (e.pre) store_row((T *)e.pre + (size_t)q * e.ldpre + p, v[y]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[y][i] = activate<T>(ACT, v[y][i]);
+            if (e.residual)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[y][i] += res[y][i];
+            store_row((T *)e.out + (size_t)q * e.ldo + p, v[y]);
+        }
+    }
+}
+
+template <class T, int PW, int QW>
+__device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
+{
+    switch (e.act) {                                // (decided once: a lane's entries decide nothing)
+        case OZIMMU_ACT_RELU: return epilogue_rows<T, OZIMMU_ACT_RELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU: return epilogue_rows<T, OZIMMU_ACT_GELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU_TANH: return epilogue_rows<T, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_SILU: return epilogue_rows<T, OZIMMU_ACT_SILU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+    }
+    epilogue_rows<T, OZIMMU_ACT_NONE, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+}
 
 template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT>
 __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float *partial, int steps_per_split, int tiles_p, int tiles_q)
 {
     using S = ProductShape<T, BP, BQ, WP, WQ>;
     constexpr int FP = S::kPW / 16, FQ = S::kQW / 16, KE = 8 * Chunk<T>::E;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wp = wave % WP * S::kPW, wq = wave / WP * S::kQW;
     int tq, tp;
     if (!tile_of_block_xcd(blockIdx.x, tiles_q, tiles_p, false, tq, tp)) return;
-    const int wp = wave % WP * S::kPW, wq = wave / WP * S::kQW;
 
     Operand<T, PK, BP, S::kWaves, DIRECT> P;
     Operand<T, QK, BQ, S::kWaves, DIRECT> Q;
@@ -186,49 +304,140 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
     v4f acc[FP][FQ];
+    auto clear = [&]() {
 #pragma unroll
-    for (int i = 0; i < FP; ++i)
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
-        for (int j = 0; j < FQ; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+            for (int j = 0; j < FQ; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+    };
 
     const int all = (a.nk + KE - 1) / KE;
     const int t0 = (int)blockIdx.y * steps_per_split, t1 = all < t0 + steps_per_split ? all : t0 + steps_per_split;
 
-    auto products = [&](const char *stage) {
+    v4u p[2][FP], q[2][FQ];                         // operands of the two halves of a step
+    const unsigned pbase = lds0 + P.reader(wp, lane), qbase = lds0 + BP * 128 + Q.reader(wq, lane);
+    // (hidden from the optimiser, which otherwise keeps every fragment's address in a register of its own)
+    auto in_stage = [&](unsigned base, int stage) __attribute__((always_inline)) {
+        unsigned from = base + stage * S::kStage;
+        asm volatile("" : "+v"(from));
+        return from;
+    };
+    auto read = [&](int stage, auto H) __attribute__((always_inline)) {
+        const unsigned fp = in_stage(pbase, stage), fq = in_stage(qbase, stage);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            v4u p[FP], q[FQ];
+        for (int j = 0; j < FQ; ++j) q[H][j] = Q.fragment(fq, j, H);
 #pragma unroll
-            for (int j = 0; j < FQ; ++j) q[j] = Q.fragment(stage + BP * 128, wq, j, s, lane);
+        for (int i = 0; i < FP; ++i) p[H][i] = P.fragment(fp, i, H);
+    };
+    auto products = [&](auto H) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < FP; ++i) p[i] = P.fragment(stage, wp, i, s, lane);
+        for (int i = 0; i < FP; ++i)
 #pragma unroll
-            for (int i = 0; i < FP; ++i)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) acc[i][j] = mma(p[i], q[j], acc[i][j], T{});
-        }
+            for (int j = 0; j < FQ; ++j) acc[i][j] = mma(p[H][i], q[H][j], acc[i][j], T{});
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, 1> second{};
+
+    auto copy = [&](int t, int stage) __attribute__((always_inline)) {
+        P.copy(t * KE, lds0 + stage * S::kStage, wave, lane);
+        Q.copy(t * KE, lds0 + stage * S::kStage + BP * 128, wave, lane);
     };
 
-    if (t0 < t1) {
+    if constexpr (DIRECT && S::kAlone) {
+        // One wavefront per SIMD: nothing but its own matrix instructions hides its reads, so every read and copy has its place
+        // among them.  While the products of a half step run, the operands of the other half are read, three reads to a row of
+        // eight instructions; behind the barrier in the middle of a step its second half's operands are in registers, so
+        // the copies of the step after the next take its stage, two to a row (more at once wait for each other in the
+        // address unit, and the wavefront with them: 437 us against 472).
+        constexpr std::integral_constant<bool, true> reads{};
+        constexpr std::integral_constant<bool, false> none{};
+        auto half = [&](auto H, auto READ, int stage, auto &&copies) __attribute__((always_inline)) {
+            constexpr int O = 1 - H;
+            const unsigned fp = in_stage(pbase, stage), fq = in_stage(qbase, stage);
+            static_for<0, FP>([&](auto I) __attribute__((always_inline)) {
+                if constexpr (READ)
+                    static_for<3 * I, 3 * I + 3>([&](auto R) __attribute__((always_inline)) {
+                        if constexpr (R < FQ) q[O][R] = Q.fragment(fq, R, O);
+                        else if constexpr (R < FQ + FP) p[O][R - FQ] = P.fragment(fp, R - FQ, O);
+                    });
+                copies(I);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) mma_in_place<(I < FP - 1)>(p[H][I], q[H][j], acc[I][j], T{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        auto nothing = [](auto) __attribute__((always_inline)) {};
+        copy(t0, 0);                                // (every part of the contraction has a step)
+        if (t0 + 1 < t1) {
+            copy(t0 + 1, 1);
+            wait_vmcnt<P.N + Q.N>();
+        } else {
+            wait_vmcnt<0>();
+        }
+        __syncthreads();
+        clear();
+        read(0, first);
+        int t = t0, now = 0;
+        // (steps whose next but one is there and whole)
+        const int whole = a.nk / KE < t1 ? a.nk / KE : t1;
+        for (int left = whole - 2 - t0; left > 0; --left, ++t, now ^= 1) {
+            half(first, reads, now, nothing);
+            wait_vmcnt<0>();
+            __syncthreads();
+            const T *from_p = P.at((t + 2) * KE), *from_q = Q.at((t + 2) * KE);
+            const unsigned to = lds0 + now * S::kStage;
+            half(second, reads, now ^ 1, [&](auto I) __attribute__((always_inline)) {
+                static_for<2 * I, 2 * I + 2>([&](auto C) __attribute__((always_inline)) {
+                    if constexpr (C < P.N) P.template copy_one<C>(from_p, to, wave);
+                    else if constexpr (C < P.N + Q.N) Q.template copy_one<C - P.N>(from_q, to + BP * 128, wave);
+                });
+            });
+        }
+        for (; t + 1 < t1; ++t, now ^= 1) {
+            half(first, reads, now, nothing);
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (t + 2 < t1) copy(t + 2, now);
+            half(second, reads, now ^ 1, nothing);
+        }
+        half(first, reads, now, nothing);
+        wait_lgkm();                        // (the operands of the last half, before another wavefront's copies of the next tile)
+        __syncthreads();
+        half(second, none, 0, nothing);
+        static_for<0, FP>([&](auto I) __attribute__((always_inline)) { settle<(I < FP - 1)>(acc[I]); });
+    } else {
+        clear();
         if constexpr (DIRECT) {
-            P.copy(t0 * KE, lds0, wave, lane);
-            Q.copy(t0 * KE, lds0 + BP * 128, wave, lane);
+            if (t0 < t1) {
+                copy(t0, 0);
+                if (t0 + 1 < t1) {
+                    copy(t0 + 1, 1);
+                    wait_vmcnt<P.N + Q.N>();
+                } else {
+                    wait_vmcnt<0>();
+                }
+                __syncthreads();
+                read(0, first);
+            }
             for (int t = t0; t < t1; ++t) {
                 const int now = (t - t0) & 1;
+                read(now, second);
+                products(first);
+                // the next step's copies are there, and nobody reads this step's stage any more
                 wait_vmcnt<0>();
-                __syncthreads();                    // the step's copies are there, and nobody reads the other stage any more
-                if (t + 1 < t1) {
-                    const unsigned to = lds0 + (now ^ 1) * S::kStage;
-                    P.copy((t + 1) * KE, to, wave, lane);
-                    Q.copy((t + 1) * KE, to + BP * 128, wave, lane);
-                }
-                products(lds + now * S::kStage);
+                __syncthreads();
+                if (t + 2 < t1) copy(t + 2, now);
+                if (t + 1 < t1) read(now ^ 1, first);
+                products(second);
             }
         } else {
-            P.load(t0 * KE, wave, lane);
-            Q.load(t0 * KE, wave, lane);
-            P.store(lds, wave, lane);
-            Q.store(lds + BP * 128, wave, lane);
+            if (t0 < t1) {
+                P.load(t0 * KE, wave, lane);
+                Q.load(t0 * KE, wave, lane);
+                P.store(lds, wave, lane);
+                Q.store(lds + BP * 128, wave, lane);
+            }
             for (int t = t0; t < t1; ++t) {
                 const int now = (t - t0) & 1;
                 __syncthreads();
@@ -236,7 +445,10 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
                     P.load((t + 1) * KE, wave, lane);
                     Q.load((t + 1) * KE, wave, lane);
                 }
-                products(lds + now * S::kStage);
+                read(now, first);
+                read(now, second);
+                products(first);
+                products(second);
                 if (t + 1 < t1) {
                     char *to = lds + (now ^ 1) * S::kStage;
                     P.store(to, wave, lane);
@@ -245,42 +457,26 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
             }
         }
     }
-
-    // Epilogue: 16 q of a wavefront's part at a time pass through LDS, so that a lane has 8 entries along p.
-    __syncthreads();
-    float *strip = (float *)lds + wave * 16 * S::kStripLd;
+    const int q0 = tq * BQ + wq, p0 = tp * BP + wp;
+    float bias[8];
+    load_bias<T, S::kPW>(a.e, p0, lane, bias);
+    __syncthreads();                                // (the sums take the stages' place)
+    float *sums = (float *)(lds + wave * S::kSums);
     const int r = lane & 15, g = lane >> 4;
-    constexpr int kRowLanes = S::kPW / 8, kRows = 64 / kRowLanes;
-    static_assert(16 % kRows == 0, "");
-    for (int jj = 0; jj < FQ; ++jj) {
-        static_for<0, FQ>([&](auto J) {
-            if (J == jj)
+#pragma nounroll
+    for (int h = 0; h < S::kQW / S::kSQ; ++h) {
+        static_for<0, S::kQW / S::kSQ>([&](auto X) __attribute__((always_inline)) {
+            if (X == h) {
 #pragma unroll
-                for (int i = 0; i < FP; ++i) *(v4f *)(strip + r * S::kStripLd + 16 * i + 4 * g) = acc[i][J];
+                for (int j = 0; j < S::kSQ / 16; ++j)
+#pragma unroll
+                    for (int i = 0; i < FP; ++i) *(v4f *)(sums + (16 * j + r) * S::kSumsLd + 16 * i + 4 * g) = acc[i][X * (S::kSQ / 16) + j];
+                // (unlike in either branch: or the last stores become one, from an address, and the sums go to memory for it)
+                asm volatile("; part %0" ::"n"((int)X));
+            }
         });
         __builtin_amdgcn_wave_barrier();
-#pragma nounroll
-        for (int y = 0; y < 16; y += kRows) {
-            const int row = y + lane / kRowLanes, col = lane % kRowLanes * 8;
-            const int q = tq * BQ + wq + 16 * jj + row, p = tp * BP + wp + col;
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const v4f x = *(const v4f *)(strip + row * S::kStripLd + col + 4 * i);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) v[4 * i + c] = x[c];
-            }
-            if (q >= a.e.nq || p >= a.e.np) continue;
-            if (partial) {
-                // (partial sums: rows of np rounded up to 8 floats, so that they are written whole)
-                const int ldn = (a.e.np + 7) & ~7;
-                float *to = partial + ((size_t)blockIdx.y * a.e.nq + q) * ldn + p;
-                *(v4f *)to = v4f{v[0], v[1], v[2], v[3]};
-                *(v4f *)(to + 4) = v4f{v[4], v[5], v[6], v[7]};
-            } else {
-                finish_row<T>(a.e, q, p, v);
-            }
-        }
+        epilogue<T, S::kPW, S::kSQ>(a.e, partial, bias, sums, q0 + h * S::kSQ, p0, lane);
         __builtin_amdgcn_wave_barrier();
     }
 }
@@ -326,7 +522,7 @@ hipError_t launch_product_order(const Product &a, const ProductPlan &plan, float
 {
     if (plan.direct) {
         if constexpr (sizeof(T) == 2)
-            if (plan.tile == 0) return launch_product_shape<T, PK, QK, 256, 256, 2, 4, true>(a, plan, partial, st);
+            if (plan.tile == 0) return launch_product_shape<T, PK, QK, 256, 256, 2, 2, true>(a, plan, partial, st);
         if (plan.tile == 1) return launch_product_shape<T, PK, QK, 128, 128, 2, 2, true>(a, plan, partial, st);
         return launch_product_shape<T, PK, QK, 64, 64, 2, 2, true>(a, plan, partial, st);
     }
