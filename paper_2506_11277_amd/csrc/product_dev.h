@@ -23,41 +23,52 @@ namespace oz {
 
 __device__ __attribute__((aligned(16))) const unsigned kZeroChunk[4] = {0, 0, 0, 0};
 
-__device__ __forceinline__ void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
 // 16 bytes per lane, any global address -> LDS (ldsaddr + lane * 16)
 __device__ __forceinline__ void lds_dma16_any(const void *p, unsigned ldsaddr)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(ldsaddr), "v"(p) : "memory", "m0");
 }
 
-// c += p q as mma(), in place and where the order in the source puts it.  (The builtin lets the register allocator move
-// accumulators about when they take half of all registers: 184 moves in a step of 128 instructions, 758 us instead of 490 for
-// 8192 x 4096 x 8192.)  ACC: c in accumulator registers, else in ordinary ones: not all of the former are used, or the
-// allocator has none to spare.  settle() has to follow before anything else reads c.
+// c[j] += p q[j] as mma(), in place and where the order in the source puts it.  (The builtin lets the register allocator move
+// accumulators about: 184 moves in a step of 128 instructions and 758 us instead of 490 for 8192 x 4096 x 8192 with 256 x 256
+// tiles, 110 moves in a step of 32 with 128 x 128.)  ACC: c in accumulator registers, else in ordinary ones; the
+// largest tile takes both, so that the allocator has some of either to spare.  settle() has to follow before anything else
+// reads c, and the same c is not used again within the next instruction.
 template <bool ACC>
-__device__ __forceinline__ void mma_in_place(v4u p, v4u q, v4f &c, bf16)
+__device__ __forceinline__ void mma_one(v4u p, v4u q, v4f &c, bf16)
 {
     if constexpr (ACC) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(p), "v"(q));
     else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(c) : "v"(p), "v"(q));
 }
 template <bool ACC>
-__device__ __forceinline__ void mma_in_place(v4u p, v4u q, v4f &c, f16)
+__device__ __forceinline__ void mma_one(v4u p, v4u q, v4f &c, f16)
 {
     if constexpr (ACC) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(p), "v"(q));
     else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(p), "v"(q));
+}
+template <bool ACC, class T, int FQ>
+__device__ __forceinline__ void mma_row(v4u p, const v4u (&q)[FQ], v4f (&c)[FQ])
+{
+    static_assert(FQ >= 2, "");
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) mma_one<ACC>(p, q[j], c[j], T{});
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j) asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c[j]) : "v"(p[e]), "v"(q[j][e]));
+    }
 }
 // the wait states between a matrix instruction and another use of its result, which the compiler does not see through the asm
 template <bool ACC, int N>
 __device__ __forceinline__ void settle(v4f (&c)[N])
 {
-    static_assert(N == 8, "");
-    if constexpr (ACC)
-        asm volatile("s_nop 15\n\ts_nop 15"
-                     : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]), "+a"(c[4]), "+a"(c[5]), "+a"(c[6]), "+a"(c[7]));
-    else
-        asm volatile("s_nop 15\n\ts_nop 15"
-                     : "+v"(c[0]), "+v"(c[1]), "+v"(c[2]), "+v"(c[3]), "+v"(c[4]), "+v"(c[5]), "+v"(c[6]), "+v"(c[7]));
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+        if constexpr (ACC) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c[j]), "+a"(c[j + 1]));
+        else asm volatile("s_nop 15\n\ts_nop 15" : "+v"(c[j]), "+v"(c[j + 1]));
+    }
 }
 
 template <class T, int BP, int BQ, int WP, int WQ>
@@ -68,7 +79,8 @@ struct ProductShape {
     static constexpr bool kAlone = kPW == 128 && kQW == 128;            // one wavefront per SIMD
     static constexpr int kSQ = kQW < 64 ? kQW : 64;                     // epilogue: q of a wavefront's part at a time
     static constexpr int kSumsLd = kPW + 4, kSums = kSQ * kSumsLd * 4;
-    static constexpr int kLds = 2 * kStage > kWaves * kSums ? 2 * kStage : kWaves * kSums;
+    static constexpr int kStages = kAlone ? 2 : 4;
+    static constexpr int kLds = kStages * kStage > kWaves * kSums ? kStages * kStage : kWaves * kSums;
     static_assert(kLds <= kLdsBytes, "LDS");
 };
 
@@ -343,12 +355,14 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
         Q.copy(t * KE, lds0 + stage * S::kStage + BP * 128, wave, lane);
     };
 
-    if constexpr (DIRECT && S::kAlone) {
-        // One wavefront per SIMD: nothing but its own matrix instructions hides its reads, so every read and copy has its place
-        // among them.  While the products of a half step run, the operands of the other half are read, three reads to a row of
-        // eight instructions; behind the barrier in the middle of a step its second half's operands are in registers, so
-        // the copies of the step after the next take its stage, two to a row (more at once wait for each other in the
-        // address unit, and the wavefront with them: 437 us against 472).
+    clear();
+    if constexpr (DIRECT) {
+        // With one to two wavefronts per SIMD little but a wavefront's own matrix instructions hides its reads, so every read and
+        // copy has its place among them.  While the products of a half step run, the operands of the other half are read,
+        // three reads to a row of instructions; behind the barrier in the middle of a step its second half's operands are in
+        // registers, so the copies of the step kStages on take its stage, two to a row (more at once wait for each other in the
+        // address unit, and the wavefront with them: 472 us instead of 437 with 256 x 256 tiles).
+        constexpr int R = S::kStages, L = P.N + Q.N;                    // L: copies of a step
         constexpr std::integral_constant<bool, true> reads{};
         constexpr std::integral_constant<bool, false> none{};
         auto half = [&](auto H, auto READ, int stage, auto &&copies) __attribute__((always_inline)) {
@@ -356,104 +370,79 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
             const unsigned fp = in_stage(pbase, stage), fq = in_stage(qbase, stage);
             static_for<0, FP>([&](auto I) __attribute__((always_inline)) {
                 if constexpr (READ)
-                    static_for<3 * I, 3 * I + 3>([&](auto R) __attribute__((always_inline)) {
-                        if constexpr (R < FQ) q[O][R] = Q.fragment(fq, R, O);
-                        else if constexpr (R < FQ + FP) p[O][R - FQ] = P.fragment(fp, R - FQ, O);
+                    static_for<3 * I, 3 * I + 3>([&](auto X) __attribute__((always_inline)) {
+                        if constexpr (X < FQ) q[O][X] = Q.fragment(fq, X, O);
+                        else if constexpr (X < FQ + FP) p[O][X - FQ] = P.fragment(fp, X - FQ, O);
                     });
                 copies(I);
                 __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) mma_in_place<(I < FP - 1)>(p[H][I], q[H][j], acc[I][j], T{});
+                mma_row<(S::kAlone && I < FP - 1), T>(p[H][I], q[H], acc[I]);
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
+        static_assert(3 * FP >= FP + FQ && L == 2 * FP, "reads and copies of a step");
         auto nothing = [](auto) __attribute__((always_inline)) {};
-        copy(t0, 0);                                // (every part of the contraction has a step)
-        if (t0 + 1 < t1) {
-            copy(t0 + 1, 1);
-            wait_vmcnt<P.N + Q.N>();
-        } else {
-            wait_vmcnt<0>();
-        }
+        // (every part of the contraction has a step)
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (t0 + i < t1) copy(t0 + i, i);
+        if (t0 + R <= t1) wait_vmcnt<(R - 1) * L>();
+        else wait_vmcnt<0>();
         __syncthreads();
-        clear();
         read(0, first);
         int t = t0, now = 0;
-        // (steps whose next but one is there and whole)
+        // (steps whose R-th next is there and whole)
         const int whole = a.nk / KE < t1 ? a.nk / KE : t1;
-        for (int left = whole - 2 - t0; left > 0; --left, ++t, now ^= 1) {
+        for (int left = whole - R - t0; left > 0; --left, ++t) {
+            const int next = now + 1 == R ? 0 : now + 1;
             half(first, reads, now, nothing);
-            wait_vmcnt<0>();
+            // the next step's copies are there, and nobody reads this step's stage any more
+            wait_vmcnt<(R - 2) * L>();
             __syncthreads();
-            const T *from_p = P.at((t + 2) * KE), *from_q = Q.at((t + 2) * KE);
+            const T *from_p = P.at((t + R) * KE), *from_q = Q.at((t + R) * KE);
             const unsigned to = lds0 + now * S::kStage;
-            half(second, reads, now ^ 1, [&](auto I) __attribute__((always_inline)) {
+            half(second, reads, next, [&](auto I) __attribute__((always_inline)) {
                 static_for<2 * I, 2 * I + 2>([&](auto C) __attribute__((always_inline)) {
                     if constexpr (C < P.N) P.template copy_one<C>(from_p, to, wave);
-                    else if constexpr (C < P.N + Q.N) Q.template copy_one<C - P.N>(from_q, to + BP * 128, wave);
+                    else if constexpr (C < L) Q.template copy_one<C - P.N>(from_q, to + BP * 128, wave);
                 });
             });
+            now = next;
         }
-        for (; t + 1 < t1; ++t, now ^= 1) {
+        for (; t + 1 < t1; ++t) {
+            const int next = now + 1 == R ? 0 : now + 1;
             half(first, reads, now, nothing);
             wait_vmcnt<0>();
             __syncthreads();
-            if (t + 2 < t1) copy(t + 2, now);
-            half(second, reads, now ^ 1, nothing);
+            if (t + R < t1) copy(t + R, now);
+            half(second, reads, next, nothing);
+            now = next;
         }
         half(first, reads, now, nothing);
-        wait_lgkm();                        // (the operands of the last half, before another wavefront's copies of the next tile)
-        __syncthreads();
         half(second, none, 0, nothing);
-        static_for<0, FP>([&](auto I) __attribute__((always_inline)) { settle<(I < FP - 1)>(acc[I]); });
+        static_for<0, FP>([&](auto I) __attribute__((always_inline)) { settle<(S::kAlone && I < FP - 1)>(acc[I]); });
     } else {
-        clear();
-        if constexpr (DIRECT) {
-            if (t0 < t1) {
-                copy(t0, 0);
-                if (t0 + 1 < t1) {
-                    copy(t0 + 1, 1);
-                    wait_vmcnt<P.N + Q.N>();
-                } else {
-                    wait_vmcnt<0>();
-                }
-                __syncthreads();
-                read(0, first);
+        if (t0 < t1) {
+            P.load(t0 * KE, wave, lane);
+            Q.load(t0 * KE, wave, lane);
+            P.store(lds, wave, lane);
+            Q.store(lds + BP * 128, wave, lane);
+        }
+        for (int t = t0; t < t1; ++t) {
+            const int now = (t - t0) & 1;
+            __syncthreads();
+            if (t + 1 < t1) {
+                P.load((t + 1) * KE, wave, lane);
+                Q.load((t + 1) * KE, wave, lane);
             }
-            for (int t = t0; t < t1; ++t) {
-                const int now = (t - t0) & 1;
-                read(now, second);
-                products(first);
-                // the next step's copies are there, and nobody reads this step's stage any more
-                wait_vmcnt<0>();
-                __syncthreads();
-                if (t + 2 < t1) copy(t + 2, now);
-                if (t + 1 < t1) read(now ^ 1, first);
-                products(second);
-            }
-        } else {
-            if (t0 < t1) {
-                P.load(t0 * KE, wave, lane);
-                Q.load(t0 * KE, wave, lane);
-                P.store(lds, wave, lane);
-                Q.store(lds + BP * 128, wave, lane);
-            }
-            for (int t = t0; t < t1; ++t) {
-                const int now = (t - t0) & 1;
-                __syncthreads();
-                if (t + 1 < t1) {
-                    P.load((t + 1) * KE, wave, lane);
-                    Q.load((t + 1) * KE, wave, lane);
-                }
-                read(now, first);
-                read(now, second);
-                products(first);
-                products(second);
-                if (t + 1 < t1) {
-                    char *to = lds + (now ^ 1) * S::kStage;
-                    P.store(to, wave, lane);
-                    Q.store(to + BP * 128, wave, lane);
-                }
+            read(now, first);
+            read(now, second);
+            products(first);
+            products(second);
+            if (t + 1 < t1) {
+                char *to = lds + (now ^ 1) * S::kStage;
+                P.store(to, wave, lane);
+                Q.store(to + BP * 128, wave, lane);
             }
         }
     }
