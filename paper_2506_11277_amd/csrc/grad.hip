@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
                         if (i < n) to[i] = (T)d[i];
             }
         }
-    if (!a.db) return;
+    if (!a.sums) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[wave][lane * 8 + i] = sum[i];
     __syncthreads();
@@ -57,33 +57,20 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void bias_grad_kernel(const float *sums, int rows, int n, T *db)
+__global__ __launch_bounds__(256) void bias_grad_kernel(BiasGrad b)
 {
-    __shared__ float part[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-    float s = 0.0f;
-    if (c < n)
-#pragma unroll 8
-        for (int r = wave; r < rows; r += 4) s += sums[(size_t)r * n + c];
-    part[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < n) db[c] = (T)((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+    __shared__ float part[256];
+    bias_grad<T>(b, blockIdx.x, part);
 }
 
 template <class T>
 hipError_t launch(const GradInput &g, hipStream_t st)
 {
     const int groups = (g.tokens + g.rows - 1) / g.rows;
+    if (groups == 0) return hipSuccess;
     if (groups > 65535) return hipErrorInvalidValue;
-    if (groups > 0) {
-        grad_input_kernel<T><<<dim3((g.n_out + 511) / 512, groups), 256, 0, st>>>(g);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
-    if (g.db) {
-        bias_grad_kernel<T><<<(g.n_out + 63) / 64, 256, 0, st>>>(g.sums, groups, g.n_out, (T *)g.db);
-        return hipGetLastError();
-    }
-    return hipSuccess;
+    grad_input_kernel<T><<<dim3((g.n_out + 511) / 512, groups), 256, 0, st>>>(g);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -91,6 +78,16 @@ hipError_t launch(const GradInput &g, hipStream_t st)
 hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st)
 {
     return type == OZIMMU_BF16 ? launch<bf16>(g, st) : type == OZIMMU_F16 ? launch<f16>(g, st) : launch<float>(g, st);
+}
+
+hipError_t launch_bias_grad(const BiasGrad &b, int type, hipStream_t st)
+{
+    const int blocks = bias_grad_blocks(b);
+    if (blocks == 0) return hipSuccess;
+    if (type == OZIMMU_BF16) bias_grad_kernel<bf16><<<blocks, 256, 0, st>>>(b);
+    else if (type == OZIMMU_F16) bias_grad_kernel<f16><<<blocks, 256, 0, st>>>(b);
+    else bias_grad_kernel<float><<<blocks, 256, 0, st>>>(b);
+    return hipGetLastError();
 }
 
 }  // namespace oz

@@ -6,15 +6,19 @@ namespace oz {
 
 inline size_t element_bytes(int type) { return type == OZIMMU_F32 ? 4 : 2; }
 
-constexpr int kFewTokens = 64;             // columns few_tokens_kernel takes
+constexpr int kFewTokens = 16;             // columns few_tokens_kernel takes
 ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows);
+int plan_pair(const Product &x, const ProductPlan &xp, const Product &w, const ProductPlan &wp, int type, bool bias);
 inline size_t product_partial_bytes(int np, int nq, const ProductPlan &p)
 {
     return p.splits > 1 ? (size_t)p.splits * nq * ((np + 7) / 8 * 8) * 4 : 0;
 }
 hipError_t launch_product_bf16(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_pair_bf16(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
 hipError_t launch_product_f16(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_pair_f16(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
 hipError_t launch_product_f32(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_pair_f32(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
 
 // dz = dy * act'(pre) and the sums of its columns (grad.hip)
 // Tokens a work-group sums: 64, fewer where that leaves fewer than 1024 work-groups, at least two a wavefront, more where
@@ -30,11 +34,11 @@ inline int grad_rows(int tokens, int n_out)
 struct GradInput {
     const void *dy, *pre;                  // pre may be null (no activation)
     void *dz;                              // null: only the sums
-    void *db;                              // null: no sums
-    float *sums;                           // [ceil(tokens / rows)][n_out]
+    float *sums;                           // [ceil(tokens / rows)][n_out], null: none
     int lddy, ldpre, lddz, tokens, n_out, rows, act, wide;
 };
 hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st);
+hipError_t launch_bias_grad(const BiasGrad &b, int type, hipStream_t st);
 
 // a mixture-of-experts layer on a few tokens (moe.hip)
 struct MoeArgs {

@@ -3,8 +3,24 @@
 
 namespace oz {
 
-// Tile and number of parts of the contraction.  A launch takes as many rounds as its work-groups need on 256 compute
-// units; a round of tiles costs their entries times the steps over the rate that tile reaches where it fills the chip.
+// Tile and number of parts of the contraction, by the time that each would take.  A launch takes as many rounds as its
+// work-groups need on 256 compute units (two 64 x 64 tiles fit one, but share its LDS, which bounds them, so that they take turns in effect).  Times in
+// us, measured on 128^3 ... 8192^3: of a launch, of a tile's start and epilogue, of a step of 64 (32 bits: 32) of k:
+//   256 x 256   2 + rounds (10 + 1.53 steps)   4096^3 bf16: 112, against 149 with 128 x 128
+//   128 x 128   3 + rounds (3 + 0.53 steps)    2048^3 bf16: 22, against 28 with 64 x 64 and 50 with 256 x 256
+//    64 x 64    3 + rounds (0.7 + 0.20 steps)  200 x 2048 x 2048: 9.7, against 18 with 128 x 128
+// (binary32: 2.07 and 0.52 a step); a join of parts 3.5 and its reads and writes at 8 TB/s.
+static const struct {
+    int edge;
+    double launch, tile, step16, step32;
+} kShapes[3] = {{256, 2, 10, 1.53, 0}, {128, 3, 3, 0.53, 2.07}, {64, 3, 0.7, 0.20, 0.52}};
+static double tiles_of(int t, int np, int nq)
+{
+    const int e = kShapes[t].edge;
+    return (double)((np + e - 1) / e) * ((nq + e - 1) / e);
+}
+static double tile_us(int t, int steps, int type) { return kShapes[t].tile + steps * (type == OZIMMU_F32 ? kShapes[t].step32 : kShapes[t].step16); }
+
 ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows)
 {
     const int ke = type == OZIMMU_F32 ? 32 : 64;
@@ -15,25 +31,33 @@ ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows)
         int s = 1;
         while (s < 16 && groups * s * 2 <= 256 && all / (2 * s) >= 16) s *= 2;
         const int steps = (all + s - 1) / s;
-        return ProductPlan{kTileFew, steps > 0 ? (all + steps - 1) / steps : 1, steps, false};
+        return ProductPlan{kTileFew, steps > 0 ? (all + steps - 1) / steps : 1, steps, false, 0};
     }
-    static const int edge[3] = {256, 128, 64};
-    static const double rate[3] = {1.0, 0.8, 0.5};
-    ProductPlan best{2, 1, all, false};
-    double least = 0;
-    for (int t = type == OZIMMU_F32 ? 1 : 0; t < 3; ++t) {
-        const double tiles = (double)((np + edge[t] - 1) / edge[t]) * ((nq + edge[t] - 1) / edge[t]);
+    ProductPlan best{kTile64, 1, all, false, 1e300};
+    for (int t = type == OZIMMU_F32 ? kTile128 : kTile256; t <= kTile64; ++t)
         for (int s = 1; s <= 16 && (s == 1 || all / s >= 4); s *= 2) {
-            const double groups = tiles * s;
-            const double rounds = __builtin_ceil(groups / 256);
             const int steps = (all + s - 1) / s;
-            // in units of a step of a 64 x 64 tile; each work-group has a start and an end, a join reads the parts
-            const double cost = rounds * (edge[t] / 64) * (edge[t] / 64) / rate[t] * (steps + 4) + (s > 1 ? 24 + (double)np * nq * s / (64 * 64 * 64) : 0);
-            if (least == 0 || cost < least) {
-                least = cost;
-                best = ProductPlan{t, (all + steps - 1) / (steps > 0 ? steps : 1), steps, false};
-                if (best.splits < 1) best.splits = 1;
-            }
+            const double us = kShapes[t].launch + __builtin_ceil(tiles_of(t, np, nq) * s / 256) * tile_us(t, steps, type) +
+                              (s > 1 ? 3.5 + (double)np * nq * s * 8 / 8e6 : 0);
+            if (us < best.us) best = ProductPlan{t, steps > 0 ? (all + steps - 1) / steps : 1, steps, false, us};
+        }
+    return best;
+}
+
+// The tile with which two products take one launch, or -1 where two launches are sooner done (2 us for the second one, 3 for
+// the bias gradient's).
+int plan_pair(const Product &x, const ProductPlan &xp, const Product &w, const ProductPlan &wp, int type, bool bias)
+{
+    const int ke = type == OZIMMU_F32 ? 32 : 64;
+    int best = -1;
+    double least = xp.us + wp.us + 2 + (bias ? 3 : 0);
+    for (int t = kTile128; t <= kTile64; ++t) {
+        const double ux = tile_us(t, (x.nk + ke - 1) / ke, type), uw = tile_us(t, (w.nk + ke - 1) / ke, type), longest = ux > uw ? ux : uw;
+        const double all = (tiles_of(t, x.e.np, x.e.nq) * ux + tiles_of(t, w.e.np, w.e.nq) * uw) / 256;
+        const double us = kShapes[t].launch + (all < longest / 2 ? longest : all + longest / 2);
+        if (us < least) {
+            least = us;
+            best = t;
         }
     }
     return best;
@@ -65,14 +89,19 @@ inline bool direct_operand(const void *p, int ld, int along, size_t size)
     return on16(p, ld, size) && (size_t)along * size % 16 == 0 && 256ull * (unsigned)ld * size < (1ull << 32);
 }
 
-hipError_t launch_product(Product a, ProductPlan plan, int type, float *partial, hipStream_t st)
+// completes a product and its plan: whether it can be copied directly, how its epilogue stores
+void prepare_product(Product &a, ProductPlan &plan, int type)
 {
     const size_t size = element_bytes(type);
     Epilogue &e = a.e;
-    if (e.np == 0 || e.nq == 0) return hipSuccess;
     plan.direct = a.nk > 0 && direct_operand(a.P, a.ldp, a.p_k_rows ? a.nk : e.np, size) && direct_operand(a.Q, a.ldq, a.q_k_rows ? a.nk : e.nq, size);
     e.wide = on16(e.out, e.ldo, size) && (!e.bias || (uintptr_t)e.bias % 16 == 0) && (!e.residual || on16(e.residual, e.ldr, size)) &&
              (!e.pre || on16(e.pre, e.ldpre, size));
+}
+
+hipError_t launch_product(const Product &a, const ProductPlan &plan, int type, float *partial, hipStream_t st)
+{
+    if (a.e.np == 0 || a.e.nq == 0) return hipSuccess;
     return type == OZIMMU_BF16  ? launch_product_bf16(a, plan, partial, st)
            : type == OZIMMU_F16 ? launch_product_f16(a, plan, partial, st)
                                 : launch_product_f32(a, plan, partial, st);
@@ -119,7 +148,7 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     if (bad_rows(tokens, n_in, x, ldx, size) || bad_rows(n_out, n_in, w, ldw, size) || bad_rows(tokens, n_out, y, ldy, size)) return OZIMMU_BAD_ARG;
     if ((uintptr_t)bias % size || (residual && bad_rows(tokens, n_out, residual, ldr, size)) || (pre && bad_rows(tokens, n_out, pre, ldpre, size)))
         return OZIMMU_BAD_ARG;
-    const ProductPlan plan = plan_product(n_out, tokens, n_in, type, true);
+    ProductPlan plan = plan_product(n_out, tokens, n_in, type, true);
     if (bad_workspace(workspace, workspace_bytes, product_partial_bytes(n_out, tokens, plan))) return OZIMMU_BAD_ARG;
     Product a{};
     a.P = w;
@@ -130,6 +159,7 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     a.q_k_rows = true;
     a.nk = n_in;
     a.e = Epilogue{bias, residual, pre, y, ldr, ldpre, ldy, n_out, tokens, activation, 0};
+    prepare_product(a, plan, type);
     return launch_product(a, plan, type, (float *)workspace, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
 }
 
@@ -161,8 +191,7 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
         g.dy = dy;
         g.pre = activation ? pre : nullptr;
         g.dz = activation && (dx || dw) ? base + ws.dz : nullptr;
-        g.db = db;
-        g.sums = (float *)(base + ws.sums);
+        g.sums = db ? (float *)(base + ws.sums) : nullptr;
         g.lddy = lddy;
         g.ldpre = ldpre;
         g.lddz = ws.lddz;
@@ -177,28 +206,37 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
         dz = base + ws.dz;
         lddz = ws.lddz;
     }
+    const int rows = grad_rows(tokens, n_out);
+    const BiasGrad bias{(const float *)(base + ws.sums), db, (tokens + rows - 1) / rows, n_out};
     float *partial = (float *)(base + ws.partial);
-    Product a{};
-    if (dx) {
-        a.P = w;
-        a.ldp = ldw;
-        a.Q = dz;
-        a.ldq = lddz;
-        a.q_k_rows = true;
-        a.nk = n_out;
-        a.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, 0};
-        if (launch_product(a, plan_product(n_in, tokens, n_out, type, false), type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    Product x_grad{}, w_grad{};
+    ProductPlan x_plan = plan_product(n_in, tokens, n_out, type, false), w_plan = plan_product(n_in, n_out, tokens, type, false);
+    x_grad.P = w;
+    x_grad.ldp = ldw;
+    x_grad.Q = dz;
+    x_grad.ldq = lddz;
+    x_grad.q_k_rows = true;
+    x_grad.nk = n_out;
+    x_grad.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, 0};
+    w_grad.P = x;
+    w_grad.ldp = ldx;
+    w_grad.Q = dz;
+    w_grad.ldq = lddz;
+    w_grad.nk = tokens;
+    w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, 0};
+    prepare_product(x_grad, x_plan, type);
+    prepare_product(w_grad, w_plan, type);
+    const bool both = dx && dw && n_in > 0 && n_out > 0 && tokens > 0 && x_plan.direct && w_plan.direct;
+    const int pair = both ? plan_pair(x_grad, x_plan, w_grad, w_plan, type, db != nullptr) : -1;
+    if (pair >= 0) {
+        const hipError_t e = type == OZIMMU_BF16  ? launch_pair_bf16(x_grad, w_grad, bias, pair, st)
+                             : type == OZIMMU_F16 ? launch_pair_f16(x_grad, w_grad, bias, pair, st)
+                                                  : launch_pair_f32(x_grad, w_grad, bias, pair, st);
+        return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
     }
-    if (dw) {
-        a.P = x;
-        a.ldp = ldx;
-        a.Q = dz;
-        a.ldq = lddz;
-        a.q_k_rows = false;
-        a.nk = tokens;
-        a.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, 0};
-        if (launch_product(a, plan_product(n_in, n_out, tokens, type, false), type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    }
+    if (launch_bias_grad(bias, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (dx && launch_product(x_grad, x_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (dw && launch_product(w_grad, w_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     return OZIMMU_OK;
 }
 

@@ -218,11 +218,32 @@ struct Product {
     Epilogue e;
 };
 
+// The bias gradient: column sums of `rows` rows of partial sums.  64 columns a work-group, always in the same order.
+struct BiasGrad {
+    const float *sums;                    // [rows][n]
+    void *db;                             // null: none
+    int rows, n;
+};
+inline int bias_grad_blocks(const BiasGrad &b) { return b.db ? (b.n + 63) / 64 : 0; }
+template <class T>
+__device__ __forceinline__ void bias_grad(const BiasGrad &b, int block, float *part)    // part: 256 floats of LDS
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = block * 64 + lane;
+    float s = 0.0f;
+    if (c < b.n)
+#pragma unroll 8
+        for (int r = wave; r < b.rows; r += 4) s += b.sums[(size_t)r * b.n + c];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (wave == 0 && c < b.n) ((T *)b.db)[c] = (T)((part[lane] + part[64 + lane]) + (part[128 + lane] + part[192 + lane]));
+}
+
 enum Tile { kTile256, kTile128, kTile64, kTileFew };      // edge; few_tokens_kernel
 struct ProductPlan {
     int tile;
     int splits, steps;       // the contraction in `splits` parts of `steps` steps of 128 bytes
     bool direct;             // copied to LDS without registers
+    double us;               // estimated
 };
 
 }  // namespace oz

@@ -7,4 +7,8 @@ hipError_t launch_product_bf16(const Product &a, const ProductPlan &plan, float 
 {
     return launch_product_type<bf16>(a, plan, partial, st);
 }
+hipError_t launch_pair_bf16(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st)
+{
+    return launch_pair_type<bf16>(dx, dw, db, tile, st);
+}
 }  // namespace oz

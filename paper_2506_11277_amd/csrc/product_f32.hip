@@ -7,4 +7,8 @@ hipError_t launch_product_f32(const Product &a, const ProductPlan &plan, float *
 {
     return launch_product_type<float>(a, plan, partial, st);
 }
+hipError_t launch_pair_f32(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st)
+{
+    return launch_pair_type<float>(dx, dw, db, tile, st);
+}
 }  // namespace oz
