@@ -14,7 +14,7 @@
 namespace oz {
 namespace {
 
-constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 8;
+constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 16;
 constexpr int kWords = OZIMMU_MOE_EXPERTS / 32;
 
 // bit map of the experts that the `n` choices name
@@ -24,6 +24,14 @@ __device__ __forceinline__ void mark_chosen(unsigned *map, const int *chosen, in
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += blockDim.x) atomicOr(&map[chosen[i] >> 5], 1u << (chosen[i] & 31));
     __syncthreads();
+}
+
+// how many experts below e are marked
+__device__ __forceinline__ int marked_before(const unsigned *map, int e)
+{
+    int n = __popc(map[e >> 5] & ((1u << (e & 31)) - 1));
+    for (int i = 0; i < e >> 5; ++i) n += __popc(map[i]);
+    return n;
 }
 
 // a > b, a NaN above everything, for a at a later place than b if `later` (ties go to the earlier one)
@@ -40,14 +48,15 @@ __global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
     constexpr int E = Chunk<T>::E;
     typedef typename Chunk<T>::V V;
     __shared__ float logits[OZIMMU_MOE_EXPERTS];
-    __shared__ float best[OZIMMU_MOE_EXPERTS];
+    __shared__ float share[OZIMMU_MOE_EXPERTS];
     __shared__ unsigned map[kWords];
     __shared__ float total;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int t = blockIdx.x;
     const T *x = (const T *)a.x + (size_t)t * a.ldx;
     for (int i = threadIdx.x; i < kWords; i += blockDim.x) map[i] = 0;
-    // four experts of a wavefront at a time
+    // four experts of a wavefront at a time, all of whose loads of four steps are issued before the first product
+    const int whole = a.width / (64 * E) * (64 * E);
     for (int e0 = wave; e0 < a.experts; e0 += 4 * kRouteWaves) {
         const T *r[4];
         float s[4] = {0, 0, 0, 0};
@@ -56,15 +65,28 @@ __global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
             const int e = e0 + i * kRouteWaves;
             r[i] = (const T *)a.router + (size_t)(e < a.experts ? e : e0) * a.width;
         }
-        for (int k = lane * E; k < a.width; k += 64 * E) {
-            const int n = a.width - k;
-            const V xv = __builtin_bit_cast(V, load_chunk(x + k, n));
+        auto products = [&](v4u xc, const v4u (&rc)[4]) {
+            const V xv = __builtin_bit_cast(V, xc);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const V rv = __builtin_bit_cast(V, load_chunk(r[i] + k, n));
+                const V rv = __builtin_bit_cast(V, rc[i]);
 #pragma unroll
                 for (int c = 0; c < E; ++c) s[i] = __builtin_fmaf((float)xv[c], (float)rv[c], s[i]);
             }
+        };
+#pragma unroll 4
+        for (int k = lane * E; k < whole; k += 64 * E) {
+            v4u xc, rc[4];
+            __builtin_memcpy(&xc, x + k, 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) __builtin_memcpy(&rc[i], r[i] + k, 16);
+            products(xc, rc);
+        }
+        if (whole + lane * E < a.width) {
+            const int k = whole + lane * E, n = a.width - k;
+            const v4u xc = load_chunk(x + k, n);
+            const v4u rc[4] = {load_chunk(r[0] + k, n), load_chunk(r[1] + k, n), load_chunk(r[2] + k, n), load_chunk(r[3] + k, n)};
+            products(xc, rc);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -74,25 +96,28 @@ __global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
-        const float l = logits[e];
+    // an expert is chosen if fewer than top_k come before it: 16 lanes count for it
+    for (int e = threadIdx.x >> 4; e < (a.experts + 3) / 4 * 4; e += 4 * kRouteWaves) {
+        const bool there = e < a.experts;
+        const float l = there ? logits[e] : 0.0f;
         int rank = 0;
-        for (int o = 0; o < a.experts; ++o) rank += o != e && before(logits[o], l, o > e);
-        if (rank < a.top_k) atomicOr(&map[e >> 5], 1u << (e & 31));
-        best[e] = l;
+        for (int o = threadIdx.x & 15; there && o < a.experts; o += 16) rank += o != e && before(logits[o], l, o > e);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) rank += __shfl_xor(rank, d);
+        if (there && (threadIdx.x & 15) == 0 && rank < a.top_k) atomicOr(&map[e >> 5], 1u << (e & 31));
     }
     __syncthreads();
-    // the largest logit and the sum of the exponentials, by one wavefront
+    // the sum of the exponentials, by one wavefront
     if (wave == 0) {
         float top = -__builtin_inff();
-        for (int e = lane; e < a.experts; e += 64) top = fmaxf(top, best[e]);
+        for (int e = lane; e < a.experts; e += 64) top = fmaxf(top, logits[e]);
 #pragma unroll
         for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
         float sum = 0.0f;
         for (int e = lane; e < a.experts; e += 64) {
-            const float x = expf(best[e] - top);
-            best[e] = x;
-            if (!a.normalise || (map[e >> 5] >> (e & 31) & 1)) sum += x;
+            const float v = expf(logits[e] - top);
+            share[e] = v;
+            if (!a.normalise || (map[e >> 5] >> (e & 31) & 1)) sum += v;
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
@@ -101,10 +126,9 @@ __global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         if (!(map[e >> 5] >> (e & 31) & 1)) continue;
-        int place = __popc(map[e >> 5] & ((1u << (e & 31)) - 1));
-        for (int i = 0; i < e >> 5; ++i) place += __popc(map[i]);
+        const int place = marked_before(map, e);
         a.chosen[t * a.top_k + place] = e;
-        a.gates[t * a.top_k + place] = best[e] / total;
+        a.gates[t * a.top_k + place] = share[e] / total;
     }
 }
 
@@ -173,45 +197,78 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
 template <class T, int NX>
 __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
 {
-    constexpr int KE = 8 * Chunk<T>::E;
+    constexpr int E = Chunk<T>::E, KE = 8 * E, U = NX == 1 ? 4 : 2;
+    constexpr int kNone = 255;
     __shared__ unsigned map[kWords];
-    __shared__ int chosen[OZIMMU_MOE_TOKENS * OZIMMU_MOE_TOP_K];
+    __shared__ int experts[OZIMMU_MOE_EXPERTS];                                // the chosen ones
+    __shared__ uint8_t places[OZIMMU_MOE_EXPERTS * 16 * NX];                   // [chosen expert][token]: its place among the token's, or kNone
     __shared__ __attribute__((aligned(16))) float sums[kOutWaves][NX][16 * kStreamLd];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int all = a.tokens * a.top_k;
-    for (int i = threadIdx.x; i < all; i += blockDim.x) chosen[i] = a.chosen[i];
+    const int all = a.tokens * a.top_k, can = all < a.experts ? all : a.experts;
+    for (int i = threadIdx.x; i < can * 16 * NX / 4; i += blockDim.x) ((unsigned *)places)[i] = ~0u;
     mark_chosen(map, a.chosen, all);
-    const int p0 = blockIdx.x * 16, row = p0 + (lane & 15) < a.width ? p0 + (lane & 15) : a.width - 1;
-    v4f acc[1][NX];
+    for (int e = threadIdx.x; e < a.experts; e += blockDim.x)
+        if (map[e >> 5] >> (e & 31) & 1) experts[marked_before(map, e)] = e;
+    for (int i = threadIdx.x; i < all; i += blockDim.x) {
+        const int t = i / a.top_k;
+        places[marked_before(map, a.chosen[i]) * 16 * NX + t] = (uint8_t)(i - t * a.top_k);
+    }
+    int chosen = 0;
+    for (int i = 0; i < kWords; ++i) chosen += __popc(map[i]);
+    __syncthreads();
+
+    const int p0 = blockIdx.x * 16, row = p0 + (lane & 15) < a.width ? p0 + (lane & 15) : a.width - 1, g = (lane >> 4) * E;
+    v4f acc[NX];
 #pragma unroll
-    for (int j = 0; j < NX; ++j) acc[0][j] = v4f{0, 0, 0, 0};
-    // the steps of all chosen experts, one after the other, are dealt to the wavefronts in turn
-    const int steps = (a.hidden + KE - 1) / KE;
-    int first = wave;
-    for (int i = 0; i < kWords; ++i)
-        for (unsigned m = map[i]; m; m &= m - 1) {
-            const int expert = i * 32 + __builtin_ctz(m);
-            if (first < steps) {
-                const T *const w[1] = {(const T *)a.w_out + ((size_t)expert * a.width + row) * a.hidden};
-                const T *x[NX];
-                bool on[NX];
+    for (int j = 0; j < NX; ++j) acc[j] = v4f{0, 0, 0, 0};
+    // The steps of all chosen experts, one after the other, are dealt to the wavefronts in turn; U steps' loads, of as many
+    // experts as it may be, are issued before the first of their products.
+    const int steps = (a.hidden + KE - 1) / KE, items = chosen * steps;
+    for (int first = wave; first < items; first += U * kOutWaves) {
+        v4u w[U][2], h[U][2][NX];
 #pragma unroll
-                for (int j = 0; j < NX; ++j) {
-                    const int t = 16 * j + (lane & 15);
-                    int choice = -1;
-                    if (t < a.tokens)
-                        for (int c = 0; c < a.top_k; ++c)
-                            if (chosen[t * a.top_k + c] == expert) choice = t * a.top_k + c;
-                    on[j] = choice >= 0;
-                    x[j] = (const T *)a.h + (size_t)(on[j] ? choice : 0) * a.ldh;
-                }
-                stream_products<T, 1, NX, NX == 1 ? 4 : 2>(acc, w, x, on, first, steps, kOutWaves, a.hidden, lane);
+        for (int u = 0; u < U; ++u) {
+            const int item = first + u * kOutWaves;
+            const bool there = item < items;
+            const int slot = there ? item / steps : 0, k0 = (there ? item - slot * steps : 0) * KE + g;
+            const T *wr = (const T *)a.w_out + ((size_t)experts[slot] * a.width + row) * a.hidden;
+            const T *hr[NX];
+            bool on[NX];
+#pragma unroll
+            for (int j = 0; j < NX; ++j) {
+                const int t = 16 * j + (lane & 15), place = places[slot * 16 * NX + t];
+                on[j] = there && place != kNone;
+                hr[j] = (const T *)a.h + (size_t)(on[j] ? t * a.top_k + place : 0) * a.ldh;
             }
-            // where this wavefront goes on in the next expert's steps
-            first = ((first - steps) % kOutWaves + kOutWaves) % kOutWaves;
+            if (there && k0 - g + KE <= a.hidden) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    __builtin_memcpy(&w[u][s], wr + k0 + s * 4 * E, 16);
+#pragma unroll
+                    for (int j = 0; j < NX; ++j) {
+                        h[u][s][j] = v4u{0, 0, 0, 0};
+                        if (on[j]) __builtin_memcpy(&h[u][s][j], hr[j] + k0 + s * 4 * E, 16);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int k = k0 + s * 4 * E, n = there ? a.hidden - k : 0;
+                    w[u][s] = load_chunk(wr + k, n);
+#pragma unroll
+                    for (int j = 0; j < NX; ++j) h[u][s][j] = load_chunk(hr[j] + k, on[j] ? n : 0);
+                }
+            }
         }
 #pragma unroll
-    for (int j = 0; j < NX; ++j) put_sums(sums[wave][j], acc[0][j], lane);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int j = 0; j < NX; ++j) acc[j] = mma(w[u][s], h[u][s][j], acc[j], T{});
+    }
+#pragma unroll
+    for (int j = 0; j < NX; ++j) put_sums(sums[wave][j], acc[j], lane);
     __syncthreads();
     for (int i = threadIdx.x; i < NX * 256; i += 64 * kOutWaves) {
         const int q = i >> 4, p = i & 15;
