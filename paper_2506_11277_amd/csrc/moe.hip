@@ -1,6 +1,7 @@
 // A mixture-of-experts layer for a few tokens.  Bound by memory: the weights of the chosen experts, read once.
 //
-//   moe_route_kernel   a work-group per token: logits of all experts, the chosen ones and their gates
+//   moe_route_kernel   a work-group per token: logits of all experts, the chosen ones and their gates (for one to four tokens and
+//                      a small router the second kernel does that by itself)
 //   moe_hidden_kernel  a work-group per 16 hidden features of an expert that some token chose: gate and up rows against
 //                      the tokens that chose it, h = gate silu(a) b rounded for the next product
 //   moe_out_kernel     a work-group per 16 output features: their rows of every chosen expert against its tokens' h, all in one
@@ -16,6 +17,7 @@ namespace {
 
 constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 16;
 constexpr int kWords = OZIMMU_MOE_EXPERTS / 32;
+constexpr int kRouteHere = 64;                                  // choices that fit the second kernel's own routing
 
 // bit map of the experts that the `n` choices name
 __device__ __forceinline__ void mark_chosen(unsigned *map, const int *chosen, int n)
@@ -42,27 +44,30 @@ __device__ __forceinline__ bool before(float a, float b, bool later)
     return later ? a > b : a >= b;
 }
 
-template <class T>
-__global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
+// The choice of token t by a work-group of WAVES wavefronts: its experts in ascending order, and their gates.
+struct RouteSpace {
+    float logits[OZIMMU_MOE_EXPERTS], share[OZIMMU_MOE_EXPERTS];
+    unsigned map[kWords];
+    float total;
+};
+template <class T, int WAVES>
+__device__ __forceinline__ void route_token(const MoeArgs &a, int t, RouteSpace &space, int *chosen, float *gates)
 {
     constexpr int E = Chunk<T>::E;
     typedef typename Chunk<T>::V V;
-    __shared__ float logits[OZIMMU_MOE_EXPERTS];
-    __shared__ float share[OZIMMU_MOE_EXPERTS];
-    __shared__ unsigned map[kWords];
-    __shared__ float total;
+    float *logits = space.logits, *share = space.share;
+    unsigned *map = space.map;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int t = blockIdx.x;
     const T *x = (const T *)a.x + (size_t)t * a.ldx;
     for (int i = threadIdx.x; i < kWords; i += blockDim.x) map[i] = 0;
     // four experts of a wavefront at a time, all of whose loads of four steps are issued before the first product
     const int whole = a.width / (64 * E) * (64 * E);
-    for (int e0 = wave; e0 < a.experts; e0 += 4 * kRouteWaves) {
+    for (int e0 = wave; e0 < a.experts; e0 += 4 * WAVES) {
         const T *r[4];
         float s[4] = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int e = e0 + i * kRouteWaves;
+            const int e = e0 + i * WAVES;
             r[i] = (const T *)a.router + (size_t)(e < a.experts ? e : e0) * a.width;
         }
         auto products = [&](v4u xc, const v4u (&rc)[4]) {
@@ -92,12 +97,12 @@ __global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
             for (int d = 32; d; d >>= 1) s[i] += __shfl_xor(s[i], d);
-            if (lane == 0 && e0 + i * kRouteWaves < a.experts) logits[e0 + i * kRouteWaves] = s[i];
+            if (lane == 0 && e0 + i * WAVES < a.experts) logits[e0 + i * WAVES] = s[i];
         }
     }
     __syncthreads();
     // an expert is chosen if fewer than top_k come before it: 16 lanes count for it
-    for (int e = threadIdx.x >> 4; e < (a.experts + 3) / 4 * 4; e += 4 * kRouteWaves) {
+    for (int e = threadIdx.x >> 4; e < (a.experts + 3) / 4 * 4; e += 4 * WAVES) {
         const bool there = e < a.experts;
         const float l = there ? logits[e] : 0.0f;
         int rank = 0;
@@ -121,28 +126,53 @@ __global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
         }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-        if (lane == 0) total = sum;
+        if (lane == 0) space.total = sum;
     }
     __syncthreads();
     for (int e = threadIdx.x; e < a.experts; e += blockDim.x) {
         if (!(map[e >> 5] >> (e & 31) & 1)) continue;
         const int place = marked_before(map, e);
-        a.chosen[t * a.top_k + place] = e;
-        a.gates[t * a.top_k + place] = share[e] / total;
+        chosen[place] = e;
+        gates[place] = share[e] / space.total;
     }
 }
 
 template <class T>
+__global__ __launch_bounds__(64 * kRouteWaves) void moe_route_kernel(MoeArgs a)
+{
+    __shared__ RouteSpace space;
+    const int t = blockIdx.x;
+    route_token<T, kRouteWaves>(a, t, space, a.chosen + t * a.top_k, a.gates + t * a.top_k);
+}
+
+// ROUTE: every work-group finds the choices for itself (the first one writes them down)
+template <class T, bool ROUTE>
 __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a)
 {
     constexpr int KE = 8 * Chunk<T>::E;
     __shared__ unsigned map[kWords];
+    __shared__ int own_chosen[ROUTE ? kRouteHere : 1];
+    __shared__ float own_gates[ROUTE ? kRouteHere : 1];
+    __shared__ typename std::conditional<ROUTE, RouteSpace, int>::type space;
     __shared__ int choices[OZIMMU_MOE_TOKENS];                 // of the tokens that chose this expert: token * top_k + place
     __shared__ int count;
     __shared__ __attribute__((aligned(16))) float sums[kHiddenWaves][2][16 * kStreamLd];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int all = a.tokens * a.top_k;
-    mark_chosen(map, a.chosen, all);
+    const int *chosen = ROUTE ? own_chosen : a.chosen;
+    const float *gates = ROUTE ? own_gates : a.gates;
+    if constexpr (ROUTE) {
+        for (int t = 0; t < a.tokens; ++t) {
+            route_token<T, kHiddenWaves>(a, t, space, own_chosen + t * a.top_k, own_gates + t * a.top_k);
+            __syncthreads();
+        }
+        if (blockIdx.x == 0 && blockIdx.y == 0)
+            for (int i = threadIdx.x; i < all; i += blockDim.x) {
+                a.chosen[i] = own_chosen[i];
+                a.gates[i] = own_gates[i];
+            }
+    }
+    mark_chosen(map, chosen, all);
     int expert = -1;
     for (int i = 0, left = blockIdx.y; i < kWords; ++i) {      // the blockIdx.y-th bit that is set
         unsigned m = map[i];
@@ -160,7 +190,7 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
         int mine = -1;
         if (lane < a.tokens)
             for (int i = 0; i < a.top_k; ++i)
-                if (a.chosen[lane * a.top_k + i] == expert) mine = lane * a.top_k + i;
+                if (chosen[lane * a.top_k + i] == expert) mine = lane * a.top_k + i;
         const unsigned long long who = __ballot(mine >= 0);
         if (mine >= 0) choices[__popcll(who & ((1ull << lane) - 1))] = mine;
         if (lane == 0) count = __popcll(who);
@@ -188,7 +218,7 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
                 u += sums[s][1][q * kStreamLd + f];
             }
             const int choice = choices[c0 + q];
-            ((T *)a.h)[(size_t)choice * a.ldh + f0 + f] = (T)(a.gates[choice] * activate<T>(OZIMMU_ACT_SILU, g) * u);
+            ((T *)a.h)[(size_t)choice * a.ldh + f0 + f] = (T)(gates[choice] * activate<T>(OZIMMU_ACT_SILU, g) * u);
         }
         __syncthreads();
     }
@@ -283,11 +313,19 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
 template <class T>
 hipError_t launch(const MoeArgs &a, hipStream_t st)
 {
-    moe_route_kernel<T><<<a.tokens, 64 * kRouteWaves, 0, st>>>(a);
-    if (hipError_t e = hipGetLastError()) return e;
     const int can = a.tokens * a.top_k < a.experts ? a.tokens * a.top_k : a.experts;
+    const dim3 hidden((a.hidden + 15) / 16, can);
+    // Where the router is small enough for every work-group of the second kernel to read it from the caches (16 MB in all take
+    // about 2 us), its launch is saved: one token, 16 experts of 1024 x 704: 21 us in three launches, 16 in two.
+    const double read = (double)hidden.x * hidden.y * a.tokens * a.experts * a.width * sizeof(T);
+    const bool here = a.hidden > 0 && a.tokens <= 4 && a.tokens * a.top_k <= kRouteHere && read <= 16e6;
+    if (!here) {
+        moe_route_kernel<T><<<a.tokens, 64 * kRouteWaves, 0, st>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
     if (a.hidden > 0) {
-        moe_hidden_kernel<T><<<dim3((a.hidden + 15) / 16, can), 64 * kHiddenWaves, 0, st>>>(a);
+        if (here) moe_hidden_kernel<T, true><<<hidden, 64 * kHiddenWaves, 0, st>>>(a);
+        else moe_hidden_kernel<T, false><<<hidden, 64 * kHiddenWaves, 0, st>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
     const int groups = (a.width + 15) / 16;

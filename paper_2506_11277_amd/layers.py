@@ -4,6 +4,7 @@ Argument marshalling only, as in `ozimmu`: PyTorch provides device memory and th
 tensors with a token (or an output feature of a weight) per row, stride(1) == 1 and any row stride.
 """
 import ctypes
+from operator import attrgetter
 
 import torch
 
@@ -13,6 +14,8 @@ from .ozimmu import BAD_ARG, OK, OzimmuError
 BF16, F16, F32, E4M3 = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
+
+_dtype, _shape = attrgetter("dtype"), attrgetter("shape")
 
 BLOCK = 256          # values that share a scale where AdamW's moments are held in 8 bits
 
@@ -63,20 +66,22 @@ def _type_of(x, what):
 
 def _ld(x, rows, cols, like, what):
     """Row stride of a [rows, cols] device tensor of `like`'s type, on its device, whose rows are contiguous."""
-    if x.dim() != 2 or x.shape[0] != rows or x.shape[1] != cols:
+    if x.shape != (rows, cols):
         raise ValueError(f"{what}: [{rows}, {cols}] expected, got {list(x.shape)}")
-    if x.dtype != like.dtype or x.device != like.device:
+    if x.dtype is not like.dtype or x.get_device() != like.get_device():
         raise ValueError(f"{what}: {like.dtype} on {like.device} expected")
-    if cols > 1 and x.stride(1) != 1:
+    ld, step = x.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{what}: contiguous rows expected (stride(1) == 1)")
-    ld = x.stride(0) if rows > 1 else max(1, cols)
-    if ld < max(1, cols):
+    if rows <= 1:
+        return cols or 1
+    if ld < cols or ld < 1:
         raise ValueError(f"{what}: row stride {ld} smaller than {cols}")
     return ld
 
 
 def _vector(x, n, like, what):
-    if x.dim() != 1 or x.shape[0] != n or x.dtype != like.dtype or x.device != like.device or (n > 1 and x.stride(0) != 1):
+    if x.shape != (n,) or x.dtype is not like.dtype or x.get_device() != like.get_device() or (n > 1 and x.stride(0) != 1):
         raise ValueError(f"{what}: contiguous [{n}] of {like.dtype} on {like.device} expected")
     return x.data_ptr()
 
@@ -98,10 +103,10 @@ def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=No
     `pre`, a [tokens, n_out] tensor, receives x @ w.T + bias for linear_grad.  `out` may be `residual` itself.
     Asynchronous on the current stream."""
     kind = _type_of(x, "x")
-    if x.dim() != 2 or w.dim() != 2:
-        raise ValueError("x and w: matrices expected")
-    tokens, n_in = x.shape
-    n_out = w.shape[0]
+    try:
+        (tokens, n_in), (n_out, _) = x.shape, w.shape
+    except ValueError:
+        raise ValueError("x and w: matrices expected") from None
     ldx, ldw = _ld(x, tokens, n_in, x, "x"), _ld(w, n_out, n_in, x, "w")
     if out is None:
         out = torch.empty((tokens, n_out), dtype=x.dtype, device=x.device)
@@ -129,10 +134,10 @@ def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=
     db is None with bias=False; of dx and dw those in `want` are formed, the others are None.  Given tensors receive
     the results.  The gradient of linear's residual is dy itself."""
     kind = _type_of(dy, "dy")
-    if dy.dim() != 2 or x.dim() != 2 or w.dim() != 2:
-        raise ValueError("dy, x and w: matrices expected")
-    tokens, n_out = dy.shape
-    n_in = x.shape[1]
+    try:
+        (tokens, n_out), (_, n_in) = dy.shape, x.shape
+    except ValueError:
+        raise ValueError("dy and x: matrices expected") from None
     lddy, ldx, ldw = _ld(dy, tokens, n_out, dy, "dy"), _ld(x, tokens, n_in, dy, "x"), _ld(w, n_out, n_in, dy, "w")
     if activation != ACT_NONE and pre is None:
         raise ValueError("pre: the values before the activation are needed")
@@ -192,6 +197,7 @@ class AdamW:
         self._list = (_AdamWTensor * n)()
         self._shapes = [p.shape for p in params]
         self._device = params[0].device if n else None
+        self._devices = [p.get_device() for p in params]
         for i, (t, p) in enumerate(zip(self._list, params)):
             kind = _type_of(p, f"params[{i}]")
             eight = m[i].dtype == torch.float8_e4m3fn
@@ -215,8 +221,10 @@ class AdamW:
     def step(self, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, seed=0):
         """One step with the gradients `grads`, contiguous tensors of the parameters' shapes; `step` counts from 1; `seed`
         makes the random words that 8-bit moments are rounded with.  Asynchronous on the current stream."""
-        kinds = [g.dtype for g in grads]
-        if [g.shape for g in grads] != self._shapes or any([g.device != self._device or not g.is_contiguous() for g in grads]):
+        # (map() over the methods: half the time of comprehensions, and 90 small tensors are host time before all else)
+        kinds = list(map(_dtype, grads))
+        if (list(map(_shape, grads)) != self._shapes or not all(map(torch.Tensor.is_contiguous, grads)) or
+                list(map(torch.Tensor.get_device, grads)) != self._devices):
             raise ValueError("grads: contiguous tensors of the parameters' shapes and device expected")
         if kinds != self._grad_types:
             for t, kind in zip(self._list, kinds):
@@ -224,7 +232,7 @@ class AdamW:
                     raise ValueError("grads: bfloat16, float16 or float32 expected")
                 t.grad_type = _TYPES[kind]
             self._grad_types = kinds
-        pointers = self._pointers(*[g.data_ptr() for g in grads])
+        pointers = self._pointers(*map(torch.Tensor.data_ptr, grads))
         rc = (_lib or lib()).ozimmu_adamw(len(self._list), self._list, pointers, lr, beta1, beta2, eps, weight_decay, step,
                                           seed & 0xffffffff, ozimmu._stream())
         if rc != OK:
@@ -246,25 +254,27 @@ def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, ga
     (ties to the lowest index) with the softmax over all experts, or over the chosen ones (normalise), as their gates.
     chosen [tokens, top_k], int32, lists them in ascending order, gates, float32, has theirs."""
     kind = _type_of(x, "x")
-    if x.dim() != 2 or router.dim() != 2 or w_in.dim() != 3 or w_out.dim() != 3:
-        raise ValueError("x and router: matrices, w_in and w_out: three dimensions expected")
-    tokens, width = x.shape
-    experts, hidden = router.shape[0], w_out.shape[2]
+    try:
+        (tokens, width), (experts, _, hidden) = x.shape, w_out.shape
+    except ValueError:
+        raise ValueError("x: a matrix, w_out: three dimensions expected") from None
+    index = x.get_device()
     for w, shape, what in ((router, (experts, width), "router"), (w_in, (experts, 2 * hidden, width), "w_in"),
                            (w_out, (experts, width, hidden), "w_out")):
-        if w.shape != shape or w.dtype != x.dtype or w.device != x.device or not w.is_contiguous():
+        if w.shape != shape or w.dtype is not x.dtype or w.get_device() != index or not w.is_contiguous():
             raise ValueError(f"{what}: contiguous {list(shape)} of {x.dtype} on {x.device} expected")
     ldx = _ld(x, tokens, width, x, "x")
     if out is None:
         out = torch.empty((tokens, width), dtype=x.dtype, device=x.device)
     ldy = _ld(out, tokens, width, x, "out")
-    if chosen is None:
-        chosen = torch.empty((tokens, top_k), dtype=torch.int32, device=x.device)
-    if gates is None:
-        gates = torch.empty((tokens, top_k), dtype=torch.float32, device=x.device)
-    for t, dtype, what in ((chosen, torch.int32, "chosen"), (gates, torch.float32, "gates")):
-        if t.shape != (tokens, top_k) or t.dtype != dtype or t.device != x.device or not t.is_contiguous():
+    def small(t, dtype, what):
+        if t is None:
+            return torch.empty((tokens, top_k), dtype=dtype, device=x.device)
+        if t.shape != (tokens, top_k) or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
             raise ValueError(f"{what}: contiguous [{tokens}, {top_k}] of {dtype} on {x.device} expected")
+        return t
+
+    chosen, gates = small(chosen, torch.int32, "chosen"), small(gates, torch.float32, "gates")
     L = _lib or lib()
     keep, ws, nbytes = _workspace(workspace, L.ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, kind)
                                   if workspace is None else 0, x.device)
