@@ -46,8 +46,19 @@ struct MoeArgs {
     int *chosen;
     float *gates;
     void *h, *y;                           // h: [tokens * top_k] rows of the hidden layer, ldh apart
+    float *parts;                          // [moe_out_parts][tokens][width]
     int ldx, ldh, ldy, tokens, width, hidden, experts, top_k, normalise;
 };
+// Parts of the experts' steps that the last launch divides among work-groups of the same features: as many as fill the 256
+// compute units, of at least 8 steps a wavefront (8 tokens, 64 experts of 2048 x 1024: 57 us in one part).
+inline int moe_out_parts(int tokens, int width, int hidden, int experts, int top_k, size_t size)
+{
+    const long long can = (long long)tokens * top_k < experts ? (long long)tokens * top_k : experts;
+    const long long items = can * ((hidden * (long long)size + 127) / 128), groups = (width + 15) / 16;
+    int parts = 1;
+    while (parts < 8 && groups * parts * 2 <= 256 && items / (parts * 2) >= 8 * 16) parts *= 2;
+    return parts;
+}
 hipError_t launch_moe(const MoeArgs &a, int type, hipStream_t st);
 
 }  // namespace oz

@@ -240,19 +240,41 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
     return OZIMMU_OK;
 }
 
+}  // extern "C"
+
+namespace {
+// parts of the workspace of ozimmu_moe
+struct MoeWorkspace {
+    size_t parts, total;
+    int ldh;
+};
+MoeWorkspace moe_workspace(int tokens, int width, int hidden, int experts, int top_k, int type)
+{
+    MoeWorkspace w{};
+    const size_t size = element_bytes(type);
+    const int parts = moe_out_parts(tokens, width, hidden, experts, top_k, size);
+    w.ldh = (hidden + 7) & ~7;
+    w.parts = padded((size_t)tokens * top_k * w.ldh * size);
+    w.total = w.parts + (parts > 1 ? padded((size_t)parts * tokens * width * 4) : 0);
+    return w;
+}
+}  // namespace
+
+extern "C" {
+
 size_t ozimmu_moe_workspace_bytes(int tokens, int width, int hidden, int experts, int top_k, int type)
 {
     if (tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || hidden < 0 || experts < 1 || experts > OZIMMU_MOE_EXPERTS || top_k < 1 ||
         top_k > experts || top_k > OZIMMU_MOE_TOP_K || bad_type(type))
         return 0;
-    return padded((size_t)tokens * top_k * ((hidden + 7) & ~7) * element_bytes(type));
+    return moe_workspace(tokens, width, hidden, experts, top_k, type).total;
 }
 
 int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int type, int normalise, const void *x, int ldx,
                const void *router, const void *w_in, const void *w_out, int32_t *chosen, float *gates, void *y, int ldy,
                void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (bad_type(type) || tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || hidden < 0 || hidden > 0x3fffffff || experts < 1 ||
+    if (bad_type(type) || tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || width > 0x3fffffff || hidden < 0 || hidden > 0x3fffffff || experts < 1 ||
         experts > OZIMMU_MOE_EXPERTS || top_k < 1 || top_k > experts || top_k > OZIMMU_MOE_TOP_K)
         return OZIMMU_BAD_ARG;
     const size_t size = element_bytes(type);
@@ -260,9 +282,11 @@ int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int ty
         bad_rows(2 * hidden, width, w_in, width > 1 ? width : 1, size) || bad_rows(width, hidden, w_out, hidden > 1 ? hidden : 1, size))
         return OZIMMU_BAD_ARG;
     if (tokens > 0 && (!chosen || !gates || (uintptr_t)chosen % 4 || (uintptr_t)gates % 4)) return OZIMMU_BAD_ARG;
-    if (bad_workspace(workspace, workspace_bytes, ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, type))) return OZIMMU_BAD_ARG;
+    const MoeWorkspace ws = moe_workspace(tokens, width, hidden, experts, top_k, type);
+    if (bad_workspace(workspace, workspace_bytes, ws.total)) return OZIMMU_BAD_ARG;
     if (tokens == 0) return OZIMMU_OK;
-    const MoeArgs a{x, router, w_in, w_out, chosen, gates, workspace, y, ldx, (hidden + 7) & ~7, ldy, tokens, width, hidden, experts, top_k, normalise != 0};
+    const MoeArgs a{x, router, w_in, w_out, chosen, gates, workspace, y, (float *)((char *)workspace + ws.parts),
+                    ldx, ws.ldh, ldy, tokens, width, hidden, experts, top_k, normalise != 0};
     return launch_moe(a, type, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
 }
 

@@ -5,7 +5,8 @@
 //   moe_hidden_kernel  a work-group per 16 hidden features of an expert that some token chose: gate and up rows against
 //                      the tokens that chose it, h = gate silu(a) b rounded for the next product
 //   moe_out_kernel     a work-group per 16 output features: their rows of every chosen expert against its tokens' h, all in one
-//                      sum, so nothing is scattered and no atomics change an order
+//                      sum, so nothing is scattered and no atomics change an order; in two to eight parts, which
+//                      moe_join_kernel adds, where the features are too few for all compute units
 //
 // Which experts are chosen is known on the device only: the second launch has a work-group for each of the min(experts,
 // tokens * top_k) experts that can be, which finds its expert in a bit map of the chosen ones and leaves if there is none.
@@ -254,12 +255,13 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
     // The steps of all chosen experts, one after the other, are dealt to the wavefronts in turn; U steps' loads, of as many
     // experts as it may be, are issued before the first of their products.
     const int steps = (a.hidden + KE - 1) / KE, items = chosen * steps;
-    for (int first = wave; first < items; first += U * kOutWaves) {
+    const int part = (items + gridDim.y - 1) / gridDim.y, begin = blockIdx.y * part, end = begin + part < items ? begin + part : items;
+    for (int first = begin + wave; first < end; first += U * kOutWaves) {
         v4u w[U][2], h[U][2][NX];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int item = first + u * kOutWaves;
-            const bool there = item < items;
+            const bool there = item < end;
             const int slot = there ? item / steps : 0, k0 = (there ? item - slot * steps : 0) * KE + g;
             const T *wr = (const T *)a.w_out + ((size_t)experts[slot] * a.width + row) * a.hidden;
             const T *hr[NX];
@@ -306,8 +308,20 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
         float v = 0.0f;
 #pragma unroll
         for (int s = 0; s < kOutWaves; ++s) v += sums[s][q >> 4][(q & 15) * kStreamLd + p];
-        ((T *)a.y)[(size_t)q * a.ldy + p0 + p] = (T)v;
+        if (gridDim.y == 1) ((T *)a.y)[(size_t)q * a.ldy + p0 + p] = (T)v;
+        else a.parts[((size_t)blockIdx.y * a.tokens + q) * a.width + p0 + p] = v;
     }
+}
+
+// the parts' sums, in their order
+template <class T>
+__global__ __launch_bounds__(256) void moe_join_kernel(MoeArgs a, int parts)
+{
+    const size_t all = (size_t)a.tokens * a.width, i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= all) return;
+    float v = 0.0f;
+    for (int y = 0; y < parts; ++y) v += a.parts[y * all + i];
+    ((T *)a.y)[i / a.width * a.ldy + i % a.width] = (T)v;
 }
 
 template <class T>
@@ -330,10 +344,16 @@ hipError_t launch(const MoeArgs &a, hipStream_t st)
     }
     const int groups = (a.width + 15) / 16;
     if (groups == 0) return hipSuccess;
-    if (a.tokens <= 16) moe_out_kernel<T, 1><<<groups, 64 * kOutWaves, 0, st>>>(a);
-    else if (a.tokens <= 32) moe_out_kernel<T, 2><<<groups, 64 * kOutWaves, 0, st>>>(a);
-    else moe_out_kernel<T, 4><<<groups, 64 * kOutWaves, 0, st>>>(a);
-    return hipGetLastError();
+    const dim3 out(groups, moe_out_parts(a.tokens, a.width, a.hidden, a.experts, a.top_k, sizeof(T)));
+    if (a.tokens <= 16) moe_out_kernel<T, 1><<<out, 64 * kOutWaves, 0, st>>>(a);
+    else if (a.tokens <= 32) moe_out_kernel<T, 2><<<out, 64 * kOutWaves, 0, st>>>(a);
+    else moe_out_kernel<T, 4><<<out, 64 * kOutWaves, 0, st>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (out.y > 1) {
+        moe_join_kernel<T><<<(unsigned)(((size_t)a.tokens * a.width + 255) / 256), 256, 0, st>>>(a, (int)out.y);
+        return hipGetLastError();
+    }
+    return hipSuccess;
 }
 
 }  // namespace
