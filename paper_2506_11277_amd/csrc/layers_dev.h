@@ -193,14 +193,20 @@ __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, floa
         }
         store_row((T *)e.out + (size_t)q * e.ldo + p, v);
     } else {
+        float b[8], r[8];                           // (all loads before the first store, which might be to the same place)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool in = p + i < e.np;
+            b[i] = in && e.bias ? (float)((const T *)e.bias)[p + i] : 0.0f;
+            r[i] = in && e.residual ? (float)((const T *)e.residual)[(size_t)q * e.ldr + p + i] : 0.0f;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (p + i >= e.np) continue;
-            float x = v[i];
-            if (e.bias) x += (float)((const T *)e.bias)[p + i];
+            float x = v[i] + b[i];
             if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)x;
             x = activate<T>(e.act, x);
-            if (e.residual) x += (float)((const T *)e.residual)[(size_t)q * e.ldr + p + i];
+            if (e.residual) x += r[i];
             ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)x;
         }
     }

@@ -96,7 +96,7 @@ struct Operand {
     const T *base;
     int ld, rows, row0, nk;
     unsigned off[DIRECT ? N : 1];                                       // bytes behind the step's base
-    v4u reg[DIRECT ? 1 : N];
+    v4u reg[2][DIRECT ? 1 : N];                                         // chunks on their way to LDS, of two steps
 
     static __device__ __forceinline__ int place(int c)                  // LDS row's chunk -> chunk of the row in memory
     {
@@ -169,25 +169,37 @@ struct Operand {
         lds_dma16(from, off[I], lds + (I * WAVES + wave) * 1024);
     }
 
+    template <int S>
     __device__ __forceinline__ void load(int k0, int wave, int lane)
     {
+        if (k0 + KE <= nk && (K_ROWS || row0 + B <= rows)) {            // (the same for all lanes)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int r, c;
+                slot(i, wave, lane, r, c);
+                const T *from = K_ROWS ? base + (size_t)(row0 + r < rows ? row0 + r : rows - 1) * ld + k0 + c * E : base + (size_t)(k0 + r) * ld + row0 + c * E;
+                __builtin_memcpy(&reg[S][i], from, 16);
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             int r, c;
             slot(i, wave, lane, r, c);
             if constexpr (K_ROWS) {
                 const int row = row0 + r < rows ? row0 + r : rows - 1, k = k0 + c * E;
-                reg[i] = load_chunk(base + (size_t)row * ld + k, nk - k);
+                reg[S][i] = load_chunk(base + (size_t)row * ld + k, nk - k);
             } else {
                 const int k = k0 + r, col = row0 + c * E;
-                reg[i] = load_chunk(base + (size_t)k * ld + col, k < nk ? rows - col : 0);
+                reg[S][i] = load_chunk(base + (size_t)k * ld + col, k < nk ? rows - col : 0);
             }
         }
     }
+    template <int S>
     __device__ __forceinline__ void store(char *lds, int wave, int lane)
     {
 #pragma unroll
-        for (int i = 0; i < N; ++i) *(v4u *)(lds + ((i * WAVES + wave) * 64 + lane) * 16) = reg[i];
+        for (int i = 0; i < N; ++i) *(v4u *)(lds + ((i * WAVES + wave) * 64 + lane) * 16) = reg[S][i];
     }
 
     // Where a lane finds its operands in a stage: fragment() of rows w0 + 16 f ... + 15 (w0: a wavefront's part, a multiple of
@@ -243,7 +255,6 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
     static_assert(QW % (ROWS * R) == 0, "");
     const int col = lane % LANES * 8, p = p0 + col;
     if (p >= e.np) return;
-    const bool whole = e.wide && p + 8 <= e.np;
 #pragma nounroll
     for (int s = lane / LANES; s < QW && q0 + s < e.nq; s += R * ROWS) {
         float v[R][8], res[R][8];
@@ -257,12 +268,6 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
 #pragma unroll
             for (int y = 0; y < R; ++y)
                 if (q0 + s + y * ROWS < e.nq) store_row(partial + ((size_t)blockIdx.y * e.nq + q0 + s + y * ROWS) * ldn + p, v[y]);
-            continue;
-        }
-        if (!whole) {
-#pragma unroll
-            for (int y = 0; y < R; ++y)
-                if (q0 + s + y * ROWS < e.nq) finish_row<T>(e, q0 + s + y * ROWS, p, v[y]);
             continue;
         }
         if (e.residual)
@@ -286,16 +291,57 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
     }
 }
 
+// ... entry by entry, where rows are not aligned or end within 8 entries: consecutive lanes take consecutive entries, four
+// rows at a time
+template <class T, int ACT, int PW, int QW>
+__device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float *sums, int q0, int p0, int lane)
+{
+    constexpr int LD = PW + 4, W = PW < 64 ? PW : 64, ROWS = 64 / W, R = 4;
+    static_assert(QW % (ROWS * R) == 0, "");
+#pragma nounroll
+    for (int c = lane % W; c < PW; c += W) {
+        const int p = p0 + c;
+        if (p >= e.np) break;
+        const float bias = e.bias ? (float)((const T *)e.bias)[p] : 0.0f;
+#pragma nounroll
+        for (int s = lane / W; s < QW && q0 + s < e.nq; s += R * ROWS) {
+            float v[R], res[R];
+#pragma unroll
+            for (int y = 0; y < R; ++y) {
+                const int q = q0 + s + y * ROWS;
+                v[y] = sums[(s + y * ROWS) * LD + c] + bias;
+                res[y] = e.residual && q < e.nq ? (float)((const T *)e.residual)[(size_t)q * e.ldr + p] : 0.0f;
+            }
+#pragma unroll
+            for (int y = 0; y < R; ++y) {
+                const int q = q0 + s + y * ROWS;
+                if (q >= e.nq) continue;
+                if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p] = (T)v[y];
+                float x = activate<T>(ACT, v[y]);
+                if (e.residual) x += res[y];
+                ((T *)e.out)[(size_t)q * e.ldo + p] = (T)x;
+            }
+        }
+    }
+}
+
+template <class T, int ACT, int PW, int QW>
+__device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
+{
+    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, ACT, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+    else epilogue_entries<T, ACT, PW, QW>(e, sums, q0, p0, lane);
+}
+
 template <class T, int PW, int QW>
 __device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
 {
     switch (e.act) {                                // (decided once: a lane's entries decide nothing)
-        case OZIMMU_ACT_RELU: return epilogue_rows<T, OZIMMU_ACT_RELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU: return epilogue_rows<T, OZIMMU_ACT_GELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU_TANH: return epilogue_rows<T, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-        case OZIMMU_ACT_SILU: return epilogue_rows<T, OZIMMU_ACT_SILU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_RELU: return epilogue_as<T, OZIMMU_ACT_RELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU: return epilogue_as<T, OZIMMU_ACT_GELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_SILU: return epilogue_as<T, OZIMMU_ACT_SILU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
     }
-    epilogue_rows<T, OZIMMU_ACT_NONE, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+    epilogue_as<T, OZIMMU_ACT_NONE, PW, QW>(e, partial, bias, sums, q0, p0, lane);
 }
 
 // one tile, or one part of its contraction
@@ -422,28 +468,33 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
         half(second, none, 0, nothing);
         static_for<0, FP>([&](auto I) __attribute__((always_inline)) { settle<(S::kAlone && I < FP - 1)>(acc[I]); });
     } else {
-        if (t0 < t1) {
-            P.load(t0 * KE, wave, lane);
-            Q.load(t0 * KE, wave, lane);
-            P.store(lds, wave, lane);
-            Q.store(lds + BP * 128, wave, lane);
-        }
-        for (int t = t0; t < t1; ++t) {
-            const int now = (t - t0) & 1;
+        // the chunks of a step are loaded two steps ahead (one: 24 us for 1531 x 1001 x 777 f16)
+        auto load = [&](int t, auto X) __attribute__((always_inline)) {
+            P.template load<X>(t * KE, wave, lane);
+            Q.template load<X>(t * KE, wave, lane);
+        };
+        auto store = [&](auto X) __attribute__((always_inline)) {       // set and stage go by the step's parity
+            P.template store<X>(lds + X * S::kStage, wave, lane);
+            Q.template store<X>(lds + X * S::kStage + BP * 128, wave, lane);
+        };
+        auto step = [&](int t, auto X) __attribute__((always_inline)) { // a step of parity X
+            constexpr std::integral_constant<int, 1 - X> other{};
             __syncthreads();
-            if (t + 1 < t1) {
-                P.load((t + 1) * KE, wave, lane);
-                Q.load((t + 1) * KE, wave, lane);
-            }
-            read(now, first);
-            read(now, second);
+            if (t + 2 < t1) load(t + 2, X);
+            read(X, first);
+            read(X, second);
             products(first);
             products(second);
-            if (t + 1 < t1) {
-                char *to = lds + (now ^ 1) * S::kStage;
-                P.store(to, wave, lane);
-                Q.store(to + BP * 128, wave, lane);
-            }
+            if (t + 1 < t1) store(other);
+        };
+        if (t0 < t1) {
+            load(t0, first);
+            if (t0 + 1 < t1) load(t0 + 1, second);
+            store(first);
+        }
+        for (int t = t0; t < t1; t += 2) {
+            step(t, first);
+            if (t + 1 < t1) step(t + 1, second);
         }
     }
     const int q0 = tq * BQ + wq, p0 = tp * BP + wp;
