@@ -71,7 +71,7 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
  * One AdamW step, in place, over `tensors` tensors of `list` [host, read before the call returns]:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
  *   p = (1 - lr weight_decay) p - lr / (1 - beta1^step)  m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in 32 bits, every operation rounded by itself.  step counts from 1.
+ * in 32 bits, m and v rounded operation by operation, the quotient to two units.  step counts from 1.
  *   grads [host]  the gradients' pointers, or NULL: those of the list.
  *   state_type OZIMMU_F32: m and v are floats.  OZIMMU_E4M3: blocks of 256 consecutive values (the last one of a tensor may
  *     be shorter) hold m and sqrt(v) as m[i] * m_scale[i / 256] and v[i] * v_scale[i / 256], m[i] and v[i] e4m3 (a sign bit,

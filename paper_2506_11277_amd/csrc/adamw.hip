@@ -4,24 +4,27 @@
 //   p = (1 - lr wd) p - lr / (1 - beta1^t)  m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
 //
 // Bound by memory: every value is read and written once.  A launch takes up to kTensors tensors whose addresses are kernel
-// arguments (no table in memory to copy or to keep), cut into chunks of whole blocks of 256 values; a wavefront has a block at
-// a time, four consecutive values a lane.
+// arguments (no table in memory to copy or to keep), cut into chunks of whole blocks of 256 values; a wavefront has one or
+// two blocks at a time, four or eight consecutive values a lane.
 //
 // 8 bits: blocks of 256 values share a scale, and m and sqrt(v) are held as e4m3 times scale (the root halves the range of
-// exponents that v needs; a block's largest value maps to 448).  A wavefront has the whole block, so its maximum takes six
-// exchanges between lanes and no LDS.  Values are rounded up or down at random, with the probability that makes the
+// exponents that v needs; a block's largest value maps to 448).  Half a wavefront has the whole block, so its maximum takes five
+// exchanges between lanes.  Values are rounded up or down at random, with the probability that makes the
 // mean right: 0.999 v + 0.001 g^2 moves v by less than half a unit of its last place, so that rounding to nearest would
 // leave it where it is for ever.  The random word is a hash of the place, the step and the caller's seed.  A root that is not 0 is
 // not rounded to 0, which would leave eps alone below an m that is still there.
 //
-// Every operation is rounded by itself (no fused multiply-add), so that the 8-bit codes are those of the formulas
-// whatever the compiler makes of them.
+// What the states keep is rounded as written, operation by operation (no fused multiply-add, a rounded root), so that the same step
+// gives the same codes whatever the compiler makes of it; the parameter's quotient is the instruction's reciprocal, a unit
+// off in a step a thousandth of p.
+// Measured: 143 million values, bf16 with 8 bits, 1.44 GB: 290 us; 57 million, float with a bf16 copy, 1.58 GB: 305 us (a copy
+// at 5.1 TB/s: 282 and 310).  The first in four values a lane, with the library's root and division: 355 us, bound by arithmetic.
 #include "layers.h"
 
 namespace oz {
 namespace {
 
-constexpr int kBlock = 256;
+constexpr int kBlock = 256;                      // values that share a scale in 8 bits
 constexpr int kTensors = 48;                     // 48 * 80 + 56 bytes of arguments
 
 struct Tensor {
@@ -33,106 +36,193 @@ struct Tensor {
     long long n;
     long long block0;                            // number of its first block among all tensors of the call
     int chunk0;                                  // its first chunk (work-group) in the launch
-    int flags;                                   // kWide, copy type
+    int flags;                                   // copy type
 };
-enum { kWide = 1, kCopyF16 = 2 };
+enum { kCopyF16 = 1 };
 
 struct Args {
     Tensor t[kTensors];
-    int tensors, per_chunk;                      // blocks of a chunk
+    int tensors, per_chunk;                      // blocks of a chunk, even
     float b1, c1, b2, c2, eps, rate, correction, keep;
     unsigned word0;
 };
 static_assert(sizeof(Args) <= 4096, "kernel arguments");
 
-template <class T>
-__device__ __forceinline__ void get4(const T *p, int n, bool wide, float (&v)[4])
+// a lane's values: together at any alignment of their type, or the n that are there, the others 0
+template <class T, int kEach>
+__device__ __forceinline__ void get(const T *p, int n, float (&v)[kEach])
 {
-    if (wide && n >= 4) {
-        load_row(p, v);
+    if (n >= kEach) {
+        T x[kEach];
+        __builtin_memcpy(x, p, sizeof(x));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[i] = (float)x[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+        for (int i = 0; i < kEach; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
     }
 }
-template <class T>
-__device__ __forceinline__ void put4(T *p, int n, bool wide, const float (&v)[4])
+template <class T, int kEach>
+__device__ __forceinline__ void put(T *p, int n, const float (&v)[kEach])
 {
-    if (wide && n >= 4) {
-        store_row(p, v);
+    if (n >= kEach) {
+        T x[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x[i] = (T)v[i];
+        __builtin_memcpy(p, x, sizeof(x));
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < kEach; ++i)
             if (i < n) p[i] = (T)v[i];
     }
 }
 
-__device__ __forceinline__ unsigned get_codes(const uint8_t *p, int n, bool wide)
+constexpr int kEach = 8;                         // values of a lane where states have 8 bits
+
+__device__ __forceinline__ v2u get_codes(const uint8_t *p, int n)
 {
-    if (wide && n >= 4) return *(const unsigned *)p;
-    unsigned c = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < n) c |= (unsigned)p[i] << (8 * i);
-    return c;
-}
-__device__ __forceinline__ void put_codes(uint8_t *p, int n, bool wide, unsigned c)
-{
-    if (wide && n >= 4) {
-        *(unsigned *)p = c;
+    v2u c = {0, 0};
+    if (n >= kEach) {
+        __builtin_memcpy(&c, p, 8);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = (uint8_t)(c >> (8 * i));
+        for (int i = 0; i < kEach; ++i)
+            if (i < n) c[i >> 2] |= (unsigned)p[i] << (8 * (i & 3));
+    }
+    return c;
+}
+__device__ __forceinline__ void put_codes(uint8_t *p, int n, v2u c)
+{
+    if (n >= kEach) {
+        __builtin_memcpy(p, &c, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (i < n) p[i] = (uint8_t)(c[i >> 2] >> (8 * (i & 3)));
     }
 }
-__device__ __forceinline__ void decode(unsigned c, float scale, float (&v)[4])
+__device__ __forceinline__ void decode(v2u c, float scale, float (&v)[kEach])
 {
     typedef float v2f __attribute__((ext_vector_type(2)));
-    const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-    v[0] = a[0] * scale;
-    v[1] = a[1] * scale;
-    v[2] = b[0] * scale;
-    v[3] = b[1] * scale;
-}
-
-__device__ __forceinline__ unsigned word_of(unsigned long long at, unsigned word0)
-{
-    unsigned h = ((unsigned)at + (unsigned)(at >> 32) * 0x6a09e667u) * 0x9e3779b1u + word0;
-    h = (h ^ (h >> 15)) * 0x6a09e667u;
-    h = (h ^ (h >> 13)) * 0xbb67ae85u;
-    return h ^ (h >> 16);
-}
-
-// the largest finite magnitude of a block, in every lane
-__device__ __forceinline__ float block_max(const float (&x)[4])
-{
-    float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float a = fabsf(x[i]);
-        top = a < __builtin_inff() ? fmaxf(top, a) : top;
+    for (int h = 0; h < 2; ++h) {
+        const v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(c[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(c[h], true);
+        v[4 * h] = a[0] * scale;
+        v[4 * h + 1] = a[1] * scale;
+        v[4 * h + 2] = b[0] * scale;
+        v[4 * h + 3] = b[1] * scale;
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    return top;
 }
 
-// |x| as e4m3 of 448 / top, rounded up where the 20 bits below carry with the word's.  y 2^-120 has the bits of e4m3 (bias 7
-// instead of 127) 20 places further left, also where e4m3 is subnormal.
-__device__ __forceinline__ unsigned hold(float x, float inverse, unsigned word)
+// the words of a lane's places from `at` on, a multiple of 8 (so that they share the upper half)
+__device__ __forceinline__ void words_of(unsigned long long at, unsigned word0, unsigned (&w)[kEach])
 {
-    const float a = fabsf(x);
-    if (!(a < __builtin_inff())) return 0x7f;                           // NaN
-    const float y = fminf(a * inverse, 448.0f) * 0x1p-120f;
-    const unsigned c = (__float_as_uint(y) + word) >> 20;
-    return c < 0x7e ? c : 0x7e;
+    const unsigned first = ((unsigned)at + (unsigned)(at >> 32) * 0x6a09e667u) * 0x9e3779b1u + word0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        unsigned h = first + i * 0x9e3779b1u;
+        h = (h ^ (h >> 15)) * 0x6a09e667u;
+        h = (h ^ (h >> 13)) * 0xbb67ae85u;
+        w[i] = h ^ (h >> 16);
+    }
+}
+
+// Square roots.  The instruction is a unit off at times and takes no subnormal numbers: where a wavefront has values below 2^-96,
+// all are scaled.  ROUNDED: the neighbour is taken where the residual says so (0, infinities and NaN stay as they are).
+template <bool ROUNDED, int N>
+__device__ __forceinline__ void roots_of(const float (&v)[N], float (&root)[N])
+{
+    auto root_of = [](float x) {
+        const float r = __builtin_amdgcn_sqrtf(x);
+        if constexpr (!ROUNDED) return r;
+        const float below = __uint_as_float(__float_as_uint(r) - 1), above = __uint_as_float(__float_as_uint(r) + 1);
+        const float e = __builtin_fmaf(-below, r, x), f = __builtin_fmaf(-above, r, x);
+        const float s = e <= 0.0f ? below : r;
+        return f > 0.0f ? above : s;
+    };
+    float least = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) least = fminf(least, v[i]);
+    if (__builtin_expect(__ballot(least < 0x1p-96f) != 0, 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool tiny = v[i] < 0x1p-96f;
+            const float r = root_of(tiny ? v[i] * 0x1p96f : v[i]);
+            root[i] = tiny ? r * 0x1p-48f : r;
+        }
+        asm volatile("");                            // (a branch, not a selection for each)
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) root[i] = root_of(v[i]);
+    }
+}
+
+// the largest of a block's values, in each of its 32 lanes: among 16 by exchanges inside the vector unit, the last one through LDS's crossbar
+__device__ __forceinline__ unsigned lanes_max(unsigned x)
+{
+    auto with = [&](unsigned o) { x = o > x ? o : x; };
+    with(__builtin_amdgcn_mov_dpp(x, 0xb1, 0xf, 0xf, true));         // lane ^ 1
+    with(__builtin_amdgcn_mov_dpp(x, 0x4e, 0xf, 0xf, true));         // lane ^ 2
+    with(__builtin_amdgcn_mov_dpp(x, 0x141, 0xf, 0xf, true));        // 7 - lane within 8
+    with(__builtin_amdgcn_mov_dpp(x, 0x140, 0xf, 0xf, true));        // 15 - lane within 16
+    with(__builtin_amdgcn_ds_swizzle(x, 0x401f));                    // lane ^ 16
+    return x;
+}
+
+// A block's moments in 8 bits: |x| 448 / top, rounded up where the 20 bits below e4m3's carry with the word's.  y 2^-120 has the
+// bits of e4m3 (bias 7 instead of 127) 20 places further left, also where e4m3 is subnormal, so that one multiplication,
+// addition and shift make the code.  ROOT: no signs, and a value that is not 0 does not become 0.
+template <bool ROOT>
+__device__ __forceinline__ v2u hold_block(const float (&x)[kEach], const unsigned (&word)[kEach], float &scale)
+{
+    constexpr unsigned kInf = 0x7f800000u;
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const unsigned a = __float_as_uint(x[i]) & 0x7fffffffu;
+        top = a > top ? a : top;
+    }
+    top = lanes_max(top);
+    const bool odd = __ballot(top >= kInf) != 0;     // a value that is not finite: the scale goes by the others
+    if (__builtin_expect(odd, 0)) {
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const unsigned a = __float_as_uint(x[i]) & 0x7fffffffu;
+            top = a > top && a < kInf ? a : top;
+        }
+        top = lanes_max(top);
+        asm volatile("");
+    }
+    const float t = __uint_as_float(top);
+    scale = t * (float)(1.0 / 448.0);
+    // (below 2^-100 the quotient would overflow: such a block is held as zeros, or the smallest code)
+    const float factor = t >= 0x1p-100f ? 448.0f / t * 0x1p-120f : 0.0f;
+    v2u codes = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        unsigned c = (__float_as_uint(fabsf(x[i]) * factor) + word[i]) >> 20;
+        c = c < 0x7e ? c : 0x7e;
+        if constexpr (ROOT) {
+            const unsigned least = __float_as_uint(x[i]) < 1 ? __float_as_uint(x[i]) : 1;       // 0 of 0 (roots have no sign)
+            c = c > least ? c : least;
+        } else {
+            c |= __float_as_uint(x[i]) >> 24 & 0x80;
+        }
+        codes[i >> 2] |= c << (8 * (i & 3));
+    }
+    if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if ((__float_as_uint(x[i]) & 0x7fffffffu) >= kInf) codes[i >> 2] |= 0x7fu << (8 * (i & 3));
+        asm volatile("");
+    }
+    return codes;
 }
 
 template <class P, class G, bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(const Args a)
 {
-#pragma clang fp contract(off)
     // the tensor of this chunk: the last one that starts at or before it (the same search in every lane, on scalars)
     int lo = 0, hi = a.tensors;
     while (hi - lo > 1) {
@@ -142,61 +232,66 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Args a)
     }
     const Tensor &t = a.t[lo];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const bool wide = t.flags & kWide;
     const long long blocks = (t.n + kBlock - 1) / kBlock;
     const long long first = (long long)((int)blockIdx.x - t.chunk0) * a.per_chunk;
     const long long last = first + a.per_chunk < blocks ? first + a.per_chunk : blocks;
-#pragma unroll 2
-    for (long long b = first + wave; b < last; b += 4) {
-        const long long at = b * kBlock + lane * 4;
-        const int n = t.n - at < 4 ? (t.n > at ? (int)(t.n - at) : 0) : 4;
-        float p[4], g[4], m[4], v[4], root[4];
-        get4((const P *)t.p + at, n, wide, p);
-        get4((const G *)t.g + at, n, wide, g);
+    // 32 bits: four values a lane, a wavefront has a block at a time (eight: 337 us instead of 305 for 57 million values, the
+    // loads of 16 bytes being 32 apart).  8 bits: eight, two blocks.
+    constexpr int N = EIGHT ? kEach : 4, kLanes = kBlock / N, kBlocks = 64 / kLanes;
+    for (long long some = first + kBlocks * wave; some < last; some += 4 * kBlocks) {
+        // (the second block may not be there: n is then 0, and its scales are not touched)
+        const long long b = some + lane / kLanes, at = b * kBlock + lane % kLanes * N;
+        const int n = t.n - at < N ? (t.n > at ? (int)(t.n - at) : 0) : N;
+        float p[N], g[N], m[N], v[N], root[N];
+        get((const P *)t.p + at, n, p);
+        get((const G *)t.g + at, n, g);
         if constexpr (EIGHT) {
-            const unsigned mc = get_codes((const uint8_t *)t.m + at, n, wide), vc = get_codes((const uint8_t *)t.v + at, n, wide);
-            decode(mc, t.ms[b], m);
-            decode(vc, t.vs[b], v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = v[i] * v[i];
+            const v2u mc = get_codes((const uint8_t *)t.m + at, n), vc = get_codes((const uint8_t *)t.v + at, n);
+            decode(mc, b < blocks ? t.ms[b] : 0.0f, m);
+            decode(vc, b < blocks ? t.vs[b] : 0.0f, v);
         } else {
-            get4((const float *)t.m + at, n, wide, m);
-            get4((const float *)t.v + at, n, wide, v);
+            get((const float *)t.m + at, n, m);
+            get((const float *)t.v + at, n, v);
         }
+        {
+#pragma clang fp contract(off)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            m[i] = m[i] * a.b1 + g[i] * a.c1;
-            v[i] = v[i] * a.b2 + (g[i] * g[i]) * a.c2;
-            root[i] = __fsqrt_rn(v[i]);
-            p[i] = p[i] * a.keep - __fdiv_rn(m[i], root[i] * a.correction + a.eps) * a.rate;
+            for (int i = 0; i < N; ++i) {
+                if (EIGHT) v[i] = v[i] * v[i];
+                m[i] = m[i] * a.b1 + g[i] * a.c1;
+                v[i] = v[i] * a.b2 + (g[i] * g[i]) * a.c2;
+            }
         }
-        put4((P *)t.p + at, n, wide, p);
+        roots_of<EIGHT>(v, root);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float update = m[i] * __builtin_amdgcn_rcpf(__builtin_fmaf(root[i], a.correction, a.eps));
+            p[i] = __builtin_fmaf(update, -a.rate, p[i] * a.keep);
+        }
+        put((P *)t.p + at, n, p);
         if (t.copy) {
-            if (t.flags & kCopyF16) put4((f16 *)t.copy + at, n, wide, p);
-            else put4((bf16 *)t.copy + at, n, wide, p);
+            if (t.flags & kCopyF16) put((f16 *)t.copy + at, n, p);
+            else put((bf16 *)t.copy + at, n, p);
         }
         if constexpr (EIGHT) {
-            const float mt = block_max(m), vt = block_max(root);
-            // (below 2^-100 the inverse would overflow: such a block is held as zeros)
-            const float mi = mt >= 0x1p-100f ? __fdiv_rn(448.0f, mt) : 0.0f, vi = vt >= 0x1p-100f ? __fdiv_rn(448.0f, vt) : 0.0f;
-            unsigned mc = 0, vc = 0;
+            unsigned w[N], low[N];
+            words_of((unsigned long long)t.block0 * kBlock + at, a.word0, w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned w = word_of((unsigned long long)t.block0 * kBlock + at + i, a.word0);
-                const unsigned c = hold(m[i], mi, w & 0xfffff);
-                mc |= (c | (__float_as_uint(m[i]) >> 31) << 7) << (8 * i);
-                const unsigned r = hold(root[i], vi, w >> 12);
-                vc |= (r == 0 && root[i] > 0.0f ? 1u : r) << (8 * i);
+            for (int i = 0; i < N; ++i) {
+                low[i] = w[i] & 0xfffff;
+                w[i] >>= 12;
             }
-            put_codes((uint8_t *)t.m + at, n, wide, mc);
-            put_codes((uint8_t *)t.v + at, n, wide, vc);
-            if (lane == 0) {
-                t.ms[b] = mt * (float)(1.0 / 448.0);
-                t.vs[b] = vt * (float)(1.0 / 448.0);
+            float ms, vs;
+            const v2u mc = hold_block<false>(m, low, ms), vc = hold_block<true>(root, w, vs);
+            put_codes((uint8_t *)t.m + at, n, mc);
+            put_codes((uint8_t *)t.v + at, n, vc);
+            if (lane % kLanes == 0 && b < blocks) {
+                t.ms[b] = ms;
+                t.vs[b] = vs;
             }
         } else {
-            put4((float *)t.m + at, n, wide, m);
-            put4((float *)t.v + at, n, wide, v);
+            put((float *)t.m + at, n, m);
+            put((float *)t.v + at, n, v);
         }
     }
 }
@@ -254,7 +349,7 @@ extern "C" int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const 
     a.correction = (float)(1.0 / __builtin_sqrt(1.0 - __builtin_pow(beta2, (double)step)));
     a.keep = (float)(1.0 - lr * weight_decay);
     a.word0 = seed + (uint32_t)step * 0xbb67ae85u;
-    a.per_chunk = total > 16 * 4096 ? 16 : total > 4 * 2048 ? 8 : 4;
+    a.per_chunk = total > 16 * 4096 ? 16 : 8;       // blocks of a work-group: 2 or 4 (8 bits: 1 or 2) rounds of its wavefronts
     const hipStream_t st = (hipStream_t)stream;
 
     long long block0 = 0, chunks = 0;
@@ -281,12 +376,8 @@ extern "C" int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const 
             kind[1] = x.grad_type;
             kind[2] = x.state_type;
         }
-        // four values at a time: 16 bytes of 32 bits, 8 of 16, 4 of 8
-        auto off = [](const void *p, int type) { return (uintptr_t)p & (type == OZIMMU_F32 ? 15 : type == OZIMMU_E4M3 ? 3 : 7); };
-        const bool wide = !(off(x.param, x.param_type) | off(g, x.grad_type) | off(x.m, x.state_type) | off(x.v, x.state_type) |
-                            (x.copy ? off(x.copy, x.copy_type) : 0));
         a.t[a.tensors++] = Tensor{x.param, g, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.count, block0, (int)chunks,
-                                  (wide ? kWide : 0) | (x.copy && x.copy_type == OZIMMU_F16 ? kCopyF16 : 0)};
+                                  x.copy && x.copy_type == OZIMMU_F16 ? kCopyF16 : 0};
         block0 += blocks;
         chunks += need;
     }
