@@ -255,6 +255,10 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
     static_assert(QW % (ROWS * R) == 0, "");
     const int col = lane % LANES * 8, p = p0 + col;
     if (p >= e.np) return;
+    auto write = [](T *to, const float (&x)[8]) __attribute__((always_inline)) {
+        if constexpr (PW == 128) stream_row(to, x);
+        else store_row(to, x);
+    };
 #pragma nounroll
     for (int s = lane / LANES; s < QW && q0 + s < e.nq; s += R * ROWS) {
         float v[R][8], res[R][8];
@@ -280,13 +284,13 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
             if (q >= e.nq) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[y][i] += bias[i];
-            if (e.pre) store_row((T *)e.pre + (size_t)q * e.ldpre + p, v[y]);
+            if (e.pre) write((T *)e.pre + (size_t)q * e.ldpre + p, v[y]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[y][i] = activate<T>(ACT, v[y][i]);
             if (e.residual)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[y][i] += res[y][i];
-            store_row((T *)e.out + (size_t)q * e.ldo + p, v[y]);
+            write((T *)e.out + (size_t)q * e.ldo + p, v[y]);
         }
     }
 }

@@ -44,3 +44,24 @@ def test_c_has_streaming_and_plain_stores(kernels, kernel):
     assert stores, sorted(kernels)[:5]
     for s in stores:
         assert any(" nt" in line for line in s) and any(" nt" not in line for line in s), (kernel, s[:4])
+
+
+@pytest.mark.parametrize("tile", [256, 128, 64])
+@pytest.mark.parametrize("kind", ["DF16b", "DF16_", "f"])
+def test_written_products_are_left_where_they_are(kernels, kind, tile):
+    # The tiled products' matrix instructions are written out, so the compiler does not know that their results take a while: behind
+    # one, up to a branch or the waits that follow the last one, it must not read an accumulator register elsewhere or spill one.
+    name = r"product_(kernelI%sLb[01]ELb[01]ELi%dELi%dE.*Lb1E|pair_kernelI%sLi%dE)" % (kind, tile, tile, kind, tile)
+    bodies = [b for n, b in kernels.items() if re.search(name, n)]
+    assert len(bodies) >= (0 if kind == "f" and tile == 256 else 3)
+    for body in bodies:
+        lines = [line.strip() for line in body.splitlines() if re.match(r"\s+[a-z]+_", line)]
+        behind, seen = False, 0
+        for line in lines:
+            if line.startswith("v_mfma"):
+                behind, seen = True, seen + 1
+            elif line.startswith(("s_branch", "s_cbranch", "s_endpgm")) or line.split("//")[0].split() == ["s_nop", "15"]:
+                behind = False
+            elif behind:
+                assert not line.startswith(("v_accvgpr_read", "v_accvgpr_mov", "scratch_store")), line
+        assert seen
