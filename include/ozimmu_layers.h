@@ -103,8 +103,8 @@ int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const void *const
  *   y = sum over the chosen experts e of  gate_e w_out[e] (silu(w_in[e][0 ... hidden) x) * (w_in[e][hidden ... 2 hidden) x))
  *   x, y [tokens, width]; router [experts, width], w_in [experts, 2 hidden, width], w_out [experts, width, hidden] contiguous;
  *   all of `type`.  chosen [tokens, top_k]: the experts of each token in ascending order; gates: theirs, float.
- * The products of the hidden layer are rounded to `type` with their gate for the second product (one rounding).  A NaN
- * logit counts as larger than any number.
+ * The values of the hidden layer, with their gate, go into the second product as one float or as the sum of two numbers of
+ * 16 bits.  A NaN logit counts as larger than any number.
  * 1 <= top_k <= experts <= OZIMMU_MOE_EXPERTS, top_k <= OZIMMU_MOE_TOP_K.
  */
 #define OZIMMU_MOE_TOKENS 64

@@ -45,7 +45,7 @@ struct MoeArgs {
     const void *x, *router, *w_in, *w_out;
     int *chosen;
     float *gates;
-    void *h, *y;                           // h: [tokens * top_k] rows of the hidden layer, ldh apart
+    void *h, *y;                           // h: [tokens * top_k] rows of the hidden layer, ldh apart (16 bits: and again, what the first ones leave)
     float *parts;                          // [moe_out_parts][tokens][width]
     int ldx, ldh, ldy, tokens, width, hidden, experts, top_k, normalise;
 };

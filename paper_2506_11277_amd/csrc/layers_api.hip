@@ -254,7 +254,7 @@ MoeWorkspace moe_workspace(int tokens, int width, int hidden, int experts, int t
     const size_t size = element_bytes(type);
     const int parts = moe_out_parts(tokens, width, hidden, experts, top_k, size);
     w.ldh = (hidden + 7) & ~7;
-    w.parts = padded((size_t)tokens * top_k * w.ldh * size);
+    w.parts = padded((size_t)tokens * top_k * w.ldh * 4);           // (one number of 32 bits or two of 16)
     w.total = w.parts + (parts > 1 ? padded((size_t)parts * tokens * width * 4) : 0);
     return w;
 }

@@ -18,6 +18,10 @@ namespace {
 
 constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 16;
 constexpr int kWords = OZIMMU_MOE_EXPERTS / 32;
+// The hidden layer is kept as the sum of two numbers of 16 bits: rounded to one, it alone would add as much to the result's error as
+// the result's own rounding.  The second one's products take matrix instructions that wait for memory anyway.
+template <class T>
+constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
 constexpr int kRouteHere = 64;                                  // choices that fit the second kernel's own routing
 
 // bit map of the experts that the `n` choices name
@@ -219,7 +223,10 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
                 u += sums[s][1][q * kStreamLd + f];
             }
             const int choice = choices[c0 + q];
-            ((T *)a.h)[(size_t)choice * a.ldh + f0 + f] = (T)(gates[choice] * activate<T>(OZIMMU_ACT_SILU, g) * u);
+            const float h = gates[choice] * activate<T>(OZIMMU_ACT_SILU, g) * u;
+            T *to = (T *)a.h + (size_t)choice * a.ldh + f0 + f;
+            *to = (T)h;
+            if constexpr (kParts<T> == 2) to[(size_t)all * a.ldh] = (T)(fabsf(h) < __builtin_inff() ? h - (float)(T)h : 0.0f);
         }
         __syncthreads();
     }
@@ -228,7 +235,7 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
 template <class T, int NX>
 __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
 {
-    constexpr int E = Chunk<T>::E, KE = 8 * E, U = NX == 1 ? 4 : 2;
+    constexpr int E = Chunk<T>::E, KE = 8 * E, H = kParts<T>, U = NX == 1 ? (H == 2 ? 3 : 4) : NX == 2 ? 2 : H == 2 ? 1 : 2;
     constexpr int kNone = 255;
     __shared__ unsigned map[kWords];
     __shared__ int experts[OZIMMU_MOE_EXPERTS];                                // the chosen ones
@@ -255,9 +262,10 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
     // The steps of all chosen experts, one after the other, are dealt to the wavefronts in turn; U steps' loads, of as many
     // experts as it may be, are issued before the first of their products.
     const int steps = (a.hidden + KE - 1) / KE, items = chosen * steps;
+    const size_t second = (size_t)all * a.ldh;                                 // from h's first numbers to its second ones
     const int part = (items + gridDim.y - 1) / gridDim.y, begin = blockIdx.y * part, end = begin + part < items ? begin + part : items;
     for (int first = begin + wave; first < end; first += U * kOutWaves) {
-        v4u w[U][2], h[U][2][NX];
+        v4u w[U][2], h[U][2][NX][H];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int item = first + u * kOutWaves;
@@ -278,8 +286,11 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
                     __builtin_memcpy(&w[u][s], wr + k0 + s * 4 * E, 16);
 #pragma unroll
                     for (int j = 0; j < NX; ++j) {
-                        h[u][s][j] = v4u{0, 0, 0, 0};
-                        if (on[j]) __builtin_memcpy(&h[u][s][j], hr[j] + k0 + s * 4 * E, 16);
+#pragma unroll
+                        for (int o = 0; o < H; ++o) {
+                            h[u][s][j][o] = v4u{0, 0, 0, 0};
+                            if (on[j]) __builtin_memcpy(&h[u][s][j][o], hr[j] + o * second + k0 + s * 4 * E, 16);
+                        }
                     }
                 }
             } else {
@@ -288,7 +299,9 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
                     const int k = k0 + s * 4 * E, n = there ? a.hidden - k : 0;
                     w[u][s] = load_chunk(wr + k, n);
 #pragma unroll
-                    for (int j = 0; j < NX; ++j) h[u][s][j] = load_chunk(hr[j] + k, on[j] ? n : 0);
+                    for (int j = 0; j < NX; ++j)
+#pragma unroll
+                        for (int o = 0; o < H; ++o) h[u][s][j][o] = load_chunk(hr[j] + o * second + k, on[j] ? n : 0);
                 }
             }
         }
@@ -297,7 +310,9 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int j = 0; j < NX; ++j) acc[j] = mma(w[u][s], h[u][s][j], acc[j], T{});
+                for (int o = 0; o < H; ++o)
+#pragma unroll
+                    for (int j = 0; j < NX; ++j) acc[j] = mma(w[u][s], h[u][s][j][o], acc[j], T{});
     }
 #pragma unroll
     for (int j = 0; j < NX; ++j) put_sums(sums[wave][j], acc[j], lane);
