@@ -15,7 +15,8 @@
  *   - Sums, activations and statistics are formed in 32 bits; what is written in 16 bits is rounded to nearest once.
  *     Results are deterministic (no atomics on floating-point values; the order of every sum is fixed by the sizes).
  *   - NaN and infinities go where the formulas take them; no entry point looks for them.
- *   - Sizes of 0 are accepted: no tokens or no output features write nothing, n_in = 0 gives products of 0.
+ *   - Sizes of 0 are accepted: no tokens or no output features write nothing, n_in = 0 gives products of 0.  Sizes up to
+ *     2^30 - 1 (ozimmu_moe's width and hidden: 2^24), offsets in 64 bits.
  */
 #ifndef OZIMMU_LAYERS_H
 #define OZIMMU_LAYERS_H

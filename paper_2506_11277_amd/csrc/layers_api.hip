@@ -71,13 +71,17 @@ namespace {
 
 inline bool bad_type(int type) { return type != OZIMMU_BF16 && type != OZIMMU_F16 && type != OZIMMU_F32; }
 
+constexpr int kMostRows = (1 << 30) - 1;       // (numbers of steps and tiles are ints)
+
 // a matrix of `rows` rows of `cols` entries, `ld` apart
 inline bool bad_rows(int rows, int cols, const void *p, int ld, size_t size)
 {
-    if (rows < 0 || cols < 0 || ld < (cols > 1 ? cols : 1)) return true;
+    if (rows < 0 || cols < 0 || rows > kMostRows || cols > kMostRows || ld < (cols > 1 ? cols : 1)) return true;
     if (rows == 0 || cols == 0) return false;
     return p == nullptr || (uintptr_t)p % size != 0;
 }
+
+inline bool bad_sizes(int a, int b, int c) { return a < 0 || b < 0 || c < 0 || a > kMostRows || b > kMostRows || c > kMostRows; }
 
 inline size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
@@ -135,7 +139,7 @@ extern "C" {
 
 size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type)
 {
-    if (tokens < 0 || n_in < 0 || n_out < 0 || bad_type(type)) return 0;
+    if (bad_sizes(tokens, n_in, n_out) || bad_type(type)) return 0;
     return product_partial_bytes(n_out, tokens, plan_product(n_out, tokens, n_in, type, true));
 }
 
@@ -165,7 +169,7 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
 
 size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation)
 {
-    if (tokens < 0 || n_in < 0 || n_out < 0 || bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU) return 0;
+    if (bad_sizes(tokens, n_in, n_out) || bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU) return 0;
     return grad_workspace(tokens, n_in, n_out, type, activation).total;
 }
 
@@ -173,7 +177,7 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
                        int ldw, const void *pre, int ldpre, int activation, void *dx, int lddx, void *dw, int lddw, void *db,
                        void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU || tokens < 0 || n_in < 0 || n_out < 0) return OZIMMU_BAD_ARG;
+    if (bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU || bad_sizes(tokens, n_in, n_out)) return OZIMMU_BAD_ARG;
     const size_t size = element_bytes(type);
     if (bad_rows(tokens, n_out, dy, lddy, size) || (activation && bad_rows(tokens, n_out, pre, ldpre, size)) || (uintptr_t)db % size) return OZIMMU_BAD_ARG;
     if (dx && (bad_rows(tokens, n_in, dx, lddx, size) || bad_rows(n_out, n_in, w, ldw, size))) return OZIMMU_BAD_ARG;
@@ -243,6 +247,8 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
 }  // extern "C"
 
 namespace {
+constexpr int kMostFeatures = 1 << 24;         // (all chosen experts' steps are counted in an int)
+
 // parts of the workspace of ozimmu_moe
 struct MoeWorkspace {
     size_t parts, total;
@@ -264,8 +270,8 @@ extern "C" {
 
 size_t ozimmu_moe_workspace_bytes(int tokens, int width, int hidden, int experts, int top_k, int type)
 {
-    if (tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || hidden < 0 || experts < 1 || experts > OZIMMU_MOE_EXPERTS || top_k < 1 ||
-        top_k > experts || top_k > OZIMMU_MOE_TOP_K || bad_type(type))
+    if (tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || width > kMostFeatures || hidden < 0 || hidden > kMostFeatures || experts < 1 ||
+        experts > OZIMMU_MOE_EXPERTS || top_k < 1 || top_k > experts || top_k > OZIMMU_MOE_TOP_K || bad_type(type))
         return 0;
     return moe_workspace(tokens, width, hidden, experts, top_k, type).total;
 }
@@ -274,7 +280,7 @@ int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int ty
                const void *router, const void *w_in, const void *w_out, int32_t *chosen, float *gates, void *y, int ldy,
                void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (bad_type(type) || tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || width > 0x3fffffff || hidden < 0 || hidden > 0x3fffffff || experts < 1 ||
+    if (bad_type(type) || tokens < 0 || tokens > OZIMMU_MOE_TOKENS || width < 0 || width > kMostFeatures || hidden < 0 || hidden > kMostFeatures || experts < 1 ||
         experts > OZIMMU_MOE_EXPERTS || top_k < 1 || top_k > experts || top_k > OZIMMU_MOE_TOP_K)
         return OZIMMU_BAD_ARG;
     const size_t size = element_bytes(type);

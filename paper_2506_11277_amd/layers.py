@@ -4,6 +4,7 @@ Argument marshalling only, as in `ozimmu`: PyTorch provides device memory and th
 tensors with a token (or an output feature of a weight) per row, stride(1) == 1 and any row stride.
 """
 import ctypes
+from array import array
 from operator import attrgetter
 
 import torch
@@ -38,7 +39,7 @@ class _AdamWTensor(ctypes.Structure):
                 ("count", _c.c_int64), ("param_type", _int), ("grad_type", _int), ("state_type", _int), ("copy_type", _int)]
 
 
-_SIGNATURES["ozimmu_adamw"] = (_int, [_int, _c.POINTER(_AdamWTensor), _c.POINTER(_ptr)] + [_c.c_double] * 5 +
+_SIGNATURES["ozimmu_adamw"] = (_int, [_int, _c.POINTER(_AdamWTensor), _ptr] + [_c.c_double] * 5 +
                                [_c.c_longlong, _c.c_uint32, _ptr])
 
 _lib = None
@@ -86,10 +87,23 @@ def _vector(x, n, like, what):
     return x.data_ptr()
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = ozimmu._raw_stream
+
+
+def _stream(index, what):
+    """The current stream of the current device, on which the tensors have to be."""
+    if index != _get_device():
+        raise ValueError(f"{what}: tensors on cuda:{index}, which is not the current device")
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
 def _workspace(given, nbytes, device):
-    """(pointer, bytes) of the caller's workspace or of a new one, which has to live until the call has returned."""
+    """(tensor, pointer, bytes) of the caller's workspace or of a new one, which has to live until the call has returned."""
     if given is None:
         given = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    elif given.device != device or not given.is_contiguous():
+        raise ValueError(f"workspace: contiguous tensor on {device} expected")
     return given, (given.data_ptr() if given is not None else None), (given.numel() * given.element_size() if given is not None else 0)
 
 
@@ -118,7 +132,8 @@ def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=No
     keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear_workspace_bytes(tokens, n_in, n_out, kind) if workspace is None else 0, x.device)
     rc = L.ozimmu_linear(tokens, n_in, n_out, kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pbias,
                          None if residual is None else residual.data_ptr(), ldr, activation,
-                         None if pre is None else pre.data_ptr(), ldp, out.data_ptr(), ldy, ws, nbytes, ozimmu._stream())
+                         None if pre is None else pre.data_ptr(), ldp, out.data_ptr(), ldy, ws, nbytes,
+                         _stream(x.get_device(), "linear"))
     if rc != OK:
         raise OzimmuError(rc, "linear")
     return out
@@ -159,7 +174,7 @@ def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=
     rc = L.ozimmu_linear_grad(tokens, n_in, n_out, kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw,
                               pre.data_ptr() if activation != ACT_NONE else None, ldp, activation,
                               None if dx is None else dx.data_ptr(), lddx, None if dw is None else dw.data_ptr(), lddw, pdb,
-                              ws, nbytes, ozimmu._stream())
+                              ws, nbytes, _stream(dy.get_device(), "linear_grad"))
     if rc != OK:
         raise OzimmuError(rc, "linear_grad")
     return dx, dw, db
@@ -216,7 +231,6 @@ class AdamW:
             if copies is not None:
                 t.copy, t.copy_type = copies[i].data_ptr(), _TYPES[copies[i].dtype]
         self._grad_types = None
-        self._pointers = _ptr * n
 
     def step(self, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, seed=0):
         """One step with the gradients `grads`, contiguous tensors of the parameters' shapes; `step` counts from 1; `seed`
@@ -232,9 +246,9 @@ class AdamW:
                     raise ValueError("grads: bfloat16, float16 or float32 expected")
                 t.grad_type = _TYPES[kind]
             self._grad_types = kinds
-        pointers = self._pointers(*map(torch.Tensor.data_ptr, grads))
-        rc = (_lib or lib()).ozimmu_adamw(len(self._list), self._list, pointers, lr, beta1, beta2, eps, weight_decay, step,
-                                          seed & 0xffffffff, ozimmu._stream())
+        pointers = array("Q", map(torch.Tensor.data_ptr, grads))
+        rc = (_lib or lib()).ozimmu_adamw(len(self._list), self._list, pointers.buffer_info()[0], lr, beta1, beta2, eps, weight_decay, step,
+                                          seed & 0xffffffff, _stream(self._devices[0] if self._devices else _get_device(), "AdamW"))
         if rc != OK:
             raise OzimmuError(rc, "adamw")
 
@@ -279,7 +293,8 @@ def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, ga
     keep, ws, nbytes = _workspace(workspace, L.ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, kind)
                                   if workspace is None else 0, x.device)
     rc = L.ozimmu_moe(tokens, width, hidden, experts, top_k, kind, int(normalise), x.data_ptr(), ldx, router.data_ptr(), w_in.data_ptr(),
-                      w_out.data_ptr(), chosen.data_ptr(), gates.data_ptr(), out.data_ptr(), ldy, ws, nbytes, ozimmu._stream())
+                      w_out.data_ptr(), chosen.data_ptr(), gates.data_ptr(), out.data_ptr(), ldy, ws, nbytes,
+                      _stream(index, "moe"))
     if rc != OK:
         raise OzimmuError(rc, "moe")
     return out, chosen, gates

@@ -48,7 +48,7 @@ def linear(h, tokens=4, n_in=8, n_out=8, type=0, x=F, ldx=8, w=F, ldw=8, bias=No
     return h.ozimmu_linear(tokens, n_in, n_out, type, x, ldx, w, ldw, bias, residual, ldr, act, pre, ldpre, y, ldy, ws, nbytes, None)
 
 
-@pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(n_in=-1), dict(n_out=-1), dict(type=3), dict(type=-1), dict(act=5), dict(act=-1),
+@pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(n_in=-1), dict(n_out=-1), dict(tokens=1 << 30), dict(n_in=1 << 30, ldx=1 << 30, ldw=1 << 30), dict(type=3), dict(type=-1), dict(act=5), dict(act=-1),
                                    dict(x=None), dict(w=None), dict(y=None), dict(ldx=7), dict(ldw=7), dict(ldy=7), dict(x=ODD), dict(w=ODD),
                                    dict(y=ODD), dict(bias=ODD), dict(residual=F, ldr=7), dict(residual=ODD), dict(pre=F, ldpre=7), dict(pre=ODD),
                                    dict(type=2, x=ctypes.c_void_p((1 << 20) + 2))])
@@ -121,7 +121,7 @@ def moe(h, tokens=4, width=8, hidden=8, experts=4, top_k=2, type=0, x=F, ldx=8, 
 
 
 @pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(tokens=65), dict(width=-1), dict(hidden=-1), dict(experts=0), dict(experts=513), dict(top_k=0),
-                                   dict(top_k=5), dict(experts=64, top_k=17), dict(type=3), dict(x=None), dict(ldx=7), dict(router=None),
+                                   dict(top_k=5), dict(hidden=(1 << 24) + 1), dict(width=(1 << 24) + 1, ldx=1 << 25, ldy=1 << 25), dict(experts=64, top_k=17), dict(type=3), dict(x=None), dict(ldx=7), dict(router=None),
                                    dict(w_in=None), dict(w_out=None), dict(chosen=None), dict(gates=None), dict(y=None), dict(ldy=7), dict(x=ODD),
                                    dict(router=ODD), dict(w_in=ODD), dict(w_out=ODD), dict(y=ODD), dict(ws=None), dict(nbytes=8),
                                    dict(chosen=ctypes.c_void_p((1 << 20) + 2)), dict(gates=ctypes.c_void_p((1 << 20) + 2))])
