@@ -49,9 +49,10 @@ extern "C" {
  *   bias, residual and pre may be NULL.  pre receives x w^T + bias, which ozimmu_linear_grad takes.
  *   residual may be y itself (same pointer and ld).
  * Workspace: ozimmu_linear_workspace_bytes (partial sums where the contraction is divided among work-groups; it may be
- * 0, then NULL is accepted).
+ * 0, then NULL is accepted).  aligned = 1: every row of x and w starts on 16 bytes.  Otherwise the size has room for copies of them in
+ * such rows; with less, down to the size for aligned = 1, a slower way is taken where they are not.
  */
-size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type);
+size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type, int aligned);
 int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int ldx, const void *w, int ldw, const void *bias,
                   const void *residual, int ldr, int activation, void *pre, int ldpre, void *y, int ldy, void *workspace,
                   size_t workspace_bytes, void *stream);
@@ -62,8 +63,9 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
  *   dx = dz w   [tokens, n_in],   dw = dz^T x   [n_out, n_in],   db = the sum of dz over the tokens   [n_out]
  * (the gradient of the residual is dy itself).  dx, dw and db may each be NULL and are then not formed; pre may be NULL for
  * OZIMMU_ACT_NONE; x may be NULL without dw, w without dx.  act'(0) = 0 for OZIMMU_ACT_RELU.
+ * Workspace: as for ozimmu_linear, `aligned` of dy, x and w.
  */
-size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation);
+size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation, int aligned);
 int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const void *w,
                        int ldw, const void *pre, int ldpre, int activation, void *dx, int lddx, void *dw, int lddw, void *db,
                        void *workspace, size_t workspace_bytes, void *stream);

@@ -41,11 +41,7 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
             for (int i = 0; i < 8; ++i) sum[i] += d[i];
             if (a.dz) {
                 T *to = (T *)a.dz + (size_t)r * a.lddz + c;
-                if (n >= 8) store_row(to, d);               // (rows of dz are the workspace's, on 16 bytes)
-                else
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < n) to[i] = (T)d[i];
+                store_row(to, d);                           // (rows of dz are the workspace's, on 16 bytes, zeros behind them)
             }
         }
     if (!a.sums) return;

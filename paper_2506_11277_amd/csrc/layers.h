@@ -7,7 +7,7 @@ namespace oz {
 inline size_t element_bytes(int type) { return type == OZIMMU_F32 ? 4 : 2; }
 
 constexpr int kFewTokens = 16;             // columns few_tokens_kernel takes
-ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows);
+ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows, bool direct);
 int plan_pair(const Product &x, const ProductPlan &xp, const Product &w, const ProductPlan &wp, int type, bool bias);
 inline size_t product_partial_bytes(int np, int nq, const ProductPlan &p)
 {
@@ -19,6 +19,18 @@ hipError_t launch_product_f16(const Product &a, const ProductPlan &plan, float *
 hipError_t launch_pair_f16(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
 hipError_t launch_product_f32(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
 hipError_t launch_pair_f32(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
+
+// rows of `cols` entries, `ld` apart, to rows `ldto` apart (a multiple of 8), zeros behind them (pad.hip)
+struct PadCopy {
+    const void *from;
+    void *to;
+    long long rows;
+    int cols, ld, ldto;
+};
+struct PadCopies {
+    PadCopy c[2];                          // rows = 0: none
+};
+hipError_t launch_pad(const PadCopies &a, int type, hipStream_t st);
 
 // dz = dy * act'(pre) and the sums of its columns (grad.hip)
 // Tokens a work-group sums: 64, fewer where that leaves fewer than 1024 work-groups, at least two a wavefront, more where

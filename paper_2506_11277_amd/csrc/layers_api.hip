@@ -19,9 +19,10 @@ static double tiles_of(int t, int np, int nq)
     const int e = kShapes[t].edge;
     return (double)((np + e - 1) / e) * ((nq + e - 1) / e);
 }
-static double tile_us(int t, int steps, int type) { return kShapes[t].tile + steps * (type == OZIMMU_F32 ? kShapes[t].step32 : kShapes[t].step16); }
+// (operands that go to LDS through registers: a step takes two to three times as long in 16 bits, a fifth longer in 32)
+static double tile_us(int t, int steps, int type, bool direct = true) { return kShapes[t].tile + steps * (type == OZIMMU_F32 ? kShapes[t].step32 : kShapes[t].step16) * (direct ? 1 : type == OZIMMU_F32 ? 1.2 : 2.5); }
 
-ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows)
+ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows, bool direct)
 {
     const int ke = type == OZIMMU_F32 ? 32 : 64;
     const int all = (nk + ke - 1) / ke;
@@ -31,15 +32,15 @@ ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows)
         int s = 1;
         while (s < 16 && groups * s * 2 <= 256 && all / (2 * s) >= 16) s *= 2;
         const int steps = (all + s - 1) / s;
-        return ProductPlan{kTileFew, steps > 0 ? (all + steps - 1) / steps : 1, steps, false, 0};
+        return ProductPlan{kTileFew, steps > 0 ? (all + steps - 1) / steps : 1, steps, direct, 0};
     }
-    ProductPlan best{kTile64, 1, all, false, 1e300};
-    for (int t = type == OZIMMU_F32 ? kTile128 : kTile256; t <= kTile64; ++t)
+    ProductPlan best{kTile64, 1, all, direct, 1e300};
+    for (int t = type == OZIMMU_F32 || !direct ? kTile128 : kTile256; t <= kTile64; ++t)
         for (int s = 1; s <= 16 && (s == 1 || all / s >= 4); s *= 2) {
             const int steps = (all + s - 1) / s;
-            const double us = kShapes[t].launch + __builtin_ceil(tiles_of(t, np, nq) * s / 256) * tile_us(t, steps, type) +
+            const double us = kShapes[t].launch + __builtin_ceil(tiles_of(t, np, nq) * s / 256) * tile_us(t, steps, type, direct) +
                               (s > 1 ? 3.5 + (double)np * nq * s * 8 / 8e6 : 0);
-            if (us < best.us) best = ProductPlan{t, steps > 0 ? (all + steps - 1) / steps : 1, steps, false, us};
+            if (us < best.us) best = ProductPlan{t, steps > 0 ? (all + steps - 1) / steps : 1, steps, direct, us};
         }
     return best;
 }
@@ -93,14 +94,44 @@ inline bool direct_operand(const void *p, int ld, int along, size_t size)
     return on16(p, ld, size) && (size_t)along * size % 16 == 0 && 256ull * (unsigned)ld * size < (1ull << 32);
 }
 
-// completes a product and its plan: whether it can be copied directly, how its epilogue stores
-void prepare_product(Product &a, ProductPlan &plan, int type)
+inline int up8(int n) { return (n + 7) & ~7; }
+
+// bytes of the copies of a product's operands (P, Q) in aligned rows
+inline size_t copy_bytes(const Product &a, bool of_p, size_t size)
+{
+    const size_t rows = of_p ? (a.p_k_rows ? a.p_rows : a.p_nk) : (a.q_k_rows ? a.q_rows : a.q_nk);
+    const int along = of_p ? (a.p_k_rows ? a.p_nk : a.p_rows) : (a.q_k_rows ? a.q_nk : a.q_rows);
+    return padded(rows * up8(along) * size);
+}
+
+// The plan of a product, and the copies that it wants first (`space`: where they go; null: there is no room, or too little).
+ProductPlan route_product(Product &a, int type, bool k_rows, char *space, size_t space_bytes, PadCopies &copies)
 {
     const size_t size = element_bytes(type);
     Epilogue &e = a.e;
-    plan.direct = a.nk > 0 && direct_operand(a.P, a.ldp, a.p_k_rows ? a.nk : e.np, size) && direct_operand(a.Q, a.ldq, a.q_k_rows ? a.nk : e.nq, size);
     e.wide = on16(e.out, e.ldo, size) && (!e.bias || (uintptr_t)e.bias % 16 == 0) && (!e.residual || on16(e.residual, e.ldr, size)) &&
              (!e.pre || on16(e.pre, e.ldpre, size));
+    copies = PadCopies{};
+    const bool p_fits = direct_operand(a.P, a.ldp, a.p_k_rows ? a.p_nk : a.p_rows, size), q_fits = direct_operand(a.Q, a.ldq, a.q_k_rows ? a.q_nk : a.q_rows, size);
+    const ProductPlan direct = plan_product(e.np, e.nq, a.nk, type, k_rows, true);
+    if (direct.tile == kTileFew || (a.nk > 0 && p_fits && q_fits)) return direct;
+    const ProductPlan other = plan_product(e.np, e.nq, a.nk, type, k_rows, false);
+    // (a copy whose rows are too long for direct operands is of no use)
+    const int p_along = a.p_k_rows ? a.p_nk : a.p_rows, q_along = a.q_k_rows ? a.q_nk : a.q_rows;
+    if (256ull * up8(p_along) * size >= (1ull << 32) || 256ull * up8(q_along) * size >= (1ull << 32)) return other;
+    const size_t p_bytes = p_fits ? 0 : copy_bytes(a, true, size), q_bytes = q_fits ? 0 : copy_bytes(a, false, size);
+    // The copies: a launch, and their bytes read and written at 4 TB/s.  Rows off 16 bytes, without and with them: 4096^3 f16 321 and
+    // 128 us (aligned: 110), 1024 x 4096 x 1024 52 and 30, 1531 x 1000 x 776 17 either way, 200 x 1000 x 4000 15 and 19.
+    if (a.nk == 0 || space == nullptr || space_bytes < p_bytes + q_bytes || direct.us + 6 + 2 * (p_bytes + q_bytes) / 4e6 >= other.us) return other;
+    auto copy = [&](PadCopy &c, const void *&x, int &ld, bool rows_along_k, int &rows, int &nk, char *to) {
+        int &along = rows_along_k ? nk : rows;
+        c = PadCopy{x, to, rows_along_k ? rows : nk, along, ld, up8(along)};
+        x = to;
+        ld = along = c.ldto;
+    };
+    if (!p_fits) copy(copies.c[0], a.P, a.ldp, a.p_k_rows, a.p_rows, a.p_nk, space);
+    if (!q_fits) copy(copies.c[1], a.Q, a.ldq, a.q_k_rows, a.q_rows, a.q_nk, space + p_bytes);
+    return direct;
 }
 
 hipError_t launch_product(const Product &a, const ProductPlan &plan, int type, float *partial, hipStream_t st)
@@ -111,20 +142,49 @@ hipError_t launch_product(const Product &a, const ProductPlan &plan, int type, f
                                 : launch_product_f32(a, plan, partial, st);
 }
 
+// partial sums of a product whichever way its operands go
+inline size_t either_partial_bytes(int np, int nq, int nk, int type, bool k_rows)
+{
+    const size_t a = product_partial_bytes(np, nq, plan_product(np, nq, nk, type, k_rows, true)), b = product_partial_bytes(np, nq, plan_product(np, nq, nk, type, k_rows, false));
+    return padded(a > b ? a : b);
+}
+
+// parts of the workspace of ozimmu_linear: partial sums, copies of x and w (where they are wanted)
+struct LinearWorkspace {
+    size_t copies, copies_bytes, total;
+};
+LinearWorkspace linear_workspace(int tokens, int n_in, int n_out, int type, bool aligned)
+{
+    LinearWorkspace w{};
+    const size_t size = element_bytes(type);
+    w.copies = either_partial_bytes(n_out, tokens, n_in, type, true);
+    const ProductPlan direct = plan_product(n_out, tokens, n_in, type, true, true), other = plan_product(n_out, tokens, n_in, type, true, false);
+    if ((!aligned || n_in * size % 16) && direct.tile != kTileFew && direct.us + 3 < other.us)
+        w.copies_bytes = padded((size_t)tokens * up8(n_in) * size) + padded((size_t)n_out * up8(n_in) * size);
+    w.total = w.copies + w.copies_bytes;
+    return w;
+}
+
 // parts of the workspace of ozimmu_linear_grad
 struct GradWorkspace {
-    size_t dz, sums, partial, total;
+    size_t dz, sums, partial, copies_x, copies_w, total;
+    bool has_dz, has_copies;
     int lddz;
 };
-GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int activation)
+GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int activation, bool aligned)
 {
     GradWorkspace w{};
-    w.lddz = (n_out + 7) & ~7;
-    w.sums = activation == OZIMMU_ACT_NONE ? 0 : padded((size_t)tokens * w.lddz * element_bytes(type));
+    const size_t size = element_bytes(type);
+    aligned = aligned && n_in * size % 16 == 0 && n_out * size % 16 == 0;
+    w.lddz = up8(n_out);
+    w.has_dz = activation != OZIMMU_ACT_NONE || !aligned;
+    w.has_copies = !aligned;
+    w.sums = w.has_dz ? padded((size_t)tokens * w.lddz * size) : 0;
     w.partial = w.sums + padded((size_t)((tokens + grad_rows(tokens, n_out) - 1) / grad_rows(tokens, n_out)) * n_out * 4);
-    const size_t dx = product_partial_bytes(n_in, tokens, plan_product(n_in, tokens, n_out, type, false));
-    const size_t dw = product_partial_bytes(n_in, n_out, plan_product(n_in, n_out, tokens, type, false));
-    w.total = w.partial + padded(dx > dw ? dx : dw);
+    const size_t dx = either_partial_bytes(n_in, tokens, n_out, type, false), dw = either_partial_bytes(n_in, n_out, tokens, type, false);
+    w.copies_x = w.partial + (dx > dw ? dx : dw);
+    w.copies_w = w.copies_x + (w.has_copies ? padded((size_t)tokens * up8(n_in) * size) : 0);
+    w.total = w.copies_w + (w.has_copies ? padded((size_t)n_out * up8(n_in) * size) : 0);
     return w;
 }
 
@@ -137,10 +197,10 @@ inline bool bad_workspace(const void *p, size_t have, size_t want)
 
 extern "C" {
 
-size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type)
+size_t ozimmu_linear_workspace_bytes(int tokens, int n_in, int n_out, int type, int aligned)
 {
     if (bad_sizes(tokens, n_in, n_out) || bad_type(type)) return 0;
-    return product_partial_bytes(n_out, tokens, plan_product(n_out, tokens, n_in, type, true));
+    return linear_workspace(tokens, n_in, n_out, type, aligned != 0).total;
 }
 
 int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int ldx, const void *w, int ldw, const void *bias,
@@ -152,25 +212,32 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     if (bad_rows(tokens, n_in, x, ldx, size) || bad_rows(n_out, n_in, w, ldw, size) || bad_rows(tokens, n_out, y, ldy, size)) return OZIMMU_BAD_ARG;
     if ((uintptr_t)bias % size || (residual && bad_rows(tokens, n_out, residual, ldr, size)) || (pre && bad_rows(tokens, n_out, pre, ldpre, size)))
         return OZIMMU_BAD_ARG;
-    ProductPlan plan = plan_product(n_out, tokens, n_in, type, true);
-    if (bad_workspace(workspace, workspace_bytes, product_partial_bytes(n_out, tokens, plan))) return OZIMMU_BAD_ARG;
+    if (bad_workspace(workspace, workspace_bytes, linear_workspace(tokens, n_in, n_out, type, true).total)) return OZIMMU_BAD_ARG;
+    if (tokens == 0 || n_out == 0) return OZIMMU_OK;
+    const LinearWorkspace ws = linear_workspace(tokens, n_in, n_out, type, false);
+    const bool room = ws.copies_bytes > 0 && workspace_bytes >= ws.total;
     Product a{};
     a.P = w;
     a.ldp = ldw;
     a.p_k_rows = true;
+    a.p_rows = n_out;
     a.Q = x;
     a.ldq = ldx;
     a.q_k_rows = true;
-    a.nk = n_in;
+    a.q_rows = tokens;
+    a.nk = a.p_nk = a.q_nk = n_in;
     a.e = Epilogue{bias, residual, pre, y, ldr, ldpre, ldy, n_out, tokens, activation, 0};
-    prepare_product(a, plan, type);
-    return launch_product(a, plan, type, (float *)workspace, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+    PadCopies copies;
+    const ProductPlan plan = route_product(a, type, true, room ? (char *)workspace + ws.copies : nullptr, ws.copies_bytes, copies);
+    const hipStream_t st = (hipStream_t)stream;
+    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    return launch_product(a, plan, type, (float *)workspace, st) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
 }
 
-size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation)
+size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation, int aligned)
 {
     if (bad_sizes(tokens, n_in, n_out) || bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU) return 0;
-    return grad_workspace(tokens, n_in, n_out, type, activation).total;
+    return grad_workspace(tokens, n_in, n_out, type, activation, aligned != 0).total;
 }
 
 int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const void *w,
@@ -182,55 +249,76 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
     if (bad_rows(tokens, n_out, dy, lddy, size) || (activation && bad_rows(tokens, n_out, pre, ldpre, size)) || (uintptr_t)db % size) return OZIMMU_BAD_ARG;
     if (dx && (bad_rows(tokens, n_in, dx, lddx, size) || bad_rows(n_out, n_in, w, ldw, size))) return OZIMMU_BAD_ARG;
     if (dw && (bad_rows(n_out, n_in, dw, lddw, size) || bad_rows(tokens, n_in, x, ldx, size))) return OZIMMU_BAD_ARG;
-    const GradWorkspace ws = grad_workspace(tokens, n_in, n_out, type, activation);
+    GradWorkspace ws = grad_workspace(tokens, n_in, n_out, type, activation, true);
     if (bad_workspace(workspace, workspace_bytes, ws.total)) return OZIMMU_BAD_ARG;
     if (n_out == 0 && !dx) return OZIMMU_OK;
     const hipStream_t st = (hipStream_t)stream;
     char *const base = (char *)workspace;
+    // (dy of no activation is read as it is where it can be copied directly, or there is no room for dz)
+    const bool dy_fits = direct_operand(dy, lddy, n_out, size);
+    if (!dy_fits || (dx && !direct_operand(w, ldw, n_in, size)) || (dw && !direct_operand(x, ldx, n_in, size))) {
+        const GradWorkspace wider = grad_workspace(tokens, n_in, n_out, type, activation, false);
+        if (workspace_bytes >= wider.total) ws = wider;
+    }
 
+    const bool own_dz = n_out > 0 && (dx || dw) && (activation || (ws.has_dz && !dy_fits));
     const void *dz = dy;
-    int lddz = lddy;
-    if (n_out > 0 && (db || (activation && (dx || dw)))) {
+    int lddz = lddy, dz_cols = n_out;
+    const int rows = grad_rows(tokens, n_out);
+    if (n_out > 0 && (db || own_dz)) {
         GradInput g{};
         g.dy = dy;
         g.pre = activation ? pre : nullptr;
-        g.dz = activation && (dx || dw) ? base + ws.dz : nullptr;
+        g.dz = own_dz ? base + ws.dz : nullptr;
         g.sums = db ? (float *)(base + ws.sums) : nullptr;
         g.lddy = lddy;
         g.ldpre = ldpre;
         g.lddz = ws.lddz;
         g.tokens = tokens;
         g.n_out = n_out;
-        g.rows = grad_rows(tokens, n_out);
+        g.rows = rows;
         g.act = activation;
         g.wide = on16(dy, lddy, size) && (!activation || on16(pre, ldpre, size));
         if (launch_grad_input(g, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     }
-    if (activation) {
+    if (own_dz) {
         dz = base + ws.dz;
-        lddz = ws.lddz;
+        lddz = dz_cols = ws.lddz;
     }
-    const int rows = grad_rows(tokens, n_out);
     const BiasGrad bias{(const float *)(base + ws.sums), db, (tokens + rows - 1) / rows, n_out};
     float *partial = (float *)(base + ws.partial);
     Product x_grad{}, w_grad{};
-    ProductPlan x_plan = plan_product(n_in, tokens, n_out, type, false), w_plan = plan_product(n_in, n_out, tokens, type, false);
     x_grad.P = w;
     x_grad.ldp = ldw;
+    x_grad.p_rows = n_in;
+    x_grad.p_nk = n_out;
     x_grad.Q = dz;
     x_grad.ldq = lddz;
     x_grad.q_k_rows = true;
+    x_grad.q_rows = tokens;
+    x_grad.q_nk = dz_cols;
     x_grad.nk = n_out;
     x_grad.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, 0};
     w_grad.P = x;
     w_grad.ldp = ldx;
+    w_grad.p_rows = n_in;
+    w_grad.p_nk = tokens;
     w_grad.Q = dz;
     w_grad.ldq = lddz;
+    w_grad.q_rows = dz_cols;
+    w_grad.q_nk = tokens;
     w_grad.nk = tokens;
     w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, 0};
-    prepare_product(x_grad, x_plan, type);
-    prepare_product(w_grad, w_plan, type);
-    const bool both = dx && dw && n_in > 0 && n_out > 0 && tokens > 0 && x_plan.direct && w_plan.direct;
+    PadCopies x_copies{}, w_copies{}, copies{};
+    ProductPlan x_plan{}, w_plan{};
+    const bool form_dx = dx && tokens > 0 && n_in > 0, form_dw = dw && n_out > 0 && n_in > 0;
+    // (of each product P alone can want a copy here: dz is the workspace's, or dy where there is no room for either)
+    if (form_dx) x_plan = route_product(x_grad, type, false, ws.has_copies ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies);
+    if (form_dw) w_plan = route_product(w_grad, type, false, ws.has_copies ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
+    copies.c[0] = x_copies.c[0];
+    copies.c[1] = w_copies.c[0];
+    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    const bool both = form_dx && form_dw && n_out > 0 && tokens > 0 && x_plan.direct && w_plan.direct;
     const int pair = both ? plan_pair(x_grad, x_plan, w_grad, w_plan, type, db != nullptr) : -1;
     if (pair >= 0) {
         const hipError_t e = type == OZIMMU_BF16  ? launch_pair_bf16(x_grad, w_grad, bias, pair, st)
@@ -239,8 +327,8 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
         return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
     }
     if (launch_bias_grad(bias, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    if (dx && launch_product(x_grad, x_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    if (dw && launch_product(w_grad, w_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (form_dx && launch_product(x_grad, x_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (form_dw && launch_product(w_grad, w_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     return OZIMMU_OK;
 }
 

@@ -239,6 +239,8 @@ struct Product {
     int ldp, ldq;
     bool p_k_rows, q_k_rows;
     int nk;
+    // what the operands hold: rows (p or q) and k; more than np, nq and nk where they are padded with zeros
+    int p_rows, q_rows, p_nk, q_nk;
     Epilogue e;
 };
 

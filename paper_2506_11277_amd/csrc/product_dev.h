@@ -15,7 +15,8 @@
 //
 // DIRECT: the copies go from memory to LDS without registers, which wants 16-byte alignment of every row; what lies
 // behind k is read from a chunk of zeros.  Otherwise 16 bytes a lane are loaded at any alignment, and written to LDS behind the
-// products.  Rows behind the operand's last are read as the last and not stored.
+// products: twice the time of a step, so larger operands are copied to aligned rows first (pad.hip).  Rows behind the
+// operand's last are read as the last and not stored.
 #pragma once
 #include "few_dev.h"
 
@@ -98,10 +99,6 @@ struct Operand {
     unsigned off[DIRECT ? N : 1];                                       // bytes behind the step's base
     v4u reg[2][DIRECT ? 1 : N];                                         // chunks on their way to LDS, of two steps
 
-    static __device__ __forceinline__ int place(int c)                  // LDS row's chunk -> chunk of the row in memory
-    {
-        return c;
-    }
     // swizzle of 16-byte chunks in LDS row r
     static __device__ __forceinline__ int twist(int r)
     {
@@ -361,8 +358,8 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
 
     Operand<T, PK, BP, S::kWaves, DIRECT> P;
     Operand<T, QK, BQ, S::kWaves, DIRECT> Q;
-    P.init(a.P, a.ldp, a.e.np, tp * BP, a.nk, wave, lane);
-    Q.init(a.Q, a.ldq, a.e.nq, tq * BQ, a.nk, wave, lane);
+    P.init(a.P, a.ldp, a.p_rows, tp * BP, a.p_nk, wave, lane);
+    Q.init(a.Q, a.ldq, a.q_rows, tq * BQ, a.q_nk, wave, lane);
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
 
     v4f acc[FP][FQ];

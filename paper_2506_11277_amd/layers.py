@@ -25,9 +25,9 @@ _TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
 _c = ctypes
 _int, _ptr, _size = _c.c_int, _c.c_void_p, _c.c_size_t
 _SIGNATURES = {
-    "ozimmu_linear_workspace_bytes": (_size, [_int] * 4),
+    "ozimmu_linear_workspace_bytes": (_size, [_int] * 5),
     "ozimmu_linear": (_int, [_int] * 4 + [_ptr, _int, _ptr, _int, _ptr, _ptr, _int, _int, _ptr, _int, _ptr, _int, _ptr, _size, _ptr]),
-    "ozimmu_linear_grad_workspace_bytes": (_size, [_int] * 5),
+    "ozimmu_linear_grad_workspace_bytes": (_size, [_int] * 6),
     "ozimmu_linear_grad": (_int, [_int] * 4 + [_ptr, _int] * 4 + [_int] + [_ptr, _int] * 2 + [_ptr, _ptr, _size, _ptr]),
     "ozimmu_moe_workspace_bytes": (_size, [_int] * 6),
     "ozimmu_moe": (_int, [_int] * 7 + [_ptr, _int] + [_ptr] * 6 + [_int, _ptr, _size, _ptr]),
@@ -107,8 +107,17 @@ def _workspace(given, nbytes, device):
     return given, (given.data_ptr() if given is not None else None), (given.numel() * given.element_size() if given is not None else 0)
 
 
-def linear_workspace_bytes(tokens, n_in, n_out, dtype):
-    return lib().ozimmu_linear_workspace_bytes(tokens, n_in, n_out, _TYPES[dtype])
+def _aligned(x, ldx, *rest):
+    """Whether every row of the matrices (tensor, row stride, ...) starts on 16 bytes."""
+    bits, size = x.data_ptr() | ldx * x.element_size(), x.element_size()
+    for w, ld in zip(rest[::2], rest[1::2]):
+        bits |= w.data_ptr() | ld * size
+    return 0 if bits & 15 else 1
+
+
+def linear_workspace_bytes(tokens, n_in, n_out, dtype, aligned=True):
+    """Bytes of workspace for linear; aligned: every row of x and w starts on 16 bytes (with less a slower way is taken)."""
+    return lib().ozimmu_linear_workspace_bytes(tokens, n_in, n_out, _TYPES[dtype], int(aligned))
 
 
 def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=None, workspace=None):
@@ -129,7 +138,8 @@ def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=No
     ldr = 0 if residual is None else _ld(residual, tokens, n_out, x, "residual")
     ldp = 0 if pre is None else _ld(pre, tokens, n_out, x, "pre")
     L = _lib or lib()
-    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear_workspace_bytes(tokens, n_in, n_out, kind) if workspace is None else 0, x.device)
+    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear_workspace_bytes(tokens, n_in, n_out, kind, _aligned(x, ldx, w, ldw))
+                                  if workspace is None else 0, x.device)
     rc = L.ozimmu_linear(tokens, n_in, n_out, kind, x.data_ptr(), ldx, w.data_ptr(), ldw, pbias,
                          None if residual is None else residual.data_ptr(), ldr, activation,
                          None if pre is None else pre.data_ptr(), ldp, out.data_ptr(), ldy, ws, nbytes,
@@ -139,8 +149,9 @@ def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=No
     return out
 
 
-def linear_grad_workspace_bytes(tokens, n_in, n_out, dtype, activation=ACT_NONE):
-    return lib().ozimmu_linear_grad_workspace_bytes(tokens, n_in, n_out, _TYPES[dtype], activation)
+def linear_grad_workspace_bytes(tokens, n_in, n_out, dtype, activation=ACT_NONE, aligned=True):
+    """Bytes of workspace for linear_grad; aligned: every row of dy, x and w starts on 16 bytes."""
+    return lib().ozimmu_linear_grad_workspace_bytes(tokens, n_in, n_out, _TYPES[dtype], activation, int(aligned))
 
 
 def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=None, db=None, want=("dx", "dw"), workspace=None):
@@ -169,7 +180,8 @@ def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=
     lddw = 0 if dw is None else _ld(dw, n_out, n_in, dy, "dw")
     pdb = None if db is None else _vector(db, n_out, dy, "db")
     L = _lib or lib()
-    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear_grad_workspace_bytes(tokens, n_in, n_out, kind, activation)
+    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear_grad_workspace_bytes(tokens, n_in, n_out, kind, activation,
+                                                                       _aligned(dy, lddy, x, ldx, w, ldw))
                                   if workspace is None else 0, dy.device)
     rc = L.ozimmu_linear_grad(tokens, n_in, n_out, kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw,
                               pre.data_ptr() if activation != ACT_NONE else None, ldp, activation,

@@ -121,6 +121,25 @@ def test_linear_grad_against_differences(name):
         assert abs(difference - slope_along) <= 1e-3 + 1e-5 * float((g.double() * d).abs().sum())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape,extra", [((700, 1001, 777), 0), ((700, 1000, 776), 3), ((1100, 520, 1032), 1), ((130, 2048, 4099), 0)])
+def test_unaligned_operands_with_and_without_room_for_copies(shape, extra, kind):
+    tokens, n_in, n_out = shape
+    x, w, bias, residual, dy = operands(tokens, n_in, n_out, kind, extra, 33)
+    for name in ("none", "gelu"):
+        a, z = layers.ACTIVATIONS[name], None if name == "none" else residual
+        results = []
+        for aligned in (False, True):       # as if they were aligned: room for partial sums only, where the sizes themselves are
+            y = layers.linear(x, w, bias, residual, a, workspace=torch.empty(max(256, layers.linear_workspace_bytes(*shape, x.dtype, aligned)),
+                                                                             dtype=torch.uint8, device="cuda"))
+            check_linear(x, w, bias, residual, name, y, None)
+            nbytes = layers.linear_grad_workspace_bytes(*shape, x.dtype, a, aligned)
+            results.append(layers.linear_grad(dy, x, w, z, a, workspace=torch.full((max(256, nbytes),), 255, dtype=torch.uint8, device="cuda")))
+        for got, other in zip(*results):    # the same products in another order of sums, of dz rounded the same
+            scale = other.double().abs().max()
+            assert bool(((got.double() - other.double()).abs() <= (2 * ROUND[x.dtype] + 64 * sum_bound(max(shape))) * scale).all())
+
+
 def test_linear_grad_forms_what_is_asked_for():
     x, w, bias, dy, z = operands(130, 70, 90, "bf16", 0, 6)
     all_ = layers.linear_grad(dy, x, w, z, layers.ACT_GELU)

@@ -58,16 +58,20 @@ def test_linear_refuses(handle, wrong):
 
 def test_linear_workspace(handle):
     need = handle.ozimmu_linear_workspace_bytes
-    assert need(-1, 1, 1, 0) == 0 and need(1, 1, 1, 9) == 0 and need(0, 0, 0, 0) == 0
+    assert need(-1, 1, 1, 0, 1) == 0 and need(1, 1, 1, 9, 1) == 0 and need(0, 0, 0, 0, 1) == 0 and need(1 << 30, 1, 1, 0, 1) == 0
     sizes = [(t, i, o) for t in (1, 64, 65, 300, 1531, 8192) for i in (1, 1001, 8192) for o in (1, 777, 2048, 8192)]
-    some = [s for s in sizes if need(*s, 0) > 0]
+    some = [s for s in sizes if need(*s, 0, 1) > 0 and s[1] % 8 == 0]
     assert some
     t, i, o = some[0]
     assert linear(handle, t, i, o, ldx=i, ldw=i, ldy=o, ws=None) == BAD
-    assert linear(handle, t, i, o, ldx=i, ldw=i, ldy=o, ws=F, nbytes=need(t, i, o, 0) - 1) == BAD
+    assert linear(handle, t, i, o, ldx=i, ldw=i, ldy=o, ws=F, nbytes=need(t, i, o, 0, 1) - 1) == BAD
     assert linear(handle, t, i, o, ldx=i, ldw=i, ldy=o, ws=ctypes.c_void_p((1 << 20) + 128), nbytes=1 << 40) == BAD
     for s in sizes:
-        assert need(*s, 0) <= 16 * 4 * s[0] * (s[2] + 7) + 256
+        aligned, other = need(*s, 0, 1), need(*s, 0, 0)
+        copies = 2 * (s[0] + s[2]) * (s[1] + 7) + 1024
+        assert other >= aligned and aligned <= 16 * 4 * s[0] * (s[2] + 7) + 512 + copies and other <= aligned + copies
+    assert need(4096, 4096, 4096, 0, 0) >= need(4096, 4096, 4096, 0, 1) + 2 * 2 * 4096 * 4096       # room for copies of x and w
+    assert need(1, 4096, 4096, 0, 0) == need(1, 4096, 4096, 0, 1)                                   # which few tokens do not want
 
 
 def grad(h, tokens=4, n_in=8, n_out=8, type=0, dy=F, lddy=8, x=F, ldx=8, w=F, ldw=8, pre=F, ldpre=8, act=2, dx=F, lddx=8, dw=F, lddw=8,
@@ -85,9 +89,10 @@ def test_linear_grad_refuses(handle, wrong):
 
 def test_linear_grad_workspace(handle):
     need = handle.ozimmu_linear_grad_workspace_bytes
-    assert need(-1, 1, 1, 0, 0) == 0 and need(1, 1, 1, 0, 5) == 0 and need(1, 1, 1, 3, 0) == 0
-    assert need(1000, 512, 700, 0, 2) >= need(1000, 512, 700, 0, 0) + 1000 * 704 * 2       # dz
-    assert need(1000, 512, 700, 2, 2) >= 1000 * 704 * 4
+    assert need(-1, 1, 1, 0, 0, 1) == 0 and need(1, 1, 1, 0, 5, 1) == 0 and need(1, 1, 1, 3, 0, 1) == 0
+    assert need(1000, 512, 704, 0, 2, 1) >= need(1000, 512, 704, 0, 0, 1) + 1000 * 704 * 2       # dz
+    assert need(1000, 512, 700, 2, 2, 1) >= 1000 * 704 * 4
+    assert need(1000, 512, 704, 0, 2, 0) >= need(1000, 512, 704, 0, 2, 1) + (1000 + 704) * 512 * 2  # copies of x and w
 
 
 def test_adamw_refuses(handle):
