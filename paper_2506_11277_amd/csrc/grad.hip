@@ -2,7 +2,8 @@
 //
 // Bound by memory: dy and pre are read once, dz is written once; the column sums ride along in registers.  A work-group
 // owns 512 columns of grad_rows() tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
-// work-group of tokens, in a second kernel, always in the same order.
+// work-group of tokens, with the products of dx and dw or in a kernel of their own, always in the same order.
+// 8192 x 8192 bf16 with gelu, 403 MB: 74 us, 5.4 TB/s (the library's erf: 110).
 #include "layers.h"
 
 namespace oz {

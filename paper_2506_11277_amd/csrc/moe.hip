@@ -8,6 +8,9 @@
 //                      sum, so nothing is scattered and no atomics change an order; in two to eight parts, which
 //                      moe_join_kernel adds, where the features are too few for all compute units
 //
+// 8 tokens, 64 experts of 2048 x 1024 bf16, 8 chosen (42 different ones): routing 9 us, hidden layer 80 (352 MB at 4.4 TB/s), output 36 to
+// 40 (176 MB at 4.4 to 4.9) and 5.
+//
 // Which experts are chosen is known on the device only: the second launch has a work-group for each of the min(experts,
 // tokens * top_k) experts that can be, which finds its expert in a bit map of the chosen ones and leaves if there is none.
 #include "layers.h"
@@ -84,8 +87,20 @@ __device__ __forceinline__ void route_token(const MoeArgs &a, int t, RouteSpace 
                 for (int c = 0; c < E; ++c) s[i] = __builtin_fmaf((float)xv[c], (float)rv[c], s[i]);
             }
         };
-#pragma unroll 4
-        for (int k = lane * E; k < whole; k += 64 * E) {
+        int k = lane * E;
+        for (; k + 3 * 64 * E < whole; k += 4 * 64 * E) {
+            v4u xc[4], rc[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                __builtin_memcpy(&xc[u], x + k + u * 64 * E, 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) __builtin_memcpy(&rc[u][i], r[i] + k + u * 64 * E, 16);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) products(xc[u], rc[u]);
+        }
+        for (; k < whole; k += 64 * E) {
             v4u xc, rc[4];
             __builtin_memcpy(&xc, x + k, 16);
 #pragma unroll

@@ -1,8 +1,13 @@
 // The tiled matrix product of the feed-forward operators: D[q][p] = act(sum_k P Q + bias) + residual.
 //
 // A work-group owns a tile of BP x BQ entries and walks k in steps of 128 bytes of an operand's row (64 entries of 16
-// bits, 32 of 32 bits).  Both operands of a step stand in LDS as BP (BQ) * 128 bytes, two stages of them: the copies of
-// step t + 1 are issued behind the barrier that opens step t and have all of its products to arrive, one barrier a step.
+// bits, 32 of 32 bits).  Both operands of a step stand in LDS as BP (BQ) * 128 bytes, in a ring of two stages (256 x 256: all
+// that fits) or four: the copies of a step are issued one to three steps before its products, one barrier a step.
+//
+// What bounds it: 256 x 256 in 16 bits the matrix instructions at the clock that the board's power leaves them, with LDS (128 KB read
+// and 64 written a step of 2048 cycles of matrix instructions) close behind: 8192^3 bf16 1.5 PFLOP/s, 4096^3 1.25, 8192 x 4096 x 8192
+// with a gelu and `pre` 1.2.  128 x 128 and 64 x 64 LDS: 96 and 48 KB a step of 512 and 128 cycles (2048^3 780 TFLOP/s,
+// 1024^3 of either 130).  32 bits: the matrix instructions (2048^3 127 TFLOP/s, 4096^3 139).
 //
 // k_rows: the entries of an operand's row are contiguous along k (activations and weights of a forward pass).  LDS row r
 //   holds its 8 chunks of 16 bytes at position chunk ^ (r / 2 % 8): the 16 rows that a matrix instruction's operand takes
@@ -530,7 +535,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
 }
 
 // dx, dw and the bias gradient of a layer in one launch: each alone leaves compute units without work in its last round, or
-// in its only one, and costs a launch (500 x 512 x 384 f32: 35 us in three launches, 22 in one; 1777 x 1024 x 2304 f16: 65 and 50).
+// in its only one, and costs a launch (500 x 512 x 384 f32: the call 35 us in three launches, 19 in one; 1777 x 1024 x 2304 f16: 63
+// and 33).
 template <class T, int BP, int BQ>
 __global__ __launch_bounds__(256) void product_pair_kernel(Product dx, Product dw, BiasGrad db, int blocks_dx, int blocks_dw)
 {
@@ -561,7 +567,8 @@ __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, const flo
     const size_t plane = (size_t)e.nq * groups * 8;
     const float *from = partial + (size_t)q * groups * 8 + p;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int s = 0; s < splits; ++s) {
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) {                  // (their loads together: up to 16 parts wait once or twice)
         const v4f a = *(const v4f *)(from + s * plane), b = *(const v4f *)(from + s * plane + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
