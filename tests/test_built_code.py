@@ -65,3 +65,29 @@ def test_written_products_are_left_where_they_are(kernels, kind, tile):
             elif behind:
                 assert not line.startswith(("v_accvgpr_read", "v_accvgpr_mov", "scratch_store")), line
         assert seen
+
+
+def _registers(operands):
+    out = set()
+    for kind, a, b in re.findall(r"\b([va])\[(\d+):(\d+)\]", operands):
+        out |= {kind + str(i) for i in range(int(a), int(b) + 1)}
+    return out | {kind + a for kind, a in re.findall(r"\b([va])(\d+)\b", operands)}
+
+
+@pytest.mark.parametrize("tile", [256, 128, 64])
+@pytest.mark.parametrize("kind", ["DF16b", "DF16_", "f"])
+def test_written_products_wait_for_their_operands(kernels, kind, tile):
+    # ... nor does it know that a matrix instruction wants two wait states behind the vector instruction that writes an operand
+    name = r"product_(kernelI%sLb[01]ELb[01]ELi%dELi%dE.*Lb1E|pair_kernelI%sLi%dE)" % (kind, tile, tile, kind, tile)
+    for body in [b for n, b in kernels.items() if re.search(name, n)]:
+        written = []                                    # registers written by the last two instructions, if by vector ones
+        for line in body.splitlines():
+            if not re.match(r"\s+[a-z]+_", line):
+                continue
+            op, _, operands = line.split("//")[0].strip().partition(" ")
+            if op.startswith("v_mfma"):
+                assert not any(w & _registers(operands) for w in written), line
+            vector = op.startswith("v_") and not op.startswith("v_mfma")
+            written = written[-1:] + [_registers(operands.split(",")[0]) if vector else set()]
+            if op == "s_nop" and int(operands.strip(), 0) >= 1:
+                written = []
