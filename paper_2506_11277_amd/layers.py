@@ -253,9 +253,9 @@ class AdamW:
                 list(map(torch.Tensor.get_device, grads)) != self._devices):
             raise ValueError("grads: contiguous tensors of the parameters' shapes and device expected")
         if kinds != self._grad_types:
+            if not all(kind in _TYPES for kind in kinds):           # (before any of them is noted)
+                raise ValueError("grads: bfloat16, float16 or float32 expected")
             for t, kind in zip(self._list, kinds):
-                if kind not in _TYPES:
-                    raise ValueError("grads: bfloat16, float16 or float32 expected")
                 t.grad_type = _TYPES[kind]
             self._grad_types = kinds
         pointers = array("Q", map(torch.Tensor.data_ptr, grads))

@@ -1,0 +1,45 @@
+"""The layers' binding on the CPU, with a stand-in for the library that notes what it is called with."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2506_11277_amd import layers
+
+
+class Library:
+    """Notes the types that each AdamW step sends for its gradients."""
+
+    def __init__(self):
+        self.grad_types = []
+
+    def ozimmu_adamw(self, n, tensors, *rest):
+        self.grad_types.append([t.grad_type for t in tensors])
+        return layers.OK
+
+
+@pytest.fixture
+def library(monkeypatch):
+    stand_in = Library()
+    monkeypatch.setattr(layers, "_lib", stand_in)
+    monkeypatch.setattr(layers, "_type_of", lambda x, what: layers._TYPES[x.dtype])
+    monkeypatch.setattr(layers, "_stream", lambda index, what: None)
+    return stand_in
+
+
+def plan_of(sizes):
+    params = [torch.ones(n) for n in sizes]
+    m, v, _, _ = layers.adamw_state(params)
+    return layers.AdamW(params, m, v)
+
+
+@pytest.mark.parametrize("first", [torch.bfloat16, torch.float32])
+def test_a_refused_step_leaves_the_plan_as_it_was(library, first):
+    plan = plan_of([5, 6])
+    plan.step([torch.ones(n, dtype=first) for n in (5, 6)], 1)
+    other = torch.float32 if first is torch.bfloat16 else torch.bfloat16
+    with pytest.raises(ValueError):
+        plan.step([torch.ones(5, dtype=other), torch.ones(6, dtype=torch.float64)], 2)
+    plan.step([torch.ones(n, dtype=first) for n in (5, 6)], 2)
+    assert library.grad_types == [[layers._TYPES[first]] * 2] * 2
+    plan.step([torch.ones(5, dtype=other), torch.ones(6, dtype=first)], 3)
+    assert library.grad_types[-1] == [layers._TYPES[other], layers._TYPES[first]]
