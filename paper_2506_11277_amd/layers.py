@@ -220,7 +220,7 @@ class AdamW:
         given = [params, m, v] + [x for x in (m_scale, v_scale, copies) if x is not None]
         if any(len(x) != n for x in given):
             raise ValueError("AdamW: lists of one length expected")
-        self._held = given
+        self._held = [list(x) for x in given]              # (the tensors: their addresses are what every step uses)
         self._list = (_AdamWTensor * n)()
         self._shapes = [p.shape for p in params]
         self._device = params[0].device if n else None

@@ -1,4 +1,7 @@
 """The layers' binding on the CPU, with a stand-in for the library that notes what it is called with."""
+import gc
+import weakref
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -43,3 +46,20 @@ def test_a_refused_step_leaves_the_plan_as_it_was(library, first):
     assert library.grad_types == [[layers._TYPES[first]] * 2] * 2
     plan.step([torch.ones(5, dtype=other), torch.ones(6, dtype=first)], 3)
     assert library.grad_types[-1] == [layers._TYPES[other], layers._TYPES[first]]
+
+
+def test_a_plan_keeps_its_tensors_whatever_becomes_of_the_lists(library):
+    params = [torch.ones(300), torch.ones(7)]
+    lists = [params, *layers.adamw_state(params, bits=8), [p.bfloat16() for p in params]]
+    kept = [weakref.ref(t) for x in lists for t in x]
+    plan = layers.AdamW(lists[0], *lists[1:5], copies=lists[5])
+    del params
+    for x in lists:
+        x[0] = torch.zeros(1)
+        x.clear()
+    gc.collect()
+    assert all(r() is not None for r in kept)
+    plan.step([torch.ones(300), torch.ones(7)], 1)
+    del plan
+    gc.collect()
+    assert all(r() is None for r in kept)
