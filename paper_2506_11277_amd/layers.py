@@ -65,6 +65,14 @@ def _type_of(x, what):
     return kind
 
 
+def _sizes(*sizes):
+    """The sizes, which the library takes as ints (larger ones would arrive there as others)."""
+    for n in sizes:
+        if not -1 << 31 <= n < 1 << 31:
+            raise ValueError(f"sizes: {n} is more than the library takes")
+    return sizes
+
+
 def _ld(x, rows, cols, like, what):
     """Row stride of a [rows, cols] device tensor of `like`'s type, on its device, whose rows are contiguous."""
     if x.shape != (rows, cols):
@@ -72,12 +80,14 @@ def _ld(x, rows, cols, like, what):
     if x.dtype is not like.dtype or x.get_device() != like.get_device():
         raise ValueError(f"{what}: {like.dtype} on {like.device} expected")
     ld, step = x.stride()
+    if (rows | cols) >> 30:
+        raise ValueError(f"{what}: sizes below 2^30 expected, got {list(x.shape)}")
     if step != 1 and cols > 1:
         raise ValueError(f"{what}: contiguous rows expected (stride(1) == 1)")
     if rows <= 1:
         return cols or 1
-    if ld < cols or ld < 1:
-        raise ValueError(f"{what}: row stride {ld} smaller than {cols}")
+    if ld < cols or ld < 1 or ld >> 31:
+        raise ValueError(f"{what}: row stride {ld} smaller than {cols} or not below 2^31")
     return ld
 
 
@@ -117,7 +127,7 @@ def _aligned(x, ldx, *rest):
 
 def linear_workspace_bytes(tokens, n_in, n_out, dtype, aligned=True):
     """Bytes of workspace for linear; aligned: every row of x and w starts on 16 bytes (with less a slower way is taken)."""
-    return lib().ozimmu_linear_workspace_bytes(tokens, n_in, n_out, _TYPES[dtype], int(aligned))
+    return lib().ozimmu_linear_workspace_bytes(*_sizes(tokens, n_in, n_out), _TYPES[dtype], int(aligned))
 
 
 def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=None, workspace=None):
@@ -151,7 +161,7 @@ def linear(x, w, bias=None, residual=None, activation=ACT_NONE, pre=None, out=No
 
 def linear_grad_workspace_bytes(tokens, n_in, n_out, dtype, activation=ACT_NONE, aligned=True):
     """Bytes of workspace for linear_grad; aligned: every row of dy, x and w starts on 16 bytes."""
-    return lib().ozimmu_linear_grad_workspace_bytes(tokens, n_in, n_out, _TYPES[dtype], activation, int(aligned))
+    return lib().ozimmu_linear_grad_workspace_bytes(*_sizes(tokens, n_in, n_out), _TYPES[dtype], activation, int(aligned))
 
 
 def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=None, db=None, want=("dx", "dw"), workspace=None):
@@ -269,7 +279,7 @@ MOE_TOKENS, MOE_EXPERTS, MOE_TOP_K = 64, 512, 16       # at most
 
 
 def moe_workspace_bytes(tokens, width, hidden, experts, top_k, dtype):
-    return lib().ozimmu_moe_workspace_bytes(tokens, width, hidden, experts, top_k, _TYPES[dtype])
+    return lib().ozimmu_moe_workspace_bytes(*_sizes(tokens, width, hidden, experts, top_k), _TYPES[dtype])
 
 
 def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, gates=None, workspace=None):
@@ -284,6 +294,8 @@ def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, ga
         (tokens, width), (experts, _, hidden) = x.shape, w_out.shape
     except ValueError:
         raise ValueError("x: a matrix, w_out: three dimensions expected") from None
+    if (experts | hidden | top_k) >> 30:
+        raise ValueError(f"moe: sizes below 2^30 expected, got {experts} experts of {hidden}, {top_k} chosen")
     index = x.get_device()
     for w, shape, what in ((router, (experts, width), "router"), (w_in, (experts, 2 * hidden, width), "w_in"),
                            (w_out, (experts, width, hidden), "w_out")):

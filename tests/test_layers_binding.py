@@ -63,3 +63,36 @@ def test_a_plan_keeps_its_tensors_whatever_becomes_of_the_lists(library):
     del plan
     gc.collect()
     assert all(r() is None for r in kept)
+
+
+@pytest.mark.parametrize("rows,cols,ld", [(2, 8, (1 << 32) + 8), (2, 8, 1 << 31), (2, (1 << 32) + 8, (1 << 32) + 8), ((1 << 32) + 2, 8, 8), (1, 1 << 30, 1 << 30)])
+def test_sizes_that_an_int_cannot_hold_are_refused(rows, cols, ld):
+    # (the library takes ints: 2^32 + 8 would arrive there as 8)
+    x = torch.empty_strided((rows, cols), (ld, 1), dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError):
+        layers._ld(x, rows, cols, x, "x")
+
+
+def test_sizes_up_to_the_largest_are_taken():
+    most = (1 << 30) - 1
+    for rows, cols, ld in ((2, most, (1 << 31) - 1), (most, 1, 1), (0, most, most), (1, 8, 1 << 40)):
+        x = torch.empty_strided((rows, cols), (ld, 1), dtype=torch.bfloat16, device="meta")
+        assert layers._ld(x, rows, cols, x, "x") == (ld if rows > 1 else cols)
+
+
+def test_workspaces_of_sizes_that_an_int_cannot_hold():
+    big = (1 << 32) + 300
+    for call in (lambda: layers.linear_workspace_bytes(big, 8, 8, torch.bfloat16), lambda: layers.linear_grad_workspace_bytes(8, big, 8, torch.bfloat16),
+                 lambda: layers.moe_workspace_bytes(4, 8, big, 8, 2, torch.bfloat16), lambda: layers.moe_workspace_bytes(4, 8, 8, 8, big, torch.bfloat16)):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_experts_that_an_int_cannot_hold_are_refused(library):
+    # (two experts too many would arrive as two)
+    def meta(*shape):
+        return torch.empty(shape, dtype=torch.bfloat16, device="meta")
+
+    for experts, hidden in (((1 << 32) + 2, 8), (2, (1 << 32) + 8)):
+        with pytest.raises(ValueError, match="sizes"):
+            layers.moe(meta(1, 8), meta(experts, 8), meta(experts, 2 * hidden, 8), meta(experts, 8, hidden), 1)
