@@ -197,11 +197,21 @@ __device__ __forceinline__ v2u hold_block(const float (&x)[kEach], const unsigne
     const float t = __uint_as_float(top);
     scale = t * (float)(1.0 / 448.0);
     // (below 2^-100 the quotient would overflow: such a block is held as zeros, or the smallest code)
-    const float factor = t >= 0x1p-100f ? 448.0f / t * 0x1p-120f : 0.0f;
+    const float quotient = t >= 0x1p-100f ? 448.0f / t : 0.0f, factor = quotient * 0x1p-120f;
+    float y[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) y[i] = fabsf(x[i]) * factor;
+    // (from 2^14 on the factor nears the subnormal numbers, and from 3e11 on it would be 0: there its parts are applied one after the other)
+    const bool large = t > 0x1p14f;
+    if (__builtin_expect(__ballot(large) != 0, 0)) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) y[i] = large ? fabsf(x[i]) * quotient * 0x1p-120f : y[i];
+        asm volatile("");
+    }
     v2u codes = {0, 0};
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        unsigned c = (__float_as_uint(fabsf(x[i]) * factor) + word[i]) >> 20;
+        unsigned c = (__float_as_uint(y[i]) + word[i]) >> 20;
         c = c < 0x7e ? c : 0x7e;
         if constexpr (ROOT) {
             const unsigned least = __float_as_uint(x[i]) < 1 ? __float_as_uint(x[i]) : 1;       // 0 of 0 (roots have no sign)
