@@ -132,7 +132,8 @@ __device__ __forceinline__ float activation_slope(int act, float z)
         }
         case OZIMMU_ACT_GELU_TANH: {
             const float s = logistic<FINE>(1.5957691216057308f * (z + 0.044715f * z * z * z));
-            return s + z * 2.0f * s * (1.0f - s) * 0.79788456080286536f * (1.0f + 0.134145f * z * z);
+            const float near = z * s * (1.0f - s) * 2.0f;             // (0 where the square overflows)
+            return near == 0.0f ? s : s + near * 0.79788456080286536f * (1.0f + 0.134145f * z * z);
         }
         case OZIMMU_ACT_SILU: {
             const float s = logistic<FINE>(z);
