@@ -329,18 +329,76 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
 #pragma unroll
                     for (int j = 0; j < NX; ++j) acc[j] = mma(w[u][s], h[u][s][j][o], acc[j], T{});
     }
+    static_assert(NX * 256 <= 64 * kOutWaves, "an entry a lane");
+    const int q = threadIdx.x >> 4, p = threadIdx.x & 15;
+    const bool mine = q < 16 * NX && q < a.tokens && p0 + p < a.width;
+    auto entry = [&]() __attribute__((always_inline)) {                        // this lane's, of the wavefronts' sums
+        __syncthreads();
+        float v = 0.0f;
+        if (mine)
+#pragma unroll
+            for (int s = 0; s < kOutWaves; ++s) v += sums[s][q >> 4][(q & 15) * kStreamLd + p];
+        return v;
+    };
+    const auto finite = [](float x) { return fabsf(x) < __builtin_inff(); };
 #pragma unroll
     for (int j = 0; j < NX; ++j) put_sums(sums[wave][j], acc[j], lane);
-    __syncthreads();
-    for (int i = threadIdx.x; i < NX * 256; i += 64 * kOutWaves) {
-        const int q = i >> 4, p = i & 15;
-        if (q >= a.tokens || p0 + p >= a.width) continue;
-        float v = 0.0f;
+    float v = entry();
+    // Infinities and NaN.  A token that did not choose an expert has zeros for its h, and an infinite weight times 0, or times h's two
+    // numbers of unlike signs, is a NaN; so where a sum of 16 tokens is not finite, the steps are gone over again in two ways: as before, but
+    // of a step a token keeps the sum only if it chose the expert (the same bits as if the others' weights were finite), and
+    // with weights and h as numbers of 32 bits.  The second is taken where the first is not finite either.
+    const int again = __syncthreads_or(mine && !finite(v)) ? NX : 0;
+#pragma nounroll
+    for (int j = 0; j < again; ++j) {
+        const bool odd = mine && q >> 4 == j && !finite(v);
+        if (!__syncthreads_or(odd)) continue;
+        // (a lane's own numbers once more: kept over the loop above, they cost it registers that it spills)
+        int own = threadIdx.x & 63;
+        asm volatile("" : "+v"(own));
+        const int t = 16 * j + (own & 15), f = p0 + (own & 15) < a.width ? p0 + (own & 15) : a.width - 1;
+        v4f same = {0, 0, 0, 0}, wide = {0, 0, 0, 0};
+#pragma nounroll
+        for (int item = begin + wave; item < end; item += kOutWaves) {
+            const int slot = item / steps, k0 = (item - slot * steps) * KE + (own >> 4) * E, place = places[slot * 16 * NX + t];
+            const bool on = place != kNone;
+            const T *wr = (const T *)a.w_out + ((size_t)experts[slot] * a.width + f) * a.hidden;
+            const T *hr = (const T *)a.h + (size_t)(on ? t * a.top_k + place : 0) * a.ldh;
 #pragma unroll
-        for (int s = 0; s < kOutWaves; ++s) v += sums[s][q >> 4][(q & 15) * kStreamLd + p];
-        if (gridDim.y == 1) ((T *)a.y)[(size_t)q * a.ldy + p0 + p] = (T)v;
-        else a.parts[((size_t)blockIdx.y * a.tokens + q) * a.width + p0 + p] = v;
+            for (int s = 0; s < 2; ++s) {
+                typedef typename Chunk<T>::V V;
+                const int k = k0 + s * 4 * E, n = a.hidden - k;
+                const v4u w = load_chunk(wr + k, n);
+                v4u h[H];
+                v4f sum = wide;
+#pragma unroll
+                for (int o = 0; o < H; ++o) h[o] = load_chunk(hr + o * second + k, on ? n : 0);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    float x = (float)__builtin_bit_cast(V, h[0])[e];
+                    if constexpr (H == 2) x += (float)__builtin_bit_cast(V, h[1])[e];
+                    sum = __builtin_amdgcn_mfma_f32_16x16x4f32((float)__builtin_bit_cast(V, w)[e], x, sum, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) wide[i] = on ? sum[i] : wide[i];
+#pragma unroll
+                for (int o = 0; o < H; ++o) {
+                    sum = mma(w, h[o], same, T{});
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) same[i] = on ? sum[i] : same[i];
+                }
+            }
+        }
+        put_sums(sums[wave][j], same, own);
+        const float first = entry();
+        __syncthreads();
+        put_sums(sums[wave][j], wide, own);
+        const float other = entry();
+        if (odd) v = finite(first) ? first : other;
     }
+    if (!mine) return;
+    if (gridDim.y == 1) ((T *)a.y)[(size_t)q * a.ldy + p0 + p] = (T)v;
+    else a.parts[((size_t)blockIdx.y * a.tokens + q) * a.width + p0 + p] = v;
 }
 
 // the parts' sums, in their order

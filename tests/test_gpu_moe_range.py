@@ -1,0 +1,73 @@
+"""ozimmu_moe where values leave the range of 16 bits, or are not finite: each goes where the formula takes it and nowhere else."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from paper_2506_11277_amd import layers
+from tests.layers_reference import TYPES, act
+
+
+def small(tokens, width, hidden, experts, kind, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+
+    def normal(*shape, std=1.0):
+        return torch.randn(*shape, device="cuda", generator=gen).mul_(std).to(TYPES[kind])
+
+    return (normal(tokens, width), normal(experts, width, std=width ** -0.5), normal(experts, 2 * hidden, width, std=width ** -0.5),
+            normal(experts, width, hidden, std=hidden ** -0.5))
+
+
+def formula(x, router, w_in, w_out, chosen, gates):
+    """y in 64 bits from the choices and gates that the library reports, and the sum of its terms' magnitudes."""
+    X, hidden = x.double(), w_out.shape[2]
+    Y, size = torch.zeros(x.shape, device="cuda", dtype=torch.float64), torch.zeros(x.shape, device="cuda", dtype=torch.float64)
+    for t in range(x.shape[0]):
+        for e, g in zip(chosen[t].tolist(), gates[t].double()):
+            both = (w_in[e].double() * X[t]).sum(1)
+            h = g * act("silu", both[:hidden]) * both[hidden:]
+            Y[t] += (w_out[e].double() * h).sum(1)
+            size[t] += (w_out[e].double() * h).abs().sum(1)
+    return Y, size
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("case", [(6, 96, 64, 12, 2), (40, 130, 100, 16, 3), (8, 512, 1024, 64, 8)])
+def test_an_expert_s_weights_reach_only_those_who_chose_it(case, bad, kind):
+    tokens, width, hidden, experts, top_k = case
+    x, router, w_in, w_out = small(tokens, width, hidden, experts, kind, 8)
+    y, chosen, gates = layers.moe(x, router, w_in, w_out, top_k)
+    count = torch.zeros(experts, dtype=torch.long, device="cuda").index_add_(0, chosen.flatten().long(), torch.ones_like(chosen.flatten()).long())
+    expert = int(((count > 0) & (count < tokens)).nonzero()[0])
+    takes = (chosen == expert).any(1)
+    rows = torch.arange(width, device="cuda") % 5 == 2            # output features that have the bad weight
+    w_out[expert, rows, hidden // 3] = bad
+    got, _, _ = layers.moe(x, router, w_in, w_out, top_k)
+    assert torch.equal(got[~takes], y[~takes])
+    assert torch.equal(got[takes][:, ~rows], y[takes][:, ~rows])
+    # the rest: a NaN, or an infinity of the sign of its hidden value (which is not 0)
+    want, _ = formula(x, router, w_in, w_out, chosen, gates)
+    there = got[takes][:, rows].double()
+    assert torch.equal(torch.nan_to_num(there, nan=7.0), torch.nan_to_num(want[takes][:, rows], nan=7.0))
+    assert not torch.isfinite(there).any()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+def test_hidden_values_that_are_not_finite_stay_their_token_s(kind):
+    tokens, width, hidden, experts, top_k = 9, 64, 40, 6, 2
+    x, router, w_in, w_out = small(tokens, width, hidden, experts, kind, 9)
+    y, chosen, gates = layers.moe(x, router, w_in, w_out, top_k)
+    expert = int(chosen[0, 0])
+    w_in[expert, hidden + 5, 0] = float("inf")                    # an up row: h is an infinity for every token of this expert
+    got, _, _ = layers.moe(x, router, w_in, w_out, top_k)
+    takes = (chosen == expert).any(1)
+    want, _ = formula(x, router, w_in, w_out, chosen, gates)
+    assert torch.equal(got[~takes], y[~takes])
+    assert torch.equal(got[takes].isnan(), want[takes].isnan()) and torch.equal(got[takes].isinf(), want[takes].isinf())
+    assert torch.equal(torch.sign(got[takes].double()), torch.sign(want[takes]))
+    router[expert] = float("nan")                                 # every token takes it, with a NaN for its gate
+    got, chosen, gates = layers.moe(x, router, w_in, w_out, top_k)
+    assert bool((chosen == expert).any(1).all()) and bool(got.isnan().all())
