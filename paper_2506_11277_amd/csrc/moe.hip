@@ -3,7 +3,7 @@
 //   moe_route_kernel   a work-group per token: logits of all experts, the chosen ones and their gates (for one to four tokens and
 //                      a small router the second kernel does that by itself)
 //   moe_hidden_kernel  a work-group per 16 hidden features of an expert that some token chose: gate and up rows against
-//                      the tokens that chose it, h = gate silu(a) b rounded for the next product
+//                      the tokens that chose it, h = gate silu(a) b
 //   moe_out_kernel     a work-group per 16 output features: their rows of every chosen expert against its tokens' h, all in one
 //                      sum, so nothing is scattered and no atomics change an order; in two to eight parts, which
 //                      moe_join_kernel adds, where the features are too few for all compute units
@@ -21,10 +21,52 @@ namespace {
 
 constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 16;
 constexpr int kWords = OZIMMU_MOE_EXPERTS / 32;
-// The hidden layer is kept as the sum of two numbers of 16 bits: rounded to one, it alone would add as much to the result's error as
-// the result's own rounding.  The second one's products take matrix instructions that wait for memory anyway.
+// The hidden layer is kept as the sum of two numbers of 16 bits (bf16: to 2^-18 of h; f16: to 2^-24 of it, but to no less than 2^-25):
+// rounded to one, it alone would add as much to the result's error as the result's own rounding.  The second one's products take
+// matrix instructions that wait for memory anyway.
 template <class T>
 constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
+
+// h's numbers: h itself, or the nearest number of 16 bits and what it leaves.  A finite h that f16 has no number for becomes a NaN for the
+// matrix instructions, so that the sums show it, and 26 bits of its own for the second look that they then get: its sign and how far
+// |h|'s bits are above those of 2^15, without the last five; the first number has the upper 9 of these 25 behind what makes it a
+// NaN, the second one the others.
+constexpr unsigned kLeastCode = 0x47000000u;                    // 2^15
+__device__ __forceinline__ void put_hidden(float h, float *first, size_t) { *first = h; }
+__device__ __forceinline__ void put_hidden(float h, bf16 *first, size_t second)
+{
+    const float most = 0x1.fep127f;                             // (bf16's largest: larger ones would be rounded to infinity)
+    const bf16 b = (bf16)(fabsf(h) < __builtin_inff() ? fminf(fmaxf(h, -most), most) : h);
+    first[0] = b;
+    first[second] = (bf16)(fabsf(h) < __builtin_inff() ? h - (float)b : 0.0f);
+}
+__device__ __forceinline__ void put_hidden(float h, f16 *first, size_t second)
+{
+    const f16 b = (f16)h;
+    unsigned short one = __builtin_bit_cast(unsigned short, b), two = 0;
+    if (h != h) {
+        one = 0x7e00;
+    } else if (fabsf(h) < __builtin_inff()) {
+        if (fabsf((float)b) < __builtin_inff()) {
+            two = __builtin_bit_cast(unsigned short, (f16)(h - (float)b));
+        } else {
+            const unsigned bits = __float_as_uint(h), code = ((bits & 0x7fffffffu) - kLeastCode) >> 5;      // (25 bits, at least 3 << 16)
+            one = (unsigned short)((bits >> 16 & 0x8000u) | 0x7e00u | code >> 16);
+            two = (unsigned short)code;
+        }
+    }
+    first[0] = __builtin_bit_cast(f16, one);
+    first[second] = __builtin_bit_cast(f16, two);
+}
+__device__ __forceinline__ float get_hidden(float first, float) { return first; }
+__device__ __forceinline__ float get_hidden(bf16 first, bf16 second) { return (float)first + (float)second; }
+__device__ __forceinline__ float get_hidden(f16 first, f16 second)
+{
+    const unsigned one = __builtin_bit_cast(unsigned short, first), two = __builtin_bit_cast(unsigned short, second);
+    if ((one & 0x7e00u) == 0x7e00u && (one & 0x1ffu) != 0)
+        return __uint_as_float((one & 0x8000u) << 16 | ((((one & 0x1ffu) << 16 | two) << 5 | 16) + kLeastCode));
+    return (float)first + (float)second;
+}
 constexpr int kRouteHere = 64;                                  // choices that fit the second kernel's own routing
 
 // bit map of the experts that the `n` choices name
@@ -239,9 +281,7 @@ __global__ __launch_bounds__(64 * kHiddenWaves) void moe_hidden_kernel(MoeArgs a
             }
             const int choice = choices[c0 + q];
             const float h = gates[choice] * activate<T>(OZIMMU_ACT_SILU, g) * u;
-            T *to = (T *)a.h + (size_t)choice * a.ldh + f0 + f;
-            *to = (T)h;
-            if constexpr (kParts<T> == 2) to[(size_t)all * a.ldh] = (T)(fabsf(h) < __builtin_inff() ? h - (float)(T)h : 0.0f);
+            put_hidden(h, (T *)a.h + (size_t)choice * a.ldh + f0 + f, (size_t)all * a.ldh);
         }
         __syncthreads();
     }
@@ -345,9 +385,10 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
     for (int j = 0; j < NX; ++j) put_sums(sums[wave][j], acc[j], lane);
     float v = entry();
     // Infinities and NaN.  A token that did not choose an expert has zeros for its h, and an infinite weight times 0, or times h's two
-    // numbers of unlike signs, is a NaN; so where a sum of 16 tokens is not finite, the steps are gone over again in two ways: as before, but
+    // numbers of unlike signs, is a NaN, and so are values of h beyond f16; so where a sum of 16 tokens is not finite, the steps are gone over again in two ways: as before, but
     // of a step a token keeps the sum only if it chose the expert (the same bits as if the others' weights were finite), and
-    // with weights and h as numbers of 32 bits.  The second is taken where the first is not finite either.
+    // with weights and h as numbers of 32 bits.  The second is taken where the first is not finite either.  (8 tokens, 64 experts of 2048 x
+    // 1024, a NaN or a large h in every work-group's sums: the launch 100 to 110 us instead of 40.)
     const int again = __syncthreads_or(mine && !finite(v)) ? NX : 0;
 #pragma nounroll
     for (int j = 0; j < again; ++j) {
@@ -375,8 +416,7 @@ __global__ __launch_bounds__(64 * kOutWaves) void moe_out_kernel(MoeArgs a)
                 for (int o = 0; o < H; ++o) h[o] = load_chunk(hr + o * second + k, on ? n : 0);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    float x = (float)__builtin_bit_cast(V, h[0])[e];
-                    if constexpr (H == 2) x += (float)__builtin_bit_cast(V, h[1])[e];
+                    const float x = get_hidden(__builtin_bit_cast(V, h[0])[e], __builtin_bit_cast(V, h[H - 1])[e]);
                     sum = __builtin_amdgcn_mfma_f32_16x16x4f32((float)__builtin_bit_cast(V, w)[e], x, sum, 0, 0, 0);
                 }
 #pragma unroll

@@ -33,6 +33,29 @@ def formula(x, router, w_in, w_out, chosen, gates):
     return Y, size
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("case", [(1, 64, 48, 4, 2), (6, 128, 80, 16, 4), (20, 96, 200, 8, 2), (50, 40, 33, 24, 3), (8, 512, 1024, 64, 8)])
+@pytest.mark.parametrize("size", [3e4, 7e4, 3e5, 1e9])
+def test_hidden_values_beyond_16_bits(case, kind, size):
+    tokens, width, hidden, experts, top_k = case
+    x, router, w_in, w_out = small(tokens, width, hidden, experts, kind, 7)
+    # a few hidden features are outliers, of about `size` where silu(a) is near a (both rows are scaled), and the output's weights
+    # are small enough for the result to fit
+    some = torch.arange(hidden, device="cuda") % 7 == 3
+    factor = min(size ** 0.5, 3e4)
+    w_in[:, :hidden][:, some] *= factor
+    w_in[:, hidden:][:, some] *= factor
+    w_out *= 2000.0 / size / 8
+    y, chosen, gates = layers.moe(x, router, w_in, w_out, top_k)
+    want, terms = formula(x, router, w_in, w_out, chosen, gates)
+    assert bool(torch.isfinite(y).all())
+    # both products' sums in 32 bits (an outlier is the product of two sums, each off by at most (width + 8) 2^-24 of its terms'
+    # magnitudes, which for random rows is several times its own size) and one rounding
+    u = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8, "f32": 2.0 ** -24}[kind]
+    off = (y.double() - want).abs()
+    assert bool((off <= u * want.abs() + 2e-5 * terms.amax(1, keepdim=True) + 2.0 ** -24).all()), float((off / terms).max())
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("case", [(6, 96, 64, 12, 2), (40, 130, 100, 16, 3), (8, 512, 1024, 64, 8)])
