@@ -215,7 +215,8 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     if (bad_workspace(workspace, workspace_bytes, linear_workspace(tokens, n_in, n_out, type, true).total)) return OZIMMU_BAD_ARG;
     if (tokens == 0 || n_out == 0) return OZIMMU_OK;
     const LinearWorkspace ws = linear_workspace(tokens, n_in, n_out, type, false);
-    const bool room = ws.copies_bytes > 0 && workspace_bytes >= ws.total;
+    // (a workspace that is not needed may be anywhere, but copies go to 16 bytes)
+    const bool room = ws.copies_bytes > 0 && workspace_bytes >= ws.total && (uintptr_t)workspace % 256 == 0;
     Product a{};
     a.P = w;
     a.ldp = ldw;
