@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kBlock = 256;                      // values that share a scale in 8 bits
 constexpr int kTensors = 48;                     // 48 * 80 + 56 bytes of arguments
+constexpr int kChunks = 0xffffff;                // work-groups of a launch: fewer than 2^32 work-items
 
 struct Tensor {
     void *p;
@@ -332,7 +333,7 @@ extern "C" int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const 
 {
     if (tensors < 0 || (tensors > 0 && list == nullptr) || step < 1) return OZIMMU_BAD_ARG;
     if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1 && eps >= 0) || lr != lr || weight_decay != weight_decay) return OZIMMU_BAD_ARG;
-    long long total = 0;
+    long long total = 0, most = 0;
     for (int i = 0; i < tensors; ++i) {
         const ozimmu_adamw_tensor &x = list[i];
         const void *g = grads ? grads[i] : x.grad;
@@ -348,6 +349,7 @@ extern "C" int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const 
             (ss == 1 && ((uintptr_t)x.m_scale % 4 || (uintptr_t)x.v_scale % 4)))
             return OZIMMU_BAD_ARG;
         total += (x.count + kBlock - 1) / kBlock;
+        most = x.count > most ? x.count : most;
     }
     Args a{};
     a.b1 = (float)beta1;
@@ -360,6 +362,7 @@ extern "C" int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const 
     a.keep = (float)(1.0 - lr * weight_decay);
     a.word0 = seed + (uint32_t)step * 0xbb67ae85u;
     a.per_chunk = total > 16 * 4096 ? 16 : 8;       // blocks of a work-group: 2 or 4 (8 bits: 1 or 2) rounds of its wavefronts
+    while (most > (long long)kChunks * kBlock * a.per_chunk) a.per_chunk *= 2;
     const hipStream_t st = (hipStream_t)stream;
 
     long long block0 = 0, chunks = 0;
@@ -379,8 +382,7 @@ extern "C" int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const 
         if (x.count == 0) continue;
         const void *g = grads ? grads[i] : x.grad;
         const long long blocks = (x.count + kBlock - 1) / kBlock, need = (blocks + a.per_chunk - 1) / a.per_chunk;
-        if (need > 0x7fffffff) return OZIMMU_BAD_ARG;
-        if (a.tensors == kTensors || chunks + need > 0x7fffffff || kind[0] != x.param_type || kind[1] != x.grad_type || kind[2] != x.state_type) {
+        if (a.tensors == kTensors || chunks + need > kChunks || kind[0] != x.param_type || kind[1] != x.grad_type || kind[2] != x.state_type) {
             if (flush() != hipSuccess) return OZIMMU_HIP_ERROR;
             kind[0] = x.param_type;
             kind[1] = x.grad_type;

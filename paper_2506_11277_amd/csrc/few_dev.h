@@ -14,7 +14,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(Product a, f
     constexpr int KE = 8 * Chunk<T>::E;
     __shared__ __attribute__((aligned(16))) float sums[kFewWaves][16 * kStreamLd];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int p0 = blockIdx.x * 16, row = p0 + (lane & 15);
+    const int p0 = (int)(blockIdx.z * kGridRow + blockIdx.x) * 16, row = p0 + (lane & 15);
+    if (p0 >= a.e.np) return;
     const T *const w[1] = {(const T *)a.P + (size_t)(row < a.e.np ? row : a.e.np - 1) * a.ldp};
     const bool on[1] = {(lane & 15) < a.e.nq};
     const T *const x[1] = {(const T *)a.Q + (size_t)(on[0] ? lane & 15 : 0) * a.ldq};
@@ -39,7 +40,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(Product a, f
 template <class T>
 hipError_t launch_few_tokens(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
-    const dim3 grid((a.e.np + 15) / 16, plan.splits);
+    const int groups = (a.e.np + 15) / 16;
+    const dim3 grid(grid_row(groups), plan.splits, grid_rows(groups));
     float *const to = plan.splits > 1 ? partial : nullptr;
     // (steps whose loads a wavefront issues together: no more than it has)
     if (plan.steps > 2 * kFewWaves) few_tokens_kernel<T, 4><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);

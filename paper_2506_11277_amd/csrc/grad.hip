@@ -57,7 +57,7 @@ template <class T>
 __global__ __launch_bounds__(256) void bias_grad_kernel(BiasGrad b)
 {
     __shared__ float part[256];
-    bias_grad<T>(b, blockIdx.x, part);
+    bias_grad<T>(b, (int)(blockIdx.y * kGridRow + blockIdx.x), part);
 }
 
 template <class T>
@@ -81,9 +81,10 @@ hipError_t launch_bias_grad(const BiasGrad &b, int type, hipStream_t st)
 {
     const int blocks = bias_grad_blocks(b);
     if (blocks == 0) return hipSuccess;
-    if (type == OZIMMU_BF16) bias_grad_kernel<bf16><<<blocks, 256, 0, st>>>(b);
-    else if (type == OZIMMU_F16) bias_grad_kernel<f16><<<blocks, 256, 0, st>>>(b);
-    else bias_grad_kernel<float><<<blocks, 256, 0, st>>>(b);
+    const dim3 grid(grid_row(blocks), grid_rows(blocks));
+    if (type == OZIMMU_BF16) bias_grad_kernel<bf16><<<grid, 256, 0, st>>>(b);
+    else if (type == OZIMMU_F16) bias_grad_kernel<f16><<<grid, 256, 0, st>>>(b);
+    else bias_grad_kernel<float><<<grid, 256, 0, st>>>(b);
     return hipGetLastError();
 }
 

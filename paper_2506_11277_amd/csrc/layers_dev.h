@@ -265,6 +265,12 @@ __device__ __forceinline__ void bias_grad(const BiasGrad &b, int block, float *p
     if (wave == 0 && c < b.n) ((T *)b.db)[c] = (T)((part[lane] + part[64 + lane]) + (part[128 + lane] + part[192 + lane]));
 }
 
+// HIP takes less than 2^32 work-items along a dimension of a grid: rows of at most kGridRow work-groups (of up to 512; a multiple of
+// the XCDs), one behind the other along y or z.
+constexpr unsigned kGridRow = 1u << 22;
+inline unsigned grid_row(long long groups) { return groups < kGridRow ? (unsigned)groups : kGridRow; }
+inline unsigned grid_rows(long long groups) { return (unsigned)((groups + kGridRow - 1) / kGridRow); }
+
 enum Tile { kTile256, kTile128, kTile64, kTileFew };      // edge; few_tokens_kernel
 struct ProductPlan {
     int tile;

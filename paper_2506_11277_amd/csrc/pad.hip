@@ -10,7 +10,7 @@ template <class T>
 __global__ __launch_bounds__(256) void pad_kernel(PadCopies a)
 {
     constexpr int E = Chunk<T>::E;
-    long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    long long i = ((long long)blockIdx.y * kGridRow + blockIdx.x) * 256 + threadIdx.x;
     const long long first = a.c[0].rows * (a.c[0].ldto / E), all = first + a.c[1].rows * (a.c[1].ldto / E);
     if (i >= all) return;
     const bool second = i >= first;
@@ -30,10 +30,10 @@ hipError_t launch_pad(const PadCopies &a, int type, hipStream_t st)
     const long long chunks = a.c[0].rows * (a.c[0].ldto / e) + a.c[1].rows * (a.c[1].ldto / e);
     if (chunks == 0) return hipSuccess;
     const long long groups = (chunks + 255) / 256;
-    if (groups > 0xffffff) return hipErrorInvalidValue;
-    if (type == OZIMMU_BF16) pad_kernel<bf16><<<(unsigned)groups, 256, 0, st>>>(a);
-    else if (type == OZIMMU_F16) pad_kernel<f16><<<(unsigned)groups, 256, 0, st>>>(a);
-    else pad_kernel<float><<<(unsigned)groups, 256, 0, st>>>(a);
+    const dim3 grid(grid_row(groups), grid_rows(groups));
+    if (type == OZIMMU_BF16) pad_kernel<bf16><<<grid, 256, 0, st>>>(a);
+    else if (type == OZIMMU_F16) pad_kernel<f16><<<grid, 256, 0, st>>>(a);
+    else pad_kernel<float><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

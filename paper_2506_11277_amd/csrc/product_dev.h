@@ -529,21 +529,24 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
 }
 
 template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT>
-__global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float *partial, int steps_per_split, int tiles_p, int tiles_q)
+__global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float *partial, int steps_per_split, int tiles_p, int tiles_q, int blocks)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    product_tile<T, PK, QK, BP, BQ, WP, WQ, DIRECT>(a, partial, steps_per_split, tiles_p, tiles_q, blockIdx.x, lds);
+    const int block = (int)(blockIdx.z * kGridRow + blockIdx.x);
+    if (block >= blocks) return;
+    product_tile<T, PK, QK, BP, BQ, WP, WQ, DIRECT>(a, partial, steps_per_split, tiles_p, tiles_q, block, lds);
 }
 
 // dx, dw and the bias gradient of a layer in one launch: each alone leaves compute units without work in its last round, or
 // in its only one, and costs a launch (500 x 512 x 384 f32: the call 35 us in three launches, 19 in one; 1777 x 1024 x 2304 f16: 63
 // and 33).
 template <class T, int BP, int BQ>
-__global__ __launch_bounds__(256) void product_pair_kernel(Product dx, Product dw, BiasGrad db, int blocks_dx, int blocks_dw)
+__global__ __launch_bounds__(256) void product_pair_kernel(Product dx, Product dw, BiasGrad db, int blocks_dx, int blocks_dw, int blocks)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     constexpr int KE = 8 * Chunk<T>::E;
-    int b = blockIdx.x;
+    int b = (int)(blockIdx.z * kGridRow + blockIdx.x);
+    if (b >= blocks) return;
     if (b < blocks_dx) {
         product_tile<T, false, true, BP, BQ, 2, 2, true>(dx, nullptr, (dx.nk + KE - 1) / KE, (dx.e.np + BP - 1) / BP, (dx.e.nq + BQ - 1) / BQ, b, lds);
         return;
@@ -562,7 +565,7 @@ template <class T>
 __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, const float *partial, int splits)
 {
     const int groups = (e.np + 7) / 8;
-    const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t at = ((size_t)blockIdx.y * kGridRow + blockIdx.x) * 256 + threadIdx.x;
     if (at >= (size_t)groups * e.nq) return;
     const int q = (int)(at / groups), p = (int)(at % groups) * 8;
     const size_t plane = (size_t)e.nq * groups * 8;
@@ -590,7 +593,8 @@ hipError_t launch_product_shape(const Product &a, const ProductPlan &plan, float
     const auto kernel = product_kernel<T, PK, QK, BP, BQ, WP, WQ, DIRECT>;
     static std::atomic<unsigned long long> done{0};
     if (hipError_t e = allow_dynamic_lds((const void *)kernel, S::kLds, done)) return e;
-    kernel<<<dim3((unsigned)blocks, plan.splits), S::kThreads, S::kLds, st>>>(a, plan.splits > 1 ? partial : nullptr, plan.steps, tiles_p, tiles_q);
+    kernel<<<dim3(grid_row(blocks), plan.splits, grid_rows(blocks)), S::kThreads, S::kLds, st>>>(a, plan.splits > 1 ? partial : nullptr, plan.steps,
+                                                                                                 tiles_p, tiles_q, (int)blocks);
     return hipGetLastError();
 }
 
@@ -620,7 +624,7 @@ hipError_t launch_join(const Product &a, const ProductPlan &plan, const float *p
 {
     const size_t threads = (size_t)a.e.nq * ((a.e.np + 7) / 8), groups = (threads + 255) / 256;
     if (groups > 0x7fffffff) return hipErrorInvalidValue;
-    product_join_kernel<T><<<(unsigned)groups, 256, 0, st>>>(a.e, partial, plan.splits);
+    product_join_kernel<T><<<dim3(grid_row(groups), grid_rows(groups)), 256, 0, st>>>(a.e, partial, plan.splits);
     return hipGetLastError();
 }
 
@@ -642,7 +646,7 @@ hipError_t launch_pair_shape(const Product &dx, const Product &dw, const BiasGra
     const auto kernel = product_pair_kernel<T, B, B>;
     static std::atomic<unsigned long long> done{0};
     if (hipError_t e = allow_dynamic_lds((const void *)kernel, S::kLds, done)) return e;
-    kernel<<<(unsigned)blocks, S::kThreads, S::kLds, st>>>(dx, dw, db, (int)bx, (int)bw);
+    kernel<<<dim3(grid_row(blocks), 1, grid_rows(blocks)), S::kThreads, S::kLds, st>>>(dx, dw, db, (int)bx, (int)bw, (int)blocks);
     return hipGetLastError();
 }
 
