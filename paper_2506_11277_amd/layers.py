@@ -2,12 +2,17 @@
 
 Argument marshalling only, as in `ozimmu`: PyTorch provides device memory and the current stream.  Matrices are torch
 tensors with a token (or an output feature of a weight) per row, stride(1) == 1 and any row stride.
+
+Nothing here is recorded by autograd: results do not require gradients whatever the operands do (linear_grad forms linear's;
+to use them under autograd, call both from a torch.autograd.Function), and a given output is overwritten without a trace in its
+version counter.  AdamW.step does raise the counters of what it writes, so that autograd notices a saved weight that changed.
 """
 import ctypes
 from array import array
 from operator import attrgetter
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import ozimmu
 from .ozimmu import BAD_ARG, OK, OzimmuError
@@ -231,6 +236,7 @@ class AdamW:
         if any(len(x) != n for x in given):
             raise ValueError("AdamW: lists of one length expected")
         self._held = [list(x) for x in given]              # (the tensors: their addresses are what every step uses)
+        self._weights = self._held[0] + (self._held[-1] if copies is not None else [])
         self._list = (_AdamWTensor * n)()
         self._shapes = [p.shape for p in params]
         self._device = params[0].device if n else None
@@ -273,6 +279,7 @@ class AdamW:
                                           seed & 0xffffffff, _stream(self._devices[0] if self._devices else _get_device(), "AdamW"))
         if rc != OK:
             raise OzimmuError(rc, "adamw")
+        increment_version(self._weights)
 
 
 MOE_TOKENS, MOE_EXPERTS, MOE_TOP_K = 64, 512, 16       # at most

@@ -96,3 +96,16 @@ def test_experts_that_an_int_cannot_hold_are_refused(library):
     for experts, hidden in (((1 << 32) + 2, 8), (2, (1 << 32) + 8)):
         with pytest.raises(ValueError, match="sizes"):
             layers.moe(meta(1, 8), meta(experts, 8), meta(experts, 2 * hidden, 8), meta(experts, 8, hidden), 1)
+
+
+def test_autograd_notices_weights_that_a_step_changed(library):
+    weight = torch.ones(3, requires_grad=True)
+    m, v, _, _ = layers.adamw_state([weight])
+    half = weight.detach().bfloat16()
+    plan = layers.AdamW([weight], m, v, copies=[half])
+    x = torch.ones(3, requires_grad=True)
+    loss, rounded = (x * weight).sum(), (x.bfloat16() * half).sum()
+    plan.step([torch.ones(3)], 1)
+    for saved in (loss, rounded):
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            saved.backward()
