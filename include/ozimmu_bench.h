@@ -107,7 +107,13 @@ int ozimmu_calibration_copy(void *dst, const void *src, size_t bytes, void *stre
  *   none).  Process-wide host state; not while another thread is inside an estimate.
  * ozimmu_debug_vectors_parts: parts of k in which an m x n x k product with s slices of both operands (leading
  *   dimensions m, k and m) runs in the few-vectors kernel, 0 where it runs in another.  Host only.
+ * ozimmu_debug_linear_tile: edge of the tiles in which ozimmu_linear (which = 0), or the dx (1) and dw (2) of ozimmu_linear_grad, multiply
+ *   operands of these sizes and this type (of ozimmu_layers.h) whose rows all start and end on 16 bytes (aligned = 1) or do not and
+ *   are not copied (0); 16 for the kernel for few tokens; which = 3: of the one launch that forms dx, dw and the bias gradient of
+ *   aligned operands, 0 where they are formed in launches of their own.
+ *   *parts [host], may be NULL, receives the parts of the contraction.  Host only; OZIMMU_BAD_ARG (1) for other arguments.
  */
+int ozimmu_debug_linear_tile(int which, int tokens, int n_in, int n_out, int type, int aligned, int *parts);
 int ozimmu_debug_diagonals(int m, int n, int k, int s, const void *workspace, int32_t *D, void *stream);
 long long ozimmu_debug_setup_threads(int m, int n, int k);
 int ozimmu_debug_vectors_parts(int m, int n, int k, int s);

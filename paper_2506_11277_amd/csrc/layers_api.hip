@@ -1,4 +1,5 @@
 // extern "C" boundary of the feed-forward operators (ozimmu_layers.h): argument checks, plans, kernel sequencing.
+#include "../../include/ozimmu_bench.h"
 #include "layers.h"
 
 namespace oz {
@@ -233,6 +234,22 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     const hipStream_t st = (hipStream_t)stream;
     if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     return launch_product(a, plan, type, (float *)workspace, st) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+}
+
+int ozimmu_debug_linear_tile(int which, int tokens, int n_in, int n_out, int type, int aligned, int *parts)
+{
+    if (which < 0 || which > 3 || bad_sizes(tokens, n_in, n_out) || bad_type(type)) return OZIMMU_BAD_ARG;
+    const int np = which == 0 ? n_out : n_in, nq = which == 2 ? n_out : tokens, nk = which == 0 ? n_in : which == 1 ? n_out : tokens;
+    const ProductPlan plan = plan_product(np, nq, nk, type, which == 0, aligned != 0);
+    if (parts) *parts = which == 3 ? 1 : plan.splits;
+    if (which < 3) return plan.tile == kTileFew ? 16 : kShapes[plan.tile].edge;
+    Product dx{}, dw{};
+    dx.nk = n_out;
+    dx.e.np = dw.e.np = n_in;
+    dx.e.nq = dw.nk = tokens;
+    dw.e.nq = n_out;
+    const int tile = plan_pair(dx, plan_product(n_in, tokens, n_out, type, false, true), dw, plan_product(n_in, n_out, tokens, type, false, true), type, true);
+    return tile < 0 ? 0 : kShapes[tile].edge;
 }
 
 size_t ozimmu_linear_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation, int aligned)
