@@ -107,7 +107,7 @@ int ozimmu_adamw(int tensors, const ozimmu_adamw_tensor *list, const void *const
  *   x, y [tokens, width]; router [experts, width], w_in [experts, 2 hidden, width], w_out [experts, width, hidden] contiguous;
  *   all of `type`.  chosen [tokens, top_k]: the experts of each token in ascending order; gates: theirs, float.
  * The values of the hidden layer, with their gate, go into the second product as one float or as the sum of two numbers of
- * 16 bits: bfloat16 to 2^-18 of them, float16 to 2^-24, but to no less than 2^-25 (beyond float16's range to 2^-18).  A NaN logit
+ * 16 bits: bfloat16 to 2^-16 of them, float16 to 2^-22, but to no less than 2^-25 (beyond float16's range to 2^-18).  A NaN logit
  * counts as larger than any number.
  * 1 <= top_k <= experts <= OZIMMU_MOE_EXPERTS, top_k <= OZIMMU_MOE_TOP_K.
  */

@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kRouteWaves = 16, kHiddenWaves = 4, kOutWaves = 16;
 constexpr int kWords = OZIMMU_MOE_EXPERTS / 32;
-// The hidden layer is kept as the sum of two numbers of 16 bits (bf16: to 2^-18 of h; f16: to 2^-24 of it, but to no less than 2^-25):
+// The hidden layer is kept as the sum of two numbers of 16 bits (bf16: to 2^-16 of h; f16: to 2^-22 of it, but to no less than 2^-25):
 // rounded to one, it alone would add as much to the result's error as the result's own rounding.  The second one's products take
 // matrix instructions that wait for memory anyway.
 template <class T>

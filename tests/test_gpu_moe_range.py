@@ -94,3 +94,35 @@ def test_hidden_values_that_are_not_finite_stay_their_token_s(kind):
     router[expert] = float("nan")                                 # every token takes it, with a NaN for its gate
     got, chosen, gates = layers.moe(x, router, w_in, w_out, top_k)
     assert bool((chosen == expert).any(1).all()) and bool(got.isnan().all())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("case", [(40, 64, 32, 4), (8, 200, 24, 6), (3, 512, 48, 5)])
+def test_the_hidden_layer_is_not_rounded_to_16_bits(case, kind):
+    # tokens with one entry, a 1, that choose one expert, whose gate is 1: the hidden layer's sums are exact, and of the result's error
+    # there is left what the activation has, the second product's sums in 32 bits, h's two numbers, and one rounding
+    tokens, width, hidden, experts = case
+    x, router, w_in, w_out = small(tokens, width, hidden, experts, kind, 10)
+    w_in *= width ** 0.5
+    x.zero_()
+    x[torch.arange(tokens), torch.arange(tokens) * 7 % width] = 1.0
+    y, chosen, gates = layers.moe(x, router, w_in, w_out, 1)
+    assert bool((gates == 1).all())
+    both = torch.stack([w_in[e].double()[:, t * 7 % width] for t, e in enumerate(chosen[:, 0].tolist())])
+    a, b = both[:, :hidden], both[:, hidden:]
+    s, W = act("silu", a), w_out[chosen[:, 0].long()].double()
+    h = s * b
+    # (a number of p bits is off by up to 2^-p of itself, two of them by 2^-2p)
+    u32, least, part = 2.0 ** -24, *{"bf16": (0.0, 2.0 ** -16), "f16": (2.0 ** -25, 2.0 ** -22)}[kind]
+    hb = 16 * u32 * (s.abs() + a.abs() * (1 + a.abs())) * b.abs() + 4 * u32 * h.abs() + part * h.abs() + least
+
+    def product(v):
+        return torch.matmul(W, v.unsqueeze(2)).squeeze(2)
+
+    want, size = product(h), torch.matmul(W.abs(), h.abs().unsqueeze(2)).squeeze(2)
+    bound = size * ((2 * hidden + 8) * u32) + torch.matmul(W.abs(), hb.unsqueeze(2)).squeeze(2)
+    least, most = (want - bound).to(TYPES[kind]), (want + bound).to(TYPES[kind])       # what rounding once can make of it
+    assert bool(((y >= least) & (y <= most)).all())
+    # ... which one number of 16 bits would not keep to
+    once = product(h.to(TYPES[kind]).double()).to(TYPES[kind])
+    assert int(((once < least) | (once > most)).sum()) > want.numel() // 100
