@@ -129,7 +129,9 @@ __device__ __forceinline__ void words_of(unsigned long long at, unsigned word0, 
 }
 
 // Square roots.  The instruction is a unit off at times and takes no subnormal numbers: where a wavefront has values below 2^-96,
-// all are scaled.  ROUNDED: the neighbour is taken where the residual says so (0, infinities and NaN stay as they are).
+// all are scaled.  ROUNDED: r is the root rounded to nearest if r (r - ulp) < x <= r (r + ulp), else a neighbour is (Tuckerman's test: Agarwal,
+// Cooley, Gustavson, Shearer, Slishman, Tuckerman, "New scalar and vector elementary functions for the IBM System/370", 1986);
+// the sign of either difference is exact in a fused multiply-add (0, infinities and NaN stay as they are).
 template <bool ROUNDED, int N>
 __device__ __forceinline__ void roots_of(const float (&v)[N], float (&root)[N])
 {

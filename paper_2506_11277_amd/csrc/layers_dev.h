@@ -231,7 +231,7 @@ __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, floa
     }
 }
 
-// ---- launchers, one set per element type (layers_bf16.hip, layers_f16.hip, layers_f32.hip)
+// ---- launchers, one set per element type (product_bf16.hip, product_f16.hip, product_f32.hip)
 
 // D[q][p] = sum over k of P Q.  An operand's rows (p or q) are contiguous along k (`k_rows`), or its entries of one k are
 // contiguous along p or q.

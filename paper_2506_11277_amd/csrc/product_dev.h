@@ -5,9 +5,9 @@
 // that fits) or four: the copies of a step are issued one to three steps before its products, one barrier a step.
 //
 // What bounds it: 256 x 256 in 16 bits the matrix instructions at the clock that the board's power leaves them, with LDS (128 KB read
-// and 64 written a step of 2048 cycles of matrix instructions) close behind: 8192^3 bf16 1.5 PFLOP/s, 4096^3 1.25, 8192 x 4096 x 8192
-// with a gelu and `pre` 1.2.  128 x 128 and 64 x 64 LDS: 96 and 48 KB a step of 512 and 128 cycles (2048^3 780 TFLOP/s,
-// 1024^3 of either 130).  32 bits: the matrix instructions (2048^3 127 TFLOP/s, 4096^3 139).
+// and 64 written a step of 2048 cycles of matrix instructions) close behind: 8192^3 bf16 1.43 PFLOP/s, 4096^3 1.36, 8192 x 4096 x 8192
+// with a gelu and `pre` 1.2.  128 x 128 and 64 x 64 LDS: 96 and 48 KB a step of 512 and 128 cycles (2048^3 770 TFLOP/s,
+// 1024^3 260).  32 bits: the matrix instructions (2048^3 133 TFLOP/s, 4096^3 140).
 //
 // k_rows: the entries of an operand's row are contiguous along k (activations and weights of a forward pass).  LDS row r
 //   holds its 8 chunks of 16 bytes at position chunk ^ (r / 2 % 8): the 16 rows that a matrix instruction's operand takes
