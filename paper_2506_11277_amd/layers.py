@@ -228,7 +228,7 @@ class AdamW:
 
     params: float32, bfloat16 or float16; m, v and their scales as adamw_state gives them (float32 moments, or float8_e4m3fn
     ones with scales); copies: None, or a bfloat16 or float16 tensor per parameter that receives it with every step.
-    The plan holds the tensors; one that is replaced or resized needs a new plan."""
+    The plan holds the tensors, which may not overlap; one that is replaced or resized needs a new plan."""
 
     def __init__(self, params, m, v, m_scale=None, v_scale=None, copies=None):
         n = len(params)
@@ -241,6 +241,7 @@ class AdamW:
         self._shapes = [p.shape for p in params]
         self._device = params[0].device if n else None
         self._devices = [p.get_device() for p in params]
+        spans = []                                         # what a step writes: addresses and bytes
         for i, (t, p) in enumerate(zip(self._list, params)):
             kind = _type_of(p, f"params[{i}]")
             eight = m[i].dtype == torch.float8_e4m3fn
@@ -258,6 +259,16 @@ class AdamW:
                 t.m_scale, t.v_scale = m_scale[i].data_ptr(), v_scale[i].data_ptr()
             if copies is not None:
                 t.copy, t.copy_type = copies[i].data_ptr(), _TYPES[copies[i].dtype]
+            count = t.count
+            if count:
+                spans += [(t.param, count * (4 if kind == F32 else 2)), (t.m, count * (1 if eight else 4)), (t.v, count * (1 if eight else 4))]
+                if eight:
+                    spans += [(t.m_scale, 4 * -(-count // BLOCK)), (t.v_scale, 4 * -(-count // BLOCK))]
+                if copies is not None:
+                    spans.append((t.copy, 2 * count))
+        spans.sort()
+        if any(start + size > after for (start, size), (after, _) in zip(spans, spans[1:])):
+            raise ValueError("AdamW: tensors that overlap (each may be in the lists once)")
         self._grad_types = None
 
     def step(self, grads, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, seed=0):

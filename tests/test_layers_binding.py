@@ -109,3 +109,21 @@ def test_autograd_notices_weights_that_a_step_changed(library):
     for saved in (loss, rounded):
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             saved.backward()
+
+
+def test_tensors_of_a_plan_that_overlap_are_refused(library):
+    # (two work-groups would update the shared values at once)
+    whole, other = torch.ones(600), torch.ones(300)
+    m, v, _, _ = layers.adamw_state([whole, other])
+    for params in ([whole, whole], [whole[:300], whole[299:599]]):
+        state = layers.adamw_state(params)[:2]
+        with pytest.raises(ValueError, match="overlap"):
+            layers.AdamW(params, *state)
+    with pytest.raises(ValueError, match="overlap"):
+        layers.AdamW([other, torch.ones(300)], [m[1], torch.zeros(300)], [v[1], m[1]])
+    half = whole[:300].bfloat16()
+    with pytest.raises(ValueError, match="overlap"):
+        layers.AdamW([other, whole[300:]], *layers.adamw_state([other, other])[:2], copies=[half, half])
+    layers.AdamW([whole[:300], whole[300:], torch.ones(0), torch.ones(0)], *layers.adamw_state([other, other, whole[:0], whole[:0]])[:2])
+    # (scales that float moments do not use are nobody's)
+    layers.AdamW([whole[:300], whole[300:]], *layers.adamw_state([other, other])[:2], m_scale=[other, other], v_scale=[other, other])
