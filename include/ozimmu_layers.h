@@ -59,7 +59,7 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
 
 /*
  * Gradients of ozimmu_linear.  With dz = dy * act'(pre), rounded to `type` for the products (one rounding, to the
- * type the matrix cores take; the bias gradient is summed from the unrounded values):
+ * type the matrix cores take; a float16 dz beyond 65504 becomes an infinity; the bias gradient is summed from the unrounded values):
  *   dx = dz w   [tokens, n_in],   dw = dz^T x   [n_out, n_in],   db = the sum of dz over the tokens   [n_out]
  * (the gradient of the residual is dy itself).  dx, dw and db may each be NULL and are then not formed; pre may be NULL for
  * OZIMMU_ACT_NONE; x may be NULL without dw, w without dx.  act'(0) = 0 for OZIMMU_ACT_RELU.
@@ -84,7 +84,8 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
  *     the others of the block stay what they are.  Where a block's
  *     largest magnitude is below 2^-100, m is held as zeros and sqrt(v) > 0 as the smallest code.
  *   copy, may be NULL: receives p in 16 bits (copy_type BF16 or F16), the weights of the next forward pass.
- * Tensors are arrays of `count` contiguous values at any alignment of their type; they must not overlap.
+ * Tensors are arrays of `count` contiguous values at any alignment of their type; they must not overlap.  A launch takes up to 48
+ * tensors of the same types that stand behind one another in the list.
  */
 typedef struct {
     void *param;

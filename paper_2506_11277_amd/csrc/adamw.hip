@@ -17,7 +17,7 @@
 // What the states keep is rounded as written, operation by operation (no fused multiply-add, a rounded root), so that the same step
 // gives the same codes whatever the compiler makes of it; the parameter's quotient is the instruction's reciprocal, a unit
 // off in a step a thousandth of p.
-// Measured: 143 million values, bf16 with 8 bits, 1.44 GB: 290 us; 57 million, float with a bf16 copy, 1.58 GB: 305 us (a copy
+// Measured: 143 million values, bf16 with 8 bits, 1.44 GB: 300 us; 57 million, float with a bf16 copy, 1.58 GB: 312 us (a copy
 // at 5.1 TB/s: 282 and 310).  The first in four values a lane, with the library's root and division: 355 us, bound by arithmetic.
 #include "layers.h"
 
