@@ -1,6 +1,7 @@
 /*
  * ozimmu layers -- the feed-forward layer of a language model on MI355X (gfx950): a linear layer with its epilogue, its
- * gradients, the AdamW step that uses them, and a mixture-of-experts layer for the few tokens of a serving step.
+ * gradients, the AdamW step that uses them, a mixture-of-experts layer for the few tokens of a serving step, the norm in front
+ * of these layers, and rows in 8 bits.
  *
  * Conventions, those of ozimmu.h where they apply
  *   - Matrices hold one token, or one output feature of a weight, per row; the entries of a row are contiguous and rows
@@ -119,6 +120,44 @@ size_t ozimmu_moe_workspace_bytes(int tokens, int width, int hidden, int experts
 int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int type, int normalise, const void *x, int ldx,
                const void *router, const void *w_in, const void *w_out, int32_t *chosen, float *gates, void *y, int ldy,
                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows in 8 bits: `codes` [rows, cols], whole numbers from -127 to 127 in rows `ldc` apart (any alignment), stand with one float
+ * `scale` for each row for code * scale.  Of a row's values t, in 32 bits, with a = the largest |t|:
+ *   code = t (127 / a) rounded to nearest, ties to even, the quotient and the product rounded to 32 bits;   scale = a / 127.
+ * Where a < 2^-100 the codes and the scale are 0.  A row with a value that is not finite has codes of 0 and a scale of NaN.
+ */
+
+/*
+ * x [rows, cols] of `type` (BF16, F16, F32) in 8 bits: activations (a scale for each token), weights (a scale for each output
+ * feature), values that a forward pass keeps for the gradients.
+ */
+int ozimmu_quantise(int rows, int cols, int type, const void *x, int ldx, int8_t *codes, int ldc, float *scale, void *stream);
+
+/*
+ * Root-mean-square norm of each token, with the residual's addition:
+ *   h = x + residual,   y = h r weight,   r = 1 / sqrt(mean of h^2 + eps)
+ *   x, residual, total and y [tokens, width], weight [width], all of `type`; residual and weight may be NULL (zeros, ones).
+ * Each of these may be NULL and is then not formed: total receives h; y the norm of the unrounded h; codes [tokens, width] and scale [tokens] the norm
+ * in 8 bits, with t = h weight for the codes (r, which is common to the row, goes into the scale: a r / 127).
+ * total may be x or residual itself (same pointer and ld).  0 < eps < infinity, as a float.  Where the squares of h leave the range of 32
+ * bits the row is taken times 2^-80, so that every finite row has its norm.
+ */
+int ozimmu_rms_norm(int tokens, int width, int type, const void *x, int ldx, const void *residual, int ldr, const void *weight,
+                    double eps, void *total, int ldt, void *y, int ldy, int8_t *codes, int ldc, float *scale, void *stream);
+
+/*
+ * Gradients of ozimmu_rms_norm from dy, that of y (of the values that codes and scale stand for, the rounding taken as the
+ * identity), and h [tokens, width], its `total`, or x where it had no residual.  With g = dy weight and n = h r:
+ *   dx = r (g - n mean(g n)) + add   [tokens, width],   dw = the sum of dy n over the tokens   [width]
+ * dx is the gradient of x and of the residual alike; add [tokens, width], may be NULL, is the gradient that reaches `total` from elsewhere.
+ * dx and dw may each be NULL.  dx may be dy, h or add itself (same pointer and ld).
+ * Workspace (for dw; NULL is accepted without it): ozimmu_rms_norm_grad_workspace_bytes.
+ */
+size_t ozimmu_rms_norm_grad_workspace_bytes(int tokens, int width);
+int ozimmu_rms_norm_grad(int tokens, int width, int type, const void *dy, int lddy, const void *h, int ldh, const void *weight,
+                         double eps, const void *add, int ldadd, void *dx, int lddx, void *dw, void *workspace,
+                         size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

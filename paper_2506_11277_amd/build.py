@@ -8,13 +8,13 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libozimmu.so")
 SOURCES = ["api.hip", "reduce.hip", "split.hip", "gemm.hip", "gemm_fused16.hip", "gemm_banded.hip", "gemm_small.hip", "gemm_vectors.hip",
            "gemm_halves16.hip", "gemm_passes.hip", "gemm_passes_4.hip", "gemm_passes_10.hip", "gemm_passes_13.hip", "gemm_passes_15.hip", "gemm_passes_17.hip", "gemm_passes_19.hip", "ceiling.hip",
-           "layers_api.hip", "product_bf16.hip", "product_f16.hip", "product_f32.hip", "pad.hip", "grad.hip", "adamw.hip", "moe.hip"]
+           "layers_api.hip", "product_bf16.hip", "product_f16.hip", "product_f32.hip", "pad.hip", "grad.hip", "adamw.hip", "moe.hip", "norm.hip", "norm_grad.hip"]
 HEADERS = [os.path.join(CSRC, "oz_common.h"), os.path.join(CSRC, "gemm_dev.h"), os.path.join(CSRC, "gemm_passes_dev.h"), os.path.join(CSRC, "slice_dev.h"), os.path.join(HERE, "..", "include", "ozimmu.h"),
            os.path.join(HERE, "..", "include", "ozimmu_bench.h")]
 # what only the feed-forward operators' sources include
 LAYER_SOURCES = SOURCES[SOURCES.index("layers_api.hip"):]
 LAYER_HEADERS = [os.path.join(CSRC, "layers.h"), os.path.join(CSRC, "layers_dev.h"), os.path.join(CSRC, "product_dev.h"),
-                 os.path.join(CSRC, "stream_dev.h"), os.path.join(CSRC, "few_dev.h"),
+                 os.path.join(CSRC, "stream_dev.h"), os.path.join(CSRC, "few_dev.h"), os.path.join(CSRC, "norm_dev.h"),
                  os.path.join(HERE, "..", "include", "ozimmu_layers.h")]
 
 HIPCC_FLAGS = [

@@ -73,4 +73,46 @@ inline int moe_out_parts(int tokens, int width, int hidden, int experts, int top
 }
 hipError_t launch_moe(const MoeArgs &a, int type, hipStream_t st);
 
+// the root-mean-square norm of rows, and rows to 8 bits (norm.hip)
+struct NormArgs {
+    const void *x, *residual, *weight;     // residual and weight may be null
+    void *total, *y;                       // either may be null
+    int8_t *codes;                         // null: no rows in 8 bits
+    float *scale;                          // null: nor scales
+    int ldx, ldr, ldt, ldy, ldc, rows, width;
+    float eps;
+    int norm;                              // 0: to 8 bits as they are
+};
+hipError_t launch_norm(const NormArgs &a, int type, hipStream_t st);
+
+// its gradients (norm_grad.hip)
+struct NormGradArgs {
+    const void *dy, *h, *weight, *add;     // weight and add may be null
+    void *dx, *dw;                         // either may be null
+    float *sums;                           // [parts][width], null without dw
+    float *factors;                        // [rows][2] where the rows are not kept in registers and there is a dw, else null
+    int lddy, ldh, ldadd, lddx, rows, width;
+    float eps;
+};
+// Parts of the rows whose sums of dw are formed apart, and how: rows in registers, dw beside them, or in a pass by columns, `group` rows a part.
+struct NormGradPlan {
+    bool in_registers;
+    int parts, group;
+};
+inline NormGradPlan plan_norm_grad(int rows, int width)
+{
+    constexpr int kMostParts = 1024;
+    NormGradPlan p{width <= 16384, 0, 64};
+    if (p.in_registers) {
+        const int each = width <= 1024 ? 4 : 1, groups = (int)((rows + each - 1LL) / each);
+        p.parts = groups < kMostParts ? groups : kMostParts;
+    } else {
+        const int least = (int)((rows + kMostParts - 1LL) / kMostParts);
+        if (least > p.group) p.group = least;
+        p.parts = (int)((rows + p.group - 1LL) / p.group);
+    }
+    return p;
+}
+hipError_t launch_norm_grad(const NormGradArgs &a, int type, hipStream_t st);
+
 }  // namespace oz

@@ -403,3 +403,76 @@ int ozimmu_moe(int tokens, int width, int hidden, int experts, int top_k, int ty
 }
 
 }  // extern "C"
+
+namespace {
+inline bool bad_eps(double eps) { return !((float)eps > 0.0f) || !((float)eps <= 3.402823466e38f); }
+
+// parts of the workspace of ozimmu_rms_norm_grad
+struct NormGradWorkspace {
+    size_t factors, total;
+};
+NormGradWorkspace norm_grad_workspace(int tokens, int width)
+{
+    const NormGradPlan p = plan_norm_grad(tokens, width);
+    NormGradWorkspace w{};
+    w.factors = padded((size_t)p.parts * width * 4);
+    w.total = w.factors + (p.in_registers ? 0 : padded((size_t)tokens * 8));
+    return w;
+}
+}  // namespace
+
+extern "C" {
+
+int ozimmu_rms_norm(int tokens, int width, int type, const void *x, int ldx, const void *residual, int ldr, const void *weight, double eps,
+                    void *total, int ldt, void *y, int ldy, int8_t *codes, int ldc, float *scale, void *stream)
+{
+    if (bad_type(type) || bad_sizes(tokens, width, 0) || bad_eps(eps)) return OZIMMU_BAD_ARG;
+    const size_t size = element_bytes(type);
+    if (bad_rows(tokens, width, x, ldx, size) || (residual && bad_rows(tokens, width, residual, ldr, size)) || (uintptr_t)weight % size ||
+        (total && bad_rows(tokens, width, total, ldt, size)) || (y && bad_rows(tokens, width, y, ldy, size)) ||
+        (codes && bad_rows(tokens, width, codes, ldc, 1)) || (codes && tokens > 0 && !scale) || (scale && !codes && tokens > 0 && width > 0) || (uintptr_t)scale % 4)
+        return OZIMMU_BAD_ARG;
+    if (!total && !y && !scale) return OZIMMU_OK;
+    const NormArgs a{x, residual, weight, total, y, codes, scale, ldx, ldr, ldt, ldy, ldc, tokens, width, (float)eps, 1};
+    return launch_norm(a, type, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+}
+
+int ozimmu_quantise(int rows, int cols, int type, const void *x, int ldx, int8_t *codes, int ldc, float *scale, void *stream)
+{
+    if (bad_type(type) || bad_sizes(rows, cols, 0)) return OZIMMU_BAD_ARG;
+    if (bad_rows(rows, cols, x, ldx, element_bytes(type)) || bad_rows(rows, cols, codes, ldc, 1) || (rows > 0 && !scale) || (uintptr_t)scale % 4) return OZIMMU_BAD_ARG;
+    NormArgs a{};
+    a.x = x;
+    a.ldx = ldx;
+    a.codes = codes;
+    a.ldc = ldc;
+    a.scale = scale;
+    a.rows = rows;
+    a.width = cols;
+    return launch_norm(a, type, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+}
+
+size_t ozimmu_rms_norm_grad_workspace_bytes(int tokens, int width)
+{
+    return bad_sizes(tokens, width, 0) ? 0 : norm_grad_workspace(tokens, width).total;
+}
+
+int ozimmu_rms_norm_grad(int tokens, int width, int type, const void *dy, int lddy, const void *h, int ldh, const void *weight, double eps,
+                         const void *add, int ldadd, void *dx, int lddx, void *dw, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (bad_type(type) || bad_sizes(tokens, width, 0) || bad_eps(eps)) return OZIMMU_BAD_ARG;
+    const size_t size = element_bytes(type);
+    if (bad_rows(tokens, width, dy, lddy, size) || bad_rows(tokens, width, h, ldh, size) || (uintptr_t)weight % size ||
+        (add && bad_rows(tokens, width, add, ldadd, size)) || (dx && bad_rows(tokens, width, dx, lddx, size)) || (uintptr_t)dw % size)
+        return OZIMMU_BAD_ARG;
+    const NormGradWorkspace ws = norm_grad_workspace(tokens, width);
+    if (dw && bad_workspace(workspace, workspace_bytes, ws.total)) return OZIMMU_BAD_ARG;
+    if (width == 0 || (!dx && !dw)) return OZIMMU_OK;
+    char *const base = (char *)workspace;
+    const bool factors = dw && !plan_norm_grad(tokens, width).in_registers;
+    const NormGradArgs a{dy, h, weight, add, dx, dw, dw ? (float *)base : nullptr, factors ? (float *)(base + ws.factors) : nullptr,
+                         lddy, ldh, ldadd, lddx, tokens, width, (float)eps};
+    return launch_norm_grad(a, type, (hipStream_t)stream) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+}
+
+}  // extern "C"

@@ -1,0 +1,205 @@
+// Root-mean-square norm of rows, with the residual's addition in front of it and its results in 8 bits behind it:
+//   h = x + residual,   y = h r w,   r = 1 / sqrt(mean of h^2 + eps),
+// and rows to 8 bits by themselves.  A row's factor r only scales it, so its codes are those of t = h w, and r goes into the scale.
+//
+// Bound by memory: every value is read once, into registers, and written once.  A row is a wavefront's (no barriers) or
+// a work-group's, C groups of 8 values a thread; rows beyond the largest of these are read twice, in a loop.
+// h^2 that leaves the range: h 2^-80 and r 2^80 take their places (a product with a power of two is exact).
+#include "norm_dev.h"
+
+namespace oz {
+namespace {
+
+template <class T, int L, int C>
+__global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
+{
+    constexpr int ROWS = L < 256 ? 256 / L : 1;
+    __shared__ SumAndTop slots[2][L / 64];
+    const int t = L < 256 ? threadIdx.x & (L - 1) : threadIdx.x;
+    const long long row = ((long long)blockIdx.y * kGridRow + blockIdx.x) * ROWS + (L < 256 ? threadIdx.x / L : 0);
+    if (row >= a.rows) return;
+    const T *x = (const T *)a.x + (size_t)row * a.ldx, *res = a.residual ? (const T *)a.residual + (size_t)row * a.ldr : nullptr;
+    const T *w = (const T *)a.weight;
+
+    // (all loads before the first store, which may be to the residual's place)
+    Eight<T> rx[C], rr[C], rw[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * L + t) * 8;
+        rx[c].load(x + at, a.width - at);
+    }
+    if (res)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * L + t) * 8;
+            rr[c].load(res + at, a.width - at);
+        }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * L + t) * 8;
+        if (w) rw[c].load(w + at, a.width - at);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rw[c].v[i] = (T)1.0f;
+    }
+    float h[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[c][i] = rx[c][i];
+    if (res)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[c][i] += rr[c][i];
+    if (a.total)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * L + t) * 8;
+            store8((T *)a.total + (size_t)row * a.ldt + at, a.width - at, h[c]);
+        }
+
+    auto statistics = [&](SumAndTop *to) __attribute__((always_inline)) {
+        float sum = 0.0f;
+        unsigned top = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sum = __builtin_fmaf(h[c][i], h[c][i], sum);
+                const unsigned m = magnitude(h[c][i] * rw[c][i]);
+                top = m > top ? m : top;
+            }
+        return over_row<L>(sum, top, to);
+    };
+    SumAndTop s = statistics(slots[0]);
+    float r = 1.0f;
+    if (a.norm) {
+        r = inverse_root(s.sum, a.width, a.eps);
+        if (__builtin_expect(!(s.sum < __uint_as_float(kInfinity)), 0)) {       // (the same for the whole row)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[c][i] *= kSmaller;
+            s = statistics(slots[1]);
+            r = inverse_root(s.sum, a.width, 0.0f);
+        }
+    }
+    const RowScale scale = row_scale(s.top);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * L + t) * 8;
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = h[c][i] * rw[c][i];
+        if (a.codes) store_codes(a.codes + (size_t)row * a.ldc + at, a.width - at, p, scale);
+        if (a.y) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] *= r;
+            store8((T *)a.y + (size_t)row * a.ldy + at, a.width - at, p);
+        }
+    }
+    if (a.scale && t == 0) a.scale[row] = scale.scale == 0.0f ? 0.0f : scale.scale * r;         // (no values: r is no number)
+}
+
+// ... of any width, its values read twice: once for the statistics and once for the results.
+// (Where the sum of the squares leaves the range they are read three times.)
+template <class T>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
+{
+    constexpr int L = 1024;
+    __shared__ SumAndTop slots[2][L / 64];
+    const long long row = (long long)blockIdx.y * kGridRow + blockIdx.x;
+    if (row >= a.rows) return;
+    const T *x = (const T *)a.x + (size_t)row * a.ldx, *res = a.residual ? (const T *)a.residual + (size_t)row * a.ldr : nullptr;
+    const T *w = (const T *)a.weight;
+    auto values = [&](int at, float (&h)[8], Eight<T> &rw) __attribute__((always_inline)) {
+        Eight<T> rx, rr;
+        rx.load(x + at, a.width - at);
+        if (res) rr.load(res + at, a.width - at);
+        if (w) rw.load(w + at, a.width - at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] = res ? rx[i] + rr[i] : rx[i];
+            if (!w) rw.v[i] = (T)1.0f;
+        }
+    };
+    auto statistics = [&](SumAndTop *to, float factor) __attribute__((always_inline)) {
+        float sum = 0.0f;
+        unsigned top = 0;
+        for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
+            float h[8];
+            Eight<T> rw;
+            values(at, h, rw);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = h[i] * factor;
+                sum = __builtin_fmaf(v, v, sum);
+                const unsigned m = magnitude(v * rw[i]);
+                top = m > top ? m : top;
+            }
+        }
+        return over_row<L>(sum, top, to);
+    };
+    SumAndTop s = statistics(slots[0], 1.0f);
+    float r = 1.0f, factor = 1.0f;
+    if (a.norm) {
+        r = inverse_root(s.sum, a.width, a.eps);
+        if (!(s.sum < __uint_as_float(kInfinity))) {
+            factor = kSmaller;
+            s = statistics(slots[1], factor);
+            r = inverse_root(s.sum, a.width, 0.0f);
+        }
+    }
+    const RowScale scale = row_scale(s.top);
+    for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
+        float h[8];
+        Eight<T> rw;
+        values(at, h, rw);                                      // (this thread's values: what total replaces, it has read)
+        if (a.total) store8((T *)a.total + (size_t)row * a.ldt + at, a.width - at, h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = h[i] * factor;
+            h[i] = v * rw[i];
+        }
+        if (a.codes) store_codes(a.codes + (size_t)row * a.ldc + at, a.width - at, h, scale);
+        if (a.y) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] *= r;
+            store8((T *)a.y + (size_t)row * a.ldy + at, a.width - at, h);
+        }
+    }
+    if (a.scale && threadIdx.x == 0) a.scale[row] = scale.scale == 0.0f ? 0.0f : scale.scale * r;
+}
+
+template <class T, int L, int C>
+hipError_t launch_rows(const NormArgs &a, hipStream_t st)
+{
+    constexpr int ROWS = L < 256 ? 256 / L : 1;
+    const long long groups = ((long long)a.rows + ROWS - 1) / ROWS;
+    norm_kernel<T, L, C><<<dim3(grid_row(groups), grid_rows(groups)), L < 256 ? 256 : L, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch(const NormArgs &a, hipStream_t st)
+{
+    if (a.rows == 0) return hipSuccess;
+    if (a.width <= 512) return launch_rows<T, 64, 1>(a, st);
+    if (a.width <= 1024) return launch_rows<T, 64, 2>(a, st);
+    if (a.width <= 2048) return launch_rows<T, 256, 1>(a, st);
+    if (a.width <= 4096) return launch_rows<T, 256, 2>(a, st);
+    if (a.width <= 8192) return launch_rows<T, 256, 4>(a, st);
+    if (a.width <= 16384) return launch_rows<T, 1024, 2>(a, st);
+    norm_long_kernel<T><<<dim3(grid_row(a.rows), grid_rows(a.rows)), 1024, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs &a, int type, hipStream_t st)
+{
+    return type == OZIMMU_BF16 ? launch<bf16>(a, st) : type == OZIMMU_F16 ? launch<f16>(a, st) : launch<float>(a, st);
+}
+
+}  // namespace oz

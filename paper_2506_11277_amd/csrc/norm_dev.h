@@ -1,0 +1,133 @@
+// What the kernels over whole rows share (norm.hip): a row in registers, sums and maxima over it, rows in 8 bits.
+#pragma once
+#include "layers.h"
+
+namespace oz {
+
+// eight elements, at any alignment of their type; `n` of them there (the others 0)
+template <class T>
+struct Eight {
+    typedef T V __attribute__((ext_vector_type(8)));
+    V v;
+    __device__ __forceinline__ void load(const T *p, int n)
+    {
+        if (n >= 8) {
+            __builtin_memcpy(&v, p, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0.0f;
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+};
+
+template <class T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&x)[8])
+{
+    typename Eight<T>::V v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
+    if (n >= 8) {
+        __builtin_memcpy(p, &v, sizeof v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+
+// f over the 64 lanes' values of a wavefront, the same in each: among 16 by exchanges inside the vector unit
+template <class X, class F>
+__device__ __forceinline__ X over_lanes(X x, F f)
+{
+    auto with = [&](unsigned o) { x = f(x, __builtin_bit_cast(X, o)); };
+    with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(unsigned, x), 0xb1, 0xf, 0xf, true));      // lane ^ 1
+    with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(unsigned, x), 0x4e, 0xf, 0xf, true));      // lane ^ 2
+    with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(unsigned, x), 0x141, 0xf, 0xf, true));     // 7 - lane within 8
+    with(__builtin_amdgcn_mov_dpp(__builtin_bit_cast(unsigned, x), 0x140, 0xf, 0xf, true));     // 15 - lane within 16
+    with(__builtin_amdgcn_ds_swizzle(__builtin_bit_cast(unsigned, x), 0x401f));                 // lane ^ 16
+    with(__shfl_xor(__builtin_bit_cast(unsigned, x), 32));
+    return x;
+}
+__device__ __forceinline__ float lanes_sum(float x) { return over_lanes(x, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ unsigned lanes_top(unsigned x) { return over_lanes(x, [](unsigned a, unsigned b) { return a > b ? a : b; }); }
+
+// two sums, or a sum and a maximum, over a row's L threads; `slots`: L / 64 pairs of LDS of this use alone
+struct SumAndTop {
+    float sum;
+    unsigned top;
+};
+template <int L>
+__device__ __forceinline__ SumAndTop over_row(float sum, unsigned top, SumAndTop *slots)
+{
+    sum = lanes_sum(sum);
+    top = lanes_top(top);
+    if constexpr (L > 64) {
+        if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = SumAndTop{sum, top};
+        __syncthreads();
+        sum = 0.0f;
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < L / 64; ++w) {
+            const SumAndTop s = slots[w];
+            sum += s.sum;
+            top = s.top > top ? s.top : top;
+        }
+    }
+    return SumAndTop{sum, top};
+}
+
+// Bits of |x|: ordered as the magnitudes are, infinities and then NaN above all numbers.
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+constexpr unsigned kInfinity = 0x7f800000u;
+
+// A row in 8 bits: code = t (127 / top) rounded to nearest, ties to even, |code| <= 127; scale = top / 127.  127 / top and the product
+// with it are rounded in 32 bits, so that the codes follow from t bit by bit.  Rows whose largest magnitude is below 2^-100
+// (127 / top might leave the range) are held as zeros; one with a value that is not finite has no scale: NaN.
+struct RowScale {
+    float inverse, scale;
+};
+__device__ __forceinline__ RowScale row_scale(unsigned top)
+{
+    const float t = __uint_as_float(top);
+    if (top >= kInfinity) return RowScale{0.0f, __uint_as_float(0x7fc00000u)};
+    if (t < 0x1p-100f) return RowScale{0.0f, 0.0f};
+    return RowScale{127.0f / t, t * (1.0f / 127.0f)};
+}
+
+// |x| < 2^22 rounded to the nearest whole number, in the low bits of a float's 32
+__device__ __forceinline__ unsigned whole_bits(float x) { return __float_as_uint(x + 12582912.0f); }
+
+__device__ __forceinline__ void store_codes(int8_t *p, int n, const float (&t)[8], const RowScale &s)
+{
+    unsigned b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float q = t[i] * s.inverse;                             // (rounded by itself: no fused multiply-add)
+        asm("" : "+v"(q));
+        b[i] = whole_bits(q);
+    }
+    if (s.inverse == 0.0f)                                      // (values that are not finite among them)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = 0;
+    v2u c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        c[i] = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u) | __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x04000c0cu);
+    if (n >= 8) {
+        __builtin_memcpy(p, &c, 8);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (int8_t)(c[i / 4] >> (8 * (i & 3)));
+    }
+}
+
+// 1 / sqrt(mean of h^2 + eps), from the sum of the squares of h 2^-shift
+constexpr float kSmaller = 0x1p-80f;
+__device__ __forceinline__ float inverse_root(float squares, int width, float eps)
+{
+    return 1.0f / sqrtf(squares / (float)width + eps);
+}
+
+}  // namespace oz

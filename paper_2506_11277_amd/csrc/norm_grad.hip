@@ -1,0 +1,291 @@
+// Gradients of the root-mean-square norm y = h r w, r = 1 / sqrt(mean of h^2 + eps): with g = dy w and n = h r
+//   dx = r (g - n mean(g n)) + add,   dw = the sum of dy n over the tokens.
+//
+// Bound by memory: a work-group takes one row after the other, its values in registers, so that they are read once; the
+// sums of dw stay in registers from row to row, and leave them as one row of partial sums for each work-group, which a
+// second kernel adds up, always in the same order.  Rows beyond what registers hold are read twice, and dw is summed
+// by columns in a pass of its own.
+#include "norm_dev.h"
+
+namespace oz {
+namespace {
+
+struct TwoSums {
+    float a, b;
+};
+template <int L>
+__device__ __forceinline__ TwoSums sums_over_row(float a, float b, TwoSums *slots)
+{
+    a = lanes_sum(a);
+    b = lanes_sum(b);
+    if constexpr (L > 64) {
+        if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = TwoSums{a, b};
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int w = 0; w < L / 64; ++w) {
+            const TwoSums s = slots[w];
+            a += s.a;
+            b += s.b;
+        }
+    }
+    return TwoSums{a, b};
+}
+
+// what a row's gradients need of it: r, and mean(g n) r; of h 2^-80 where `factor` is 2^-80
+struct RowGrad {
+    float r, mean, factor;
+};
+__device__ __forceinline__ RowGrad row_grad(const TwoSums &s, int width, float eps, float factor)
+{
+    const float r = inverse_root(s.a, width, factor == 1.0f ? eps : 0.0f);
+    return RowGrad{r, s.b * r / (float)width, factor};
+}
+// (r of h itself is r factor; g and n are of ordinary size, whatever h is)
+__device__ __forceinline__ float input_grad(const RowGrad &s, float h, float g)
+{
+    const float n = h * s.factor * s.r;
+    return (g - n * s.mean) * (s.r * s.factor);
+}
+
+template <class T, int L, int C>
+__global__ __launch_bounds__(L < 256 ? 256 : L) void norm_grad_kernel(NormGradArgs a)
+{
+    constexpr int ROWS = L < 256 ? 256 / L : 1;
+    __shared__ TwoSums slots[3][L / 64];
+    __shared__ float part[L < 256 ? 256 * 8 : 1];
+    const int t = L < 256 ? threadIdx.x & (L - 1) : threadIdx.x, which = L < 256 ? threadIdx.x / L : 0;
+    float dw[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0.0f;
+    Eight<T> rw[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * L + t) * 8;
+        if (a.weight) rw[c].load((const T *)a.weight + at, a.width - at);
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) rw[c].v[i] = (T)1.0f;
+    }
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * ROWS + which; row < a.rows; row += (long long)gridDim.x * ROWS, turn ^= 1) {
+        Eight<T> rh[C], rd[C], ra[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * L + t) * 8;
+            rh[c].load((const T *)a.h + (size_t)row * a.ldh + at, a.width - at);
+            rd[c].load((const T *)a.dy + (size_t)row * a.lddy + at, a.width - at);
+            if (a.add) ra[c].load((const T *)a.add + (size_t)row * a.ldadd + at, a.width - at);
+        }
+        auto statistics = [&](float factor, TwoSums *to) __attribute__((always_inline)) {
+            float squares = 0.0f, products = 0.0f;
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float h = rh[c][i] * factor;
+                    squares = __builtin_fmaf(h, h, squares);
+                    products = __builtin_fmaf(rd[c][i] * rw[c][i], h, products);
+                }
+            return sums_over_row<L>(squares, products, to);
+        };
+        // (two sets of slots in turn: a row's are read before anyone is behind the next row's barrier)
+        RowGrad s;
+        const TwoSums first = statistics(1.0f, slots[turn]);
+        if (__builtin_expect(first.a < __uint_as_float(kInfinity), 1)) {
+            s = row_grad(first, a.width, a.eps, 1.0f);
+        } else {
+            if constexpr (L > 64) __syncthreads();
+            s = row_grad(statistics(kSmaller, slots[2]), a.width, a.eps, kSmaller);
+            if constexpr (L > 64) __syncthreads();
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int at = (c * L + t) * 8;
+            float dx[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = rd[c][i], h = rh[c][i];
+                dx[i] = input_grad(s, h, d * rw[c][i]);
+                if (a.add) dx[i] += ra[c][i];
+                dw[c][i] = __builtin_fmaf(d, h * s.factor * s.r, dw[c][i]);
+            }
+            if (a.dx) store8((T *)a.dx + (size_t)row * a.lddx + at, a.width - at, dx);
+        }
+    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int at = (c * L + t) * 8;
+        if constexpr (L < 256) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[(which * L + t) * 8 + i] = dw[c][i];
+            __syncthreads();
+            if (which == 0)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int q = 1; q < ROWS; ++q) dw[c][i] += part[(q * L + t) * 8 + i];
+        }
+        if (which == 0) store8(a.sums + (size_t)blockIdx.x * a.width + at, a.width - at, dw[c]);
+    }
+}
+
+// Rows of any width: dx, and for the sums by columns r and the factor that h is taken with.
+template <class T>
+__global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a)
+{
+    constexpr int L = 1024;
+    __shared__ TwoSums slots[2][L / 64];
+    const long long row = (long long)blockIdx.y * kGridRow + blockIdx.x;
+    if (row >= a.rows) return;
+    const T *hs = (const T *)a.h + (size_t)row * a.ldh, *ds = (const T *)a.dy + (size_t)row * a.lddy, *w = (const T *)a.weight;
+    const T *add = a.add ? (const T *)a.add + (size_t)row * a.ldadd : nullptr;
+    auto values = [&](int at, float (&h)[8], float (&g)[8]) __attribute__((always_inline)) {
+        Eight<T> rh, rd, rw;
+        rh.load(hs + at, a.width - at);
+        rd.load(ds + at, a.width - at);
+        if (w) rw.load(w + at, a.width - at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] = rh[i];
+            g[i] = w ? rd[i] * rw[i] : rd[i];
+        }
+    };
+    auto statistics = [&](float factor, TwoSums *to) __attribute__((always_inline)) {
+        float squares = 0.0f, products = 0.0f;
+        for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
+            float h[8], g[8];
+            values(at, h, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = h[i] * factor;
+                squares = __builtin_fmaf(v, v, squares);
+                products = __builtin_fmaf(g[i], v, products);
+            }
+        }
+        return sums_over_row<L>(squares, products, to);
+    };
+    RowGrad s;
+    const TwoSums first = statistics(1.0f, slots[0]);
+    if (first.a < __uint_as_float(kInfinity)) s = row_grad(first, a.width, a.eps, 1.0f);
+    else s = row_grad(statistics(kSmaller, slots[1]), a.width, a.eps, kSmaller);
+    if (a.dx)
+        for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
+            float h[8], g[8];
+            values(at, h, g);
+            Eight<T> ra;
+            if (add) ra.load(add + at, a.width - at);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[i] = input_grad(s, h[i], g[i]);
+                if (add) h[i] += ra[i];
+            }
+            store8((T *)a.dx + (size_t)row * a.lddx + at, a.width - at, h);
+        }
+    if (a.factors && threadIdx.x == 0) ((float2 *)a.factors)[row] = float2{s.r, s.factor};
+}
+
+// the sums of dw over `group` tokens, 512 columns a work-group
+template <class T>
+__global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormGradArgs a, int group)
+{
+    __shared__ float part[4][512];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 512 + lane * 8;
+    const long long first = (long long)blockIdx.y * group, last = first + group < a.rows ? first + group : a.rows;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (c < a.width)
+        for (long long row = first + wave; row < last; row += 4) {
+            Eight<T> rh, rd;
+            rh.load((const T *)a.h + (size_t)row * a.ldh + c, a.width - c);
+            rd.load((const T *)a.dy + (size_t)row * a.lddy + c, a.width - c);
+            const float2 f = ((const float2 *)a.factors)[row];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(rd[i], rh[i] * f.y * f.x, sum[i]);
+        }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[wave][lane * 8 + i] = sum[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += 256) {
+        const long long col = (long long)blockIdx.x * 512 + i;
+        if (col < a.width) a.sums[(size_t)blockIdx.y * a.width + col] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+    }
+}
+
+// dw: the partial sums' rows, 64 columns a work-group, its wavefronts every sixteenth row
+template <class T>
+__global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float *sums, T *dw, int rows, int width)
+{
+    __shared__ float part[16][64];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const long long c = ((long long)blockIdx.y * kGridRow + blockIdx.x) * 64 + lane;
+    float s = 0.0f;
+    if (c < width)
+#pragma unroll 8
+        for (int r = wave; r < rows; r += 16) s += sums[(size_t)r * width + c];
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < width) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) s += part[w][lane];
+        dw[c] = (T)s;
+    }
+}
+
+template <class T, int L, int C>
+hipError_t launch_rows(const NormGradArgs &a, int groups, hipStream_t st)
+{
+    norm_grad_kernel<T, L, C><<<groups, L < 256 ? 256 : L, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch(const NormGradArgs &a, hipStream_t st)
+{
+    const NormGradPlan plan = plan_norm_grad(a.rows, a.width);
+    hipError_t e = hipSuccess;
+    if (a.rows > 0 && (a.dx || a.sums)) {
+        if (plan.in_registers) {
+            e = a.width <= 512    ? launch_rows<T, 64, 1>(a, plan.parts, st)
+                : a.width <= 1024 ? launch_rows<T, 64, 2>(a, plan.parts, st)
+                : a.width <= 2048 ? launch_rows<T, 256, 1>(a, plan.parts, st)
+                : a.width <= 4096 ? launch_rows<T, 256, 2>(a, plan.parts, st)
+                : a.width <= 8192 ? launch_rows<T, 256, 4>(a, plan.parts, st)
+                                  : launch_rows<T, 1024, 2>(a, plan.parts, st);
+        } else {
+            // (where dx takes the place of what the columns are summed from, it is formed behind them)
+            const dim3 grid(grid_row(a.rows), grid_rows(a.rows));
+            const bool behind = a.sums && a.dx && (a.dx == a.dy || a.dx == a.h);
+            NormGradArgs b = a;
+            if (behind) b.dx = nullptr;
+            norm_grad_long_kernel<T><<<grid, 1024, 0, st>>>(b);
+            e = hipGetLastError();
+            if (e == hipSuccess && a.sums) {
+                norm_grad_columns_kernel<T><<<dim3((unsigned)((a.width + 511LL) / 512), plan.parts), 256, 0, st>>>(a, plan.group);
+                e = hipGetLastError();
+            }
+            if (e == hipSuccess && behind) {
+                b = a;
+                b.factors = nullptr;
+                norm_grad_long_kernel<T><<<grid, 1024, 0, st>>>(b);
+                e = hipGetLastError();
+            }
+        }
+    }
+    if (e != hipSuccess || !a.dw) return e;
+    const long long groups = (a.width + 63LL) / 64;
+    norm_grad_join_kernel<T><<<dim3(grid_row(groups), grid_rows(groups)), 1024, 0, st>>>(a.sums, (T *)a.dw, a.rows > 0 ? plan.parts : 0, a.width);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm_grad(const NormGradArgs &a, int type, hipStream_t st)
+{
+    return type == OZIMMU_BF16 ? launch<bf16>(a, st) : type == OZIMMU_F16 ? launch<f16>(a, st) : launch<float>(a, st);
+}
+
+}  // namespace oz

@@ -35,6 +35,10 @@ _SIGNATURES = {
     "ozimmu_linear_grad_workspace_bytes": (_size, [_int] * 6),
     "ozimmu_linear_grad": (_int, [_int] * 4 + [_ptr, _int] * 4 + [_int] + [_ptr, _int] * 2 + [_ptr, _ptr, _size, _ptr]),
     "ozimmu_moe_workspace_bytes": (_size, [_int] * 6),
+    "ozimmu_quantise": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _ptr]),
+    "ozimmu_rms_norm": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _c.c_double, _ptr, _int, _ptr, _int, _ptr, _int, _ptr, _ptr]),
+    "ozimmu_rms_norm_grad_workspace_bytes": (_size, [_int] * 2),
+    "ozimmu_rms_norm_grad": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _c.c_double] + [_ptr, _int] * 2 + [_ptr, _ptr, _size, _ptr]),
     "ozimmu_moe": (_int, [_int] * 7 + [_ptr, _int] + [_ptr] * 6 + [_int, _ptr, _size, _ptr]),
 }
 
@@ -340,3 +344,115 @@ def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, ga
     if rc != OK:
         raise OzimmuError(rc, "moe")
     return out, chosen, gates
+
+
+def _matrix(x, what):
+    if x.dim() != 2:
+        raise ValueError(f"{what}: a matrix expected")
+    return x.shape
+
+
+def _codes(out, scale, rows, cols, like):
+    """(codes, their row stride, scales) of rows in 8 bits: given tensors or new ones."""
+    index = like.get_device()
+    if out is None:
+        out = torch.empty((rows, cols), dtype=torch.int8, device=like.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=like.device)
+    return out, _ld_codes(out, rows, cols, index, "out"), scale, _scale(scale, rows, index, "scale")
+
+
+def _ld_codes(x, rows, cols, index, what):
+    if x.dtype is not torch.int8 or x.get_device() != index:
+        raise ValueError(f"{what}: int8 on cuda:{index} expected")
+    return _ld(x, rows, cols, x, what)
+
+
+def _scale(x, n, index, what):
+    if x.shape != (n,) or x.dtype is not torch.float32 or x.get_device() != index or (n > 1 and x.stride(0) != 1):
+        raise ValueError(f"{what}: contiguous [{n}] of float32 on cuda:{index} expected")
+    return x.data_ptr()
+
+
+def quantise(x, out=None, scale=None):
+    """x [rows, cols] in 8 bits: (codes, scale), int8 [rows, cols] and float32 [rows], that stand for codes * scale[:, None].
+
+    scale is the row's largest magnitude / 127, codes are rounded to nearest; a row with a value that is not finite has
+    a scale of NaN.  Asynchronous on the current stream."""
+    kind = _type_of(x, "x")
+    rows, cols = _matrix(x, "x")
+    ldx = _ld(x, rows, cols, x, "x")
+    out, ldc, scale, pscale = _codes(out, scale, rows, cols, x)
+    rc = (_lib or lib()).ozimmu_quantise(rows, cols, kind, x.data_ptr(), ldx, out.data_ptr(), ldc, pscale, _stream(x.get_device(), "quantise"))
+    if rc != OK:
+        raise OzimmuError(rc, "quantise")
+    return out, scale
+
+
+def _norm(x, weight, residual, eps, total, y, codes, scale, what):
+    """The norm's call: (tensors that it made or was given)."""
+    kind = _type_of(x, "x")
+    tokens, width = _matrix(x, "x")
+    ldx = _ld(x, tokens, width, x, "x")
+    pw = None if weight is None else _vector(weight, width, x, "weight")
+    ldr = ldt = ldy = ldc = 0
+    py = pc = ps = pt = pr = None
+    if residual is not None:
+        ldr, pr = _ld(residual, tokens, width, x, "residual"), residual.data_ptr()
+        if total is None:
+            total = torch.empty((tokens, width), dtype=x.dtype, device=x.device)
+    if total is not None:
+        ldt, pt = _ld(total, tokens, width, x, "total"), total.data_ptr()
+    if what == "rms_norm":
+        if y is None:
+            y = torch.empty((tokens, width), dtype=x.dtype, device=x.device)
+        ldy, py = _ld(y, tokens, width, x, "out"), y.data_ptr()
+    else:
+        codes, ldc, scale, ps = _codes(codes, scale, tokens, width, x)
+        pc = codes.data_ptr()
+    rc = (_lib or lib()).ozimmu_rms_norm(tokens, width, kind, x.data_ptr(), ldx, pr, ldr, pw, eps, pt, ldt, py, ldy, pc, ldc, ps,
+                                         _stream(x.get_device(), what))
+    if rc != OK:
+        raise OzimmuError(rc, what)
+    return y, codes, scale, x if total is None else total
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, total=None, out=None):
+    """Root-mean-square norm of each row of h = x + residual: (y, total), y = h * (mean(h^2) + eps)^-1/2 * weight, total = h.
+
+    x, residual [tokens, width], weight [width] (None: ones).  `total` receives h, rounded (y goes by the unrounded h), and may be
+    x or residual itself; without a residual it is x unless a tensor is given.  Asynchronous on the current stream."""
+    y, _, _, total = _norm(x, weight, residual, eps, total, out, None, None, "rms_norm")
+    return y, total
+
+
+def rms_norm8(x, weight=None, residual=None, eps=1e-6, total=None, out=None, scale=None):
+    """rms_norm with its result in 8 bits, as linear8 takes it: (codes, scale, total)."""
+    return _norm(x, weight, residual, eps, total, None, out, scale, "rms_norm8")[1:]
+
+
+def rms_norm_grad_workspace_bytes(tokens, width):
+    return lib().ozimmu_rms_norm_grad_workspace_bytes(*_sizes(tokens, width))
+
+
+def rms_norm_grad(dy, total, weight=None, eps=1e-6, add=None, dx=None, dw=None, want=("dx", "dw"), workspace=None):
+    """Gradients (dx, dw) of rms_norm, or of the values that rms_norm8's results stand for, from dy [tokens, width] and its `total`.
+
+    dx is the gradient of x and of the residual; `add` [tokens, width], the gradient that reaches `total` from elsewhere, is added to
+    it, and dx may be dy, total or add itself.  Of dx and dw those in `want` are formed, the others are None."""
+    kind = _type_of(dy, "dy")
+    tokens, width = _matrix(dy, "dy")
+    lddy, ldh = _ld(dy, tokens, width, dy, "dy"), _ld(total, tokens, width, dy, "total")
+    pw = None if weight is None else _vector(weight, width, dy, "weight")
+    lda = 0 if add is None else _ld(add, tokens, width, dy, "add")
+    dx = None if "dx" not in want else torch.empty((tokens, width), dtype=dy.dtype, device=dy.device) if dx is None else dx
+    dw = None if "dw" not in want else torch.empty(width, dtype=dy.dtype, device=dy.device) if dw is None else dw
+    lddx = 0 if dx is None else _ld(dx, tokens, width, dy, "dx")
+    pdw = None if dw is None else _vector(dw, width, dy, "dw")
+    L = _lib or lib()
+    keep, ws, nbytes = _workspace(workspace, L.ozimmu_rms_norm_grad_workspace_bytes(tokens, width) if workspace is None and dw is not None else 0, dy.device)
+    rc = L.ozimmu_rms_norm_grad(tokens, width, kind, dy.data_ptr(), lddy, total.data_ptr(), ldh, pw, eps, None if add is None else add.data_ptr(), lda,
+                                None if dx is None else dx.data_ptr(), lddx, pdw, ws, nbytes, _stream(dy.get_device(), "rms_norm_grad"))
+    if rc != OK:
+        raise OzimmuError(rc, "rms_norm_grad")
+    return dx, dw

@@ -1,0 +1,95 @@
+"""CPU-side checks of the operators on rows in 8 bits: refused arguments, sizes of workspaces, what the binding refuses."""
+import ctypes
+import os
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+BAD, OK = 1, 0
+F = ctypes.c_void_p(1 << 20)           # never read: every call below is refused, or has nothing to do, before a kernel starts
+ODD = ctypes.c_void_p((1 << 20) + 1)
+MOST = (1 << 30) - 1
+
+
+@pytest.fixture(scope="module")
+def handle():
+    from paper_2506_11277_amd import build, layers, ozimmu
+    if not os.path.exists(ozimmu.LIB_PATH):
+        build.build_lib()
+    return layers.lib()
+
+
+def norm(h, tokens=4, width=8, type=0, x=F, ldx=8, residual=None, ldr=8, weight=F, eps=1e-6, total=None, ldt=8, y=F, ldy=8, codes=None, ldc=8, scale=None):
+    return h.ozimmu_rms_norm(tokens, width, type, x, ldx, residual, ldr, weight, eps, total, ldt, y, ldy, codes, ldc, scale, None)
+
+
+@pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(width=-1), dict(tokens=1 << 30), dict(width=1 << 30, ldx=1 << 30, ldy=1 << 30), dict(type=3), dict(type=-1),
+                                   dict(x=None), dict(x=ODD), dict(ldx=7), dict(residual=F, ldr=7), dict(residual=ODD), dict(weight=ODD), dict(eps=0.0),
+                                   dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(eps=1e-60), dict(eps=1e60), dict(total=F, ldt=7), dict(total=ODD), dict(y=ODD), dict(ldy=7),
+                                   dict(codes=F, scale=None), dict(codes=F, scale=F, ldc=7), dict(codes=F, scale=ODD), dict(codes=None, scale=F),
+                                   dict(type=2, x=ctypes.c_void_p((1 << 20) + 2))])
+def test_norm_refuses(handle, wrong):
+    assert norm(handle, **wrong) == BAD
+
+
+def test_norm_of_nothing(handle):
+    assert norm(handle, tokens=0, x=None, y=None) == OK and norm(handle, y=None) == OK
+
+
+def quantise(h, rows=4, cols=8, type=0, x=F, ldx=8, codes=F, ldc=8, scale=F):
+    return h.ozimmu_quantise(rows, cols, type, x, ldx, codes, ldc, scale, None)
+
+
+@pytest.mark.parametrize("wrong", [dict(rows=-1), dict(cols=-1), dict(rows=1 << 30), dict(cols=1 << 30, ldx=1 << 30, ldc=1 << 30), dict(type=4), dict(type=-1), dict(x=None),
+                                   dict(x=ODD), dict(ldx=7), dict(codes=None), dict(ldc=7), dict(scale=None), dict(scale=ODD)])
+def test_quantise_refuses(handle, wrong):
+    assert quantise(handle, **wrong) == BAD
+
+
+def norm_grad(h, tokens=4, width=8, type=0, dy=F, lddy=8, x=F, ldh=8, weight=F, eps=1e-6, add=None, ldadd=8, dx=F, lddx=8, dw=F, ws=F, nbytes=1 << 40):
+    return h.ozimmu_rms_norm_grad(tokens, width, type, dy, lddy, x, ldh, weight, eps, add, ldadd, dx, lddx, dw, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(width=-1), dict(tokens=1 << 30), dict(width=1 << 30, lddy=1 << 30, ldh=1 << 30, lddx=1 << 30), dict(type=3), dict(dy=None),
+                                   dict(dy=ODD), dict(lddy=7), dict(x=None), dict(x=ODD), dict(ldh=7), dict(weight=ODD), dict(eps=0.0), dict(eps=float("nan")),
+                                   dict(add=F, ldadd=7), dict(add=ODD), dict(dx=ODD), dict(lddx=7), dict(dw=ODD), dict(ws=None), dict(nbytes=0),
+                                   dict(ws=ctypes.c_void_p((1 << 20) + 128))])
+def test_norm_grad_refuses(handle, wrong):
+    assert norm_grad(handle, **wrong) == BAD
+
+
+def test_norm_grad_workspace(handle):
+    need = handle.ozimmu_rms_norm_grad_workspace_bytes
+    assert need(-1, 8) == 0 and need(8, 1 << 30) == 0 and need(0, 8) == 0 and need(8, 0) == 0
+    for tokens in (1, 5, 1000, 1 << 20, MOST):
+        for width in (1, 1001, 4096, 16384, 16385, 1 << 20):
+            assert 4 * width <= need(tokens, width) <= 1024 * 4 * (width + 64) + 8 * (tokens + 32)
+            assert norm_grad(handle, tokens, width, lddy=width, ldh=width, lddx=width, nbytes=need(tokens, width) - 1) == BAD
+    assert norm_grad(handle, width=0) == OK and norm_grad(handle, dx=None, dw=None, ws=None, nbytes=0) == OK
+
+
+def bf16(*shape, dtype=torch.bfloat16):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def test_the_binding_refuses(monkeypatch):
+    from paper_2506_11277_amd import layers
+    with pytest.raises(ValueError):
+        layers.quantise(bf16(2, 8))                       # not a CUDA tensor
+    monkeypatch.setattr(layers, "_type_of", lambda x, what: layers._TYPES[x.dtype])
+    monkeypatch.setattr(layers, "_stream", lambda index, what: None)
+    x, w, f32 = bf16(2, 8), bf16(8), torch.float32
+    for call in (lambda: layers.quantise(bf16(8)), lambda: layers.quantise(x, out=bf16(2, 8)), lambda: layers.quantise(x, out=bf16(2, 7, dtype=torch.int8)),
+                 lambda: layers.quantise(x, scale=bf16(2)), lambda: layers.quantise(x, scale=bf16(3, dtype=f32)), lambda: layers.quantise(bf16(8, 2).t()),
+                 lambda: layers.quantise(x, scale=bf16(4, dtype=f32)[::2]),
+                 lambda: layers.rms_norm(x, bf16(7)), lambda: layers.rms_norm(x, bf16(8, dtype=f32)), lambda: layers.rms_norm(x, w, bf16(3, 8)),
+                 lambda: layers.rms_norm(x, w, bf16(2, 8, dtype=f32)), lambda: layers.rms_norm(x, w, out=bf16(2, 7)), lambda: layers.rms_norm(bf16(1, 2, 8), w),
+                 lambda: layers.rms_norm(x, w, x, total=bf16(2, 7)), lambda: layers.rms_norm8(x, w, out=x), lambda: layers.rms_norm8(x, w, scale=bf16(2)),
+                 lambda: layers.rms_norm_grad(x, bf16(3, 8), w), lambda: layers.rms_norm_grad(x, x, bf16(9)), lambda: layers.rms_norm_grad(x, x, w, add=bf16(2, 9)),
+                 lambda: layers.rms_norm_grad(x, x, w, dx=bf16(2, 8, dtype=f32)), lambda: layers.rms_norm_grad(x, x, w, dw=bf16(7)),
+                 lambda: layers.rms_norm_grad_workspace_bytes(1 << 32, 8)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(layers.OzimmuError):
+        layers.rms_norm(x, w, eps=0.0)
