@@ -159,6 +159,19 @@ int ozimmu_rms_norm_grad(int tokens, int width, int type, const void *dy, int ld
                          double eps, const void *add, int ldadd, void *dx, int lddx, void *dw, void *workspace,
                          size_t workspace_bytes, void *stream);
 
+/*
+ * y = act(x w^T + bias) + residual with x and w in 8 bits:
+ *   x [tokens, n_in] with x_scale [tokens], w [n_out, n_in] with w_scale [n_out], n_in <= OZIMMU_LINEAR8_IN (any codes from -128 to 127); bias [n_out],
+ *   residual, pre and y [tokens, n_out] of `type`, as in ozimmu_linear.
+ * The sum of the products of codes is exact; it is rounded to 32 bits, multiplied by x_scale and then by w_scale, and what follows is
+ * ozimmu_linear's.  Workspace: as for ozimmu_linear.
+ */
+#define OZIMMU_LINEAR8_IN 131071
+size_t ozimmu_linear8_workspace_bytes(int tokens, int n_in, int n_out, int aligned);
+int ozimmu_linear8(int tokens, int n_in, int n_out, int type, const int8_t *x, int ldx, const float *x_scale, const int8_t *w, int ldw,
+                   const float *w_scale, const void *bias, const void *residual, int ldr, int activation, void *pre, int ldpre,
+                   void *y, int ldy, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

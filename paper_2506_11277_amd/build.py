@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libozimmu.so")
 SOURCES = ["api.hip", "reduce.hip", "split.hip", "gemm.hip", "gemm_fused16.hip", "gemm_banded.hip", "gemm_small.hip", "gemm_vectors.hip",
            "gemm_halves16.hip", "gemm_passes.hip", "gemm_passes_4.hip", "gemm_passes_10.hip", "gemm_passes_13.hip", "gemm_passes_15.hip", "gemm_passes_17.hip", "gemm_passes_19.hip", "ceiling.hip",
-           "layers_api.hip", "product_bf16.hip", "product_f16.hip", "product_f32.hip", "pad.hip", "grad.hip", "adamw.hip", "moe.hip", "norm.hip", "norm_grad.hip"]
+           "layers_api.hip", "product_bf16.hip", "product_f16.hip", "product_f32.hip", "product8_bf16.hip", "product8_f16.hip", "product8_f32.hip", "pad.hip", "grad.hip", "adamw.hip", "moe.hip", "norm.hip", "norm_grad.hip"]
 HEADERS = [os.path.join(CSRC, "oz_common.h"), os.path.join(CSRC, "gemm_dev.h"), os.path.join(CSRC, "gemm_passes_dev.h"), os.path.join(CSRC, "slice_dev.h"), os.path.join(HERE, "..", "include", "ozimmu.h"),
            os.path.join(HERE, "..", "include", "ozimmu_bench.h")]
 # what only the feed-forward operators' sources include

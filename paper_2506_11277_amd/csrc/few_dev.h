@@ -8,7 +8,7 @@ namespace oz {
 
 constexpr int kFewWaves = 8;
 
-template <class T, int U>
+template <class T, class O, int U>
 __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(Product a, float *partial, int steps_per_split)
 {
     constexpr int KE = 8 * Chunk<T>::E;
@@ -31,21 +31,21 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(Product a, f
     for (int s = 0; s < kFewWaves; ++s) {
         const float *from = &sums[s][q * kStreamLd + c];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += from[e];
+        for (int e = 0; e < 8; ++e) v[e] = add_sums<T>(v[e], from[e]);
     }
     if (partial) store_row(partial + ((size_t)blockIdx.y * a.e.nq + q) * ((a.e.np + 7) & ~7) + p, v);
-    else finish_row<T>(a.e, q, p, v);
+    else finish_row<T, O>(a.e, q, p, v);
 }
 
-template <class T>
+template <class T, class O = T>
 hipError_t launch_few_tokens(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
     const int groups = (a.e.np + 15) / 16;
     const dim3 grid(grid_row(groups), plan.splits, grid_rows(groups));
     float *const to = plan.splits > 1 ? partial : nullptr;
     // (steps whose loads a wavefront issues together: no more than it has)
-    if (plan.steps > 2 * kFewWaves) few_tokens_kernel<T, 4><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
-    else few_tokens_kernel<T, 2><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
+    if (plan.steps > 2 * kFewWaves) few_tokens_kernel<T, O, 4><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
+    else few_tokens_kernel<T, O, 2><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
     return hipGetLastError();
 }
 

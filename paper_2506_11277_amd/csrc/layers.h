@@ -4,7 +4,8 @@
 
 namespace oz {
 
-inline size_t element_bytes(int type) { return type == OZIMMU_F32 ? 4 : 2; }
+constexpr int kType8 = 8;                  // operands in 8 bits (whole numbers), beside the types that callers name
+inline size_t element_bytes(int type) { return type == OZIMMU_F32 ? 4 : type == kType8 ? 1 : 2; }
 
 constexpr int kFewTokens = 16;             // columns few_tokens_kernel takes
 ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows, bool direct);
@@ -19,8 +20,12 @@ hipError_t launch_product_f16(const Product &a, const ProductPlan &plan, float *
 hipError_t launch_pair_f16(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
 hipError_t launch_product_f32(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
 hipError_t launch_pair_f32(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st);
+// operands in 8 bits, results of the named type
+hipError_t launch_product8_bf16(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_product8_f16(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
+hipError_t launch_product8_f32(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st);
 
-// rows of `cols` entries, `ld` apart, to rows `ldto` apart (a multiple of 8), zeros behind them (pad.hip)
+// rows of `cols` entries, `ld` apart, to rows `ldto` apart (a multiple of 8, in 8 bits of 16), zeros behind them (pad.hip)
 struct PadCopy {
     const void *from;
     void *to;

@@ -21,11 +21,13 @@ static double tiles_of(int t, int np, int nq)
     return (double)((np + e - 1) / e) * ((nq + e - 1) / e);
 }
 // (operands that go to LDS through registers: a step takes two to three times as long in 16 bits, a fifth longer in 32)
+// (a step of 128 bytes of k takes operands of 8 bits as long as those of 16, with twice the k)
+static int step_entries(int type) { return 128 / (int)element_bytes(type); }
 static double tile_us(int t, int steps, int type, bool direct = true) { return kShapes[t].tile + steps * (type == OZIMMU_F32 ? kShapes[t].step32 : kShapes[t].step16) * (direct ? 1 : type == OZIMMU_F32 ? 1.2 : 2.5); }
 
 ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows, bool direct)
 {
-    const int ke = type == OZIMMU_F32 ? 32 : 64;
+    const int ke = step_entries(type);
     const int all = (nk + ke - 1) / ke;
     if (k_rows && nq <= kFewTokens) {
         // work-groups of 16 features; the contraction is divided where they leave most compute units without one
@@ -50,7 +52,7 @@ ProductPlan plan_product(int np, int nq, int nk, int type, bool k_rows, bool dir
 // the bias gradient's).
 int plan_pair(const Product &x, const ProductPlan &xp, const Product &w, const ProductPlan &wp, int type, bool bias)
 {
-    const int ke = type == OZIMMU_F32 ? 32 : 64;
+    const int ke = step_entries(type);
     int best = -1;
     double least = xp.us + wp.us + 2 + (bias ? 3 : 0);
     for (int t = kTile128; t <= kTile64; ++t) {
@@ -95,6 +97,8 @@ inline bool direct_operand(const void *p, int ld, int along, size_t size)
     return on16(p, ld, size) && (size_t)along * size % 16 == 0 && 256ull * (unsigned)ld * size < (1ull << 32);
 }
 
+// entries of a row of a copy
+inline int up(int n, size_t size) { return size == 1 ? (n + 15) & ~15 : (n + 7) & ~7; }
 inline int up8(int n) { return (n + 7) & ~7; }
 
 // bytes of the copies of a product's operands (P, Q) in aligned rows
@@ -102,16 +106,17 @@ inline size_t copy_bytes(const Product &a, bool of_p, size_t size)
 {
     const size_t rows = of_p ? (a.p_k_rows ? a.p_rows : a.p_nk) : (a.q_k_rows ? a.q_rows : a.q_nk);
     const int along = of_p ? (a.p_k_rows ? a.p_nk : a.p_rows) : (a.q_k_rows ? a.q_nk : a.q_rows);
-    return padded(rows * up8(along) * size);
+    return padded(rows * up(along, size) * size);
 }
 
 // The plan of a product, and the copies that it wants first (`space`: where they go; null: there is no room, or too little).
-ProductPlan route_product(Product &a, int type, bool k_rows, char *space, size_t space_bytes, PadCopies &copies)
+// type: of the operands, result: of what the epilogue reads and writes.
+ProductPlan route_product(Product &a, int type, int result, bool k_rows, char *space, size_t space_bytes, PadCopies &copies)
 {
-    const size_t size = element_bytes(type);
+    const size_t size = element_bytes(type), out = element_bytes(result);
     Epilogue &e = a.e;
-    e.wide = on16(e.out, e.ldo, size) && (!e.bias || (uintptr_t)e.bias % 16 == 0) && (!e.residual || on16(e.residual, e.ldr, size)) &&
-             (!e.pre || on16(e.pre, e.ldpre, size));
+    e.wide = on16(e.out, e.ldo, out) && (!e.bias || (uintptr_t)e.bias % 16 == 0) && (!e.residual || on16(e.residual, e.ldr, out)) &&
+             (!e.pre || on16(e.pre, e.ldpre, out)) && (uintptr_t)e.p_scale % 16 == 0;
     copies = PadCopies{};
     const bool p_fits = direct_operand(a.P, a.ldp, a.p_k_rows ? a.p_nk : a.p_rows, size), q_fits = direct_operand(a.Q, a.ldq, a.q_k_rows ? a.q_nk : a.q_rows, size);
     const ProductPlan direct = plan_product(e.np, e.nq, a.nk, type, k_rows, true);
@@ -119,14 +124,14 @@ ProductPlan route_product(Product &a, int type, bool k_rows, char *space, size_t
     const ProductPlan other = plan_product(e.np, e.nq, a.nk, type, k_rows, false);
     // (a copy whose rows are too long for direct operands is of no use)
     const int p_along = a.p_k_rows ? a.p_nk : a.p_rows, q_along = a.q_k_rows ? a.q_nk : a.q_rows;
-    if (256ull * up8(p_along) * size >= (1ull << 32) || 256ull * up8(q_along) * size >= (1ull << 32)) return other;
+    if (256ull * up(p_along, size) * size >= (1ull << 32) || 256ull * up(q_along, size) * size >= (1ull << 32)) return other;
     const size_t p_bytes = p_fits ? 0 : copy_bytes(a, true, size), q_bytes = q_fits ? 0 : copy_bytes(a, false, size);
     // The copies: a launch, and their bytes read and written at 4 TB/s.  Rows off 16 bytes, without and with them: 4096^3 f16 321 and
     // 128 us (aligned: 110), 1024 x 4096 x 1024 52 and 30, 1531 x 1000 x 776 17 either way, 200 x 1000 x 4000 15 and 19.
     if (a.nk == 0 || space == nullptr || space_bytes < p_bytes + q_bytes || direct.us + 6 + 2 * (p_bytes + q_bytes) / 4e6 >= other.us) return other;
     auto copy = [&](PadCopy &c, const void *&x, int &ld, bool rows_along_k, int &rows, int &nk, char *to) {
         int &along = rows_along_k ? nk : rows;
-        c = PadCopy{x, to, rows_along_k ? rows : nk, along, ld, up8(along)};
+        c = PadCopy{x, to, rows_along_k ? rows : nk, along, ld, up(along, size)};
         x = to;
         ld = along = c.ldto;
     };
@@ -161,7 +166,7 @@ LinearWorkspace linear_workspace(int tokens, int n_in, int n_out, int type, bool
     w.copies = either_partial_bytes(n_out, tokens, n_in, type, true);
     const ProductPlan direct = plan_product(n_out, tokens, n_in, type, true, true), other = plan_product(n_out, tokens, n_in, type, true, false);
     if ((!aligned || n_in * size % 16) && direct.tile != kTileFew && direct.us + 3 < other.us)
-        w.copies_bytes = padded((size_t)tokens * up8(n_in) * size) + padded((size_t)n_out * up8(n_in) * size);
+        w.copies_bytes = padded((size_t)tokens * up(n_in, size) * size) + padded((size_t)n_out * up(n_in, size) * size);
     w.total = w.copies + w.copies_bytes;
     return w;
 }
@@ -194,6 +199,39 @@ inline bool bad_workspace(const void *p, size_t have, size_t want)
     return want > 0 && (p == nullptr || have < want || (uintptr_t)p % 256 != 0);
 }
 
+// ozimmu_linear and ozimmu_linear8, their arguments checked but for the workspace: operands of `type`, the rest of `result`
+int linear(int tokens, int n_in, int n_out, int type, int result, const void *x, int ldx, const float *x_scale, const void *w, int ldw, const float *w_scale,
+           const void *bias, const void *residual, int ldr, int activation, void *pre, int ldpre, void *y, int ldy, void *workspace,
+           size_t workspace_bytes, void *stream)
+{
+    if (bad_workspace(workspace, workspace_bytes, linear_workspace(tokens, n_in, n_out, type, true).total)) return OZIMMU_BAD_ARG;
+    if (tokens == 0 || n_out == 0) return OZIMMU_OK;
+    const LinearWorkspace ws = linear_workspace(tokens, n_in, n_out, type, false);
+    // (a workspace that is not needed may be anywhere, but copies go to 16 bytes)
+    const bool room = ws.copies_bytes > 0 && workspace_bytes >= ws.total && (uintptr_t)workspace % 256 == 0;
+    Product a{};
+    a.P = w;
+    a.ldp = ldw;
+    a.p_k_rows = true;
+    a.p_rows = n_out;
+    a.Q = x;
+    a.ldq = ldx;
+    a.q_k_rows = true;
+    a.q_rows = tokens;
+    a.nk = a.p_nk = a.q_nk = n_in;
+    a.e = Epilogue{bias, residual, pre, y, ldr, ldpre, ldy, n_out, tokens, activation, x_scale, w_scale, 0};
+    PadCopies copies;
+    const ProductPlan plan = route_product(a, type, result, true, room ? (char *)workspace + ws.copies : nullptr, ws.copies_bytes, copies);
+    const hipStream_t st = (hipStream_t)stream;
+    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    float *const partial = (float *)workspace;
+    const hipError_t e = type != kType8            ? launch_product(a, plan, type, partial, st)
+                         : result == OZIMMU_BF16 ? launch_product8_bf16(a, plan, partial, st)
+                         : result == OZIMMU_F16  ? launch_product8_f16(a, plan, partial, st)
+                                                 : launch_product8_f32(a, plan, partial, st);
+    return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+}
+
 }  // namespace
 
 extern "C" {
@@ -213,32 +251,32 @@ int ozimmu_linear(int tokens, int n_in, int n_out, int type, const void *x, int 
     if (bad_rows(tokens, n_in, x, ldx, size) || bad_rows(n_out, n_in, w, ldw, size) || bad_rows(tokens, n_out, y, ldy, size)) return OZIMMU_BAD_ARG;
     if ((uintptr_t)bias % size || (residual && bad_rows(tokens, n_out, residual, ldr, size)) || (pre && bad_rows(tokens, n_out, pre, ldpre, size)))
         return OZIMMU_BAD_ARG;
-    if (bad_workspace(workspace, workspace_bytes, linear_workspace(tokens, n_in, n_out, type, true).total)) return OZIMMU_BAD_ARG;
-    if (tokens == 0 || n_out == 0) return OZIMMU_OK;
-    const LinearWorkspace ws = linear_workspace(tokens, n_in, n_out, type, false);
-    // (a workspace that is not needed may be anywhere, but copies go to 16 bytes)
-    const bool room = ws.copies_bytes > 0 && workspace_bytes >= ws.total && (uintptr_t)workspace % 256 == 0;
-    Product a{};
-    a.P = w;
-    a.ldp = ldw;
-    a.p_k_rows = true;
-    a.p_rows = n_out;
-    a.Q = x;
-    a.ldq = ldx;
-    a.q_k_rows = true;
-    a.q_rows = tokens;
-    a.nk = a.p_nk = a.q_nk = n_in;
-    a.e = Epilogue{bias, residual, pre, y, ldr, ldpre, ldy, n_out, tokens, activation, 0};
-    PadCopies copies;
-    const ProductPlan plan = route_product(a, type, true, room ? (char *)workspace + ws.copies : nullptr, ws.copies_bytes, copies);
-    const hipStream_t st = (hipStream_t)stream;
-    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    return launch_product(a, plan, type, (float *)workspace, st) == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+    return linear(tokens, n_in, n_out, type, type, x, ldx, nullptr, w, ldw, nullptr, bias, residual, ldr, activation, pre, ldpre, y, ldy, workspace, workspace_bytes, stream);
+}
+
+size_t ozimmu_linear8_workspace_bytes(int tokens, int n_in, int n_out, int aligned)
+{
+    if (bad_sizes(tokens, n_in, n_out) || n_in > OZIMMU_LINEAR8_IN) return 0;
+    return linear_workspace(tokens, n_in, n_out, kType8, aligned != 0).total;
+}
+
+int ozimmu_linear8(int tokens, int n_in, int n_out, int type, const int8_t *x, int ldx, const float *x_scale, const int8_t *w, int ldw,
+                   const float *w_scale, const void *bias, const void *residual, int ldr, int activation, void *pre, int ldpre, void *y,
+                   int ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU || n_in > OZIMMU_LINEAR8_IN) return OZIMMU_BAD_ARG;
+    const size_t size = element_bytes(type);
+    if (bad_rows(tokens, n_in, x, ldx, 1) || bad_rows(n_out, n_in, w, ldw, 1) || bad_rows(tokens, n_out, y, ldy, size)) return OZIMMU_BAD_ARG;
+    if ((uintptr_t)bias % size || (residual && bad_rows(tokens, n_out, residual, ldr, size)) || (pre && bad_rows(tokens, n_out, pre, ldpre, size)))
+        return OZIMMU_BAD_ARG;
+    if ((tokens > 0 && !x_scale) || (n_out > 0 && !w_scale) || (uintptr_t)x_scale % 4 || (uintptr_t)w_scale % 4) return OZIMMU_BAD_ARG;
+    return linear(tokens, n_in, n_out, kType8, type, x, ldx, x_scale, w, ldw, w_scale, bias, residual, ldr, activation, pre, ldpre, y, ldy, workspace,
+                  workspace_bytes, stream);
 }
 
 int ozimmu_debug_linear_tile(int which, int tokens, int n_in, int n_out, int type, int aligned, int *parts)
 {
-    if (which < 0 || which > 3 || bad_sizes(tokens, n_in, n_out) || bad_type(type)) return OZIMMU_BAD_ARG;
+    if (which < 0 || which > 3 || bad_sizes(tokens, n_in, n_out) || (bad_type(type) && !(which == 0 && type == kType8))) return OZIMMU_BAD_ARG;
     const int np = which == 0 ? n_out : n_in, nq = which == 2 ? n_out : tokens, nk = which == 0 ? n_in : which == 1 ? n_out : tokens;
     const ProductPlan plan = plan_product(np, nq, nk, type, which == 0, aligned != 0);
     if (parts) *parts = which == 3 ? 1 : plan.splits;
@@ -316,7 +354,7 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
     x_grad.q_rows = tokens;
     x_grad.q_nk = dz_cols;
     x_grad.nk = n_out;
-    x_grad.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, 0};
+    x_grad.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
     w_grad.P = x;
     w_grad.ldp = ldx;
     w_grad.p_rows = n_in;
@@ -326,13 +364,13 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
     w_grad.q_rows = dz_cols;
     w_grad.q_nk = tokens;
     w_grad.nk = tokens;
-    w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, 0};
+    w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
     PadCopies x_copies{}, w_copies{}, copies{};
     ProductPlan x_plan{}, w_plan{};
     const bool form_dx = dx && tokens > 0 && n_in > 0, form_dw = dw && n_out > 0 && n_in > 0;
     // (of each product P alone can want a copy here: dz is the workspace's, or dy where there is no room for either)
-    if (form_dx) x_plan = route_product(x_grad, type, false, ws.has_copies ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies);
-    if (form_dw) w_plan = route_product(w_grad, type, false, ws.has_copies ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
+    if (form_dx) x_plan = route_product(x_grad, type, type, false, ws.has_copies ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies);
+    if (form_dw) w_plan = route_product(w_grad, type, type, false, ws.has_copies ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
     copies.c[0] = x_copies.c[0];
     copies.c[1] = w_copies.c[0];
     if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;

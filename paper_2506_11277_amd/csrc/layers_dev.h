@@ -44,6 +44,20 @@ __device__ __forceinline__ v4f mma(v4u p, v4u q, v4f c, float)
     return c;
 }
 
+// Operands of 8 bits: one 16x16x64 instruction, lane l holds row l % 16 and k 16 (l / 16) ... + 15.  Sums are whole numbers of 32 bits, exact for
+// up to 131071 products; where sums of either kind pass through the same places (registers, LDS, memory) they stand there as bits.
+__device__ __forceinline__ v4f mma(v4u p, v4u q, v4f c, int8_t)
+{
+    return __builtin_bit_cast(v4f, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, p), __builtin_bit_cast(v4i, q), __builtin_bit_cast(v4i, c), 0, 0, 0));
+}
+// a + b of operands of type T
+template <class T>
+__device__ __forceinline__ float add_sums(float a, float b)
+{
+    if constexpr (sizeof(T) == 1) return __int_as_float(__float_as_int(a) + __float_as_int(b));
+    else return a + b;
+}
+
 // 16 bytes from an address that is aligned to the element only, `n` elements of them there (the others 0)
 template <class T>
 __device__ __forceinline__ v4u load_chunk(const T *p, int n)
@@ -151,6 +165,7 @@ struct Epilogue {
     int ldr, ldpre, ldo;
     int np, nq;
     int act;
+    const float *q_scale, *p_scale;       // operands of 8 bits: the rows' scales; sum * q_scale[q] * p_scale[p] takes the sum's place
     int wide;                             // every row of 8 entries that starts at a multiple of 8 is aligned to its size, up to 16 bytes
 };
 
@@ -190,10 +205,23 @@ __device__ __forceinline__ void stream_row(T *p, const float (&v)[N])
     }
 }
 
-// N = 8 (p a multiple of 8) entries of row q
+// The sum of operands of type T, scaled: the whole number to the nearest float, two products.
 template <class T>
+__device__ __forceinline__ float scaled(float sum, float q_scale, float p_scale)
+{
+    if constexpr (sizeof(T) == 1) return (float)__float_as_int(sum) * q_scale * p_scale;
+    else return sum;
+}
+
+// N = 8 (p a multiple of 8) entries of row q: sums of operands of type S, results of type T
+template <class S, class T = S>
 __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, float (&v)[8])
 {
+    if constexpr (sizeof(S) == 1) {
+        const float x = e.q_scale[q];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = scaled<S>(v[i], x, p + i < e.np ? e.p_scale[p + i] : 0.0f);
+    }
     if (e.wide && p + 8 <= e.np) {
         float t[8];
         if (e.bias) {

@@ -26,12 +26,13 @@ __global__ __launch_bounds__(256) void pad_kernel(PadCopies a)
 
 hipError_t launch_pad(const PadCopies &a, int type, hipStream_t st)
 {
-    const int e = type == OZIMMU_F32 ? 4 : 8;
+    const int e = 16 / (int)element_bytes(type);
     const long long chunks = a.c[0].rows * (a.c[0].ldto / e) + a.c[1].rows * (a.c[1].ldto / e);
     if (chunks == 0) return hipSuccess;
     const long long groups = (chunks + 255) / 256;
     const dim3 grid(grid_row(groups), grid_rows(groups));
-    if (type == OZIMMU_BF16) pad_kernel<bf16><<<grid, 256, 0, st>>>(a);
+    if (type == kType8) pad_kernel<int8_t><<<grid, 256, 0, st>>>(a);
+    else if (type == OZIMMU_BF16) pad_kernel<bf16><<<grid, 256, 0, st>>>(a);
     else if (type == OZIMMU_F16) pad_kernel<f16><<<grid, 256, 0, st>>>(a);
     else pad_kernel<float><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();

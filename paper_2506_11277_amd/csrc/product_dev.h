@@ -52,11 +52,17 @@ __device__ __forceinline__ void mma_one(v4u p, v4u q, v4f &c, f16)
     if constexpr (ACC) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(p), "v"(q));
     else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+v"(c) : "v"(p), "v"(q));
 }
+template <bool ACC>
+__device__ __forceinline__ void mma_one(v4u p, v4u q, v4f &c, int8_t)
+{
+    if constexpr (ACC) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(p), "v"(q));
+    else asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+v"(c) : "v"(p), "v"(q));
+}
 template <bool ACC, class T, int FQ>
 __device__ __forceinline__ void mma_row(v4u p, const v4u (&q)[FQ], v4f (&c)[FQ])
 {
     static_assert(FQ >= 2, "");
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) <= 2) {
 #pragma unroll
         for (int j = 0; j < FQ; ++j) mma_one<ACC>(p, q[j], c[j], T{});
     } else {
@@ -240,24 +246,33 @@ struct Operand {
 // Epilogue of a wavefront's part of the tile: its sums pass through LDS, 64 q of it at a time (a loop over them with the
 // accumulators in registers would have to pick them by number, which puts them in memory), so that a lane has 8
 // entries along p of a row, always of the same columns: its bias is loaded once.
-template <class T, int PW>
-__device__ __forceinline__ void load_bias(const Epilogue &e, int p0, int lane, float (&bias)[8])
+template <class T>
+struct Columns {
+    float bias[8], scale[sizeof(T) == 1 ? 8 : 1];
+};
+template <class T, class Out, int PW>
+__device__ __forceinline__ void load_columns(const Epilogue &e, int p0, int lane, Columns<T> &c)
 {
     const int p = p0 + lane % (PW / 8) * 8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
-    if (e.bias && e.wide && p + 8 <= e.np) load_row((const T *)e.bias + p, bias);
+    for (int i = 0; i < 8; ++i) c.bias[i] = 0.0f;
+    if (e.bias && e.wide && p + 8 <= e.np) load_row((const Out *)e.bias + p, c.bias);
+    if constexpr (sizeof(T) == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c.scale[i] = 0.0f;
+        if (e.wide && p + 8 <= e.np) load_row(e.p_scale + p, c.scale);
+    }
 }
 
 // rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time
-template <class T, int ACT, int PW, int QW>
-__device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
+template <class T, class Out, int ACT, int PW, int QW>
+__device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, R = QW / ROWS < 4 ? QW / ROWS : 4;
     static_assert(QW % (ROWS * R) == 0, "");
     const int col = lane % LANES * 8, p = p0 + col;
     if (p >= e.np) return;
-    auto write = [](T *to, const float (&x)[8]) __attribute__((always_inline)) {
+    auto write = [](Out *to, const float (&x)[8]) __attribute__((always_inline)) {
         if constexpr (PW == 128) stream_row(to, x);
         else store_row(to, x);
     };
@@ -276,23 +291,27 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
                 if (q0 + s + y * ROWS < e.nq) store_row(partial + ((size_t)blockIdx.y * e.nq + q0 + s + y * ROWS) * ldn + p, v[y]);
             continue;
         }
+        float x[sizeof(T) == 1 ? R : 1];
+        if constexpr (sizeof(T) == 1)
+#pragma unroll
+            for (int y = 0; y < R; ++y) x[y] = q0 + s + y * ROWS < e.nq ? e.q_scale[q0 + s + y * ROWS] : 0.0f;
         if (e.residual)
 #pragma unroll
             for (int y = 0; y < R; ++y)
-                if (q0 + s + y * ROWS < e.nq) load_row((const T *)e.residual + (size_t)(q0 + s + y * ROWS) * e.ldr + p, res[y]);
+                if (q0 + s + y * ROWS < e.nq) load_row((const Out *)e.residual + (size_t)(q0 + s + y * ROWS) * e.ldr + p, res[y]);
 #pragma unroll
         for (int y = 0; y < R; ++y) {
             const int q = q0 + s + y * ROWS;
             if (q >= e.nq) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[y][i] += bias[i];
-            if (e.pre) write((T *)e.pre + (size_t)q * e.ldpre + p, v[y]);
+            for (int i = 0; i < 8; ++i) v[y][i] = scaled<T>(v[y][i], x[sizeof(T) == 1 ? y : 0], columns.scale[sizeof(T) == 1 ? i : 0]) + columns.bias[i];
+            if (e.pre) write((Out *)e.pre + (size_t)q * e.ldpre + p, v[y]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[y][i] = activate<T>(ACT, v[y][i]);
+            for (int i = 0; i < 8; ++i) v[y][i] = activate<Out>(ACT, v[y][i]);
             if (e.residual)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[y][i] += res[y][i];
-            write((T *)e.out + (size_t)q * e.ldo + p, v[y]);
+            write((Out *)e.out + (size_t)q * e.ldo + p, v[y]);
         }
     }
 }
@@ -300,7 +319,7 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
 // ... entry by entry, where rows are not aligned or end within 8 entries: consecutive lanes take consecutive entries, four
 // rows at a time; all 16 of a lane in a 64 x 64 tile (1531 x 1008 x 777 f16 with a residual 11.8 us against 12.2; in a 128 x 128
 // tile more than four are slower, 4097 x 1024 x 4095 f16 166 us against 155)
-template <class T, int ACT, int PW, int QW>
+template <class T, class Out, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float *sums, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, W = PW < 64 ? PW : 64, ROWS = 64 / W, R = PW == 32 ? 16 : 4;
@@ -309,50 +328,50 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
     for (int c = lane % W; c < PW; c += W) {
         const int p = p0 + c;
         if (p >= e.np) break;
-        const float bias = e.bias ? (float)((const T *)e.bias)[p] : 0.0f;
+        const float bias = e.bias ? (float)((const Out *)e.bias)[p] : 0.0f, p_scale = sizeof(T) == 1 ? e.p_scale[p] : 0.0f;
 #pragma nounroll
         for (int s = lane / W; s < QW && q0 + s < e.nq; s += R * ROWS) {
             float v[R], res[R];
 #pragma unroll
             for (int y = 0; y < R; ++y) {
                 const int q = q0 + s + y * ROWS;
-                v[y] = sums[(s + y * ROWS) * LD + c] + bias;
-                res[y] = e.residual && q < e.nq ? (float)((const T *)e.residual)[(size_t)q * e.ldr + p] : 0.0f;
+                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], sizeof(T) == 1 && q < e.nq ? e.q_scale[q] : 0.0f, p_scale) + bias;
+                res[y] = e.residual && q < e.nq ? (float)((const Out *)e.residual)[(size_t)q * e.ldr + p] : 0.0f;
             }
 #pragma unroll
             for (int y = 0; y < R; ++y) {
                 const int q = q0 + s + y * ROWS;
                 if (q >= e.nq) continue;
-                if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p] = (T)v[y];
-                float x = activate<T>(ACT, v[y]);
+                if (e.pre) ((Out *)e.pre)[(size_t)q * e.ldpre + p] = (Out)v[y];
+                float x = activate<Out>(ACT, v[y]);
                 if (e.residual) x += res[y];
-                ((T *)e.out)[(size_t)q * e.ldo + p] = (T)x;
+                ((Out *)e.out)[(size_t)q * e.ldo + p] = (Out)x;
             }
         }
     }
 }
 
-template <class T, int ACT, int PW, int QW>
-__device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
+template <class T, class Out, int ACT, int PW, int QW>
+__device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
 {
-    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, ACT, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-    else epilogue_entries<T, ACT, PW, QW>(e, sums, q0, p0, lane);
+    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, Out, ACT, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+    else epilogue_entries<T, Out, ACT, PW, QW>(e, sums, q0, p0, lane);
 }
 
-template <class T, int PW, int QW>
-__device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const float (&bias)[8], const float *sums, int q0, int p0, int lane)
+template <class T, class Out, int PW, int QW>
+__device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
 {
     switch (e.act) {                                // (decided once: a lane's entries decide nothing)
-        case OZIMMU_ACT_RELU: return epilogue_as<T, OZIMMU_ACT_RELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU: return epilogue_as<T, OZIMMU_ACT_GELU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, bias, sums, q0, p0, lane);
-        case OZIMMU_ACT_SILU: return epilogue_as<T, OZIMMU_ACT_SILU, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+        case OZIMMU_ACT_RELU: return epilogue_as<T, Out, OZIMMU_ACT_RELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU: return epilogue_as<T, Out, OZIMMU_ACT_GELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, Out, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_SILU: return epilogue_as<T, Out, OZIMMU_ACT_SILU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
     }
-    epilogue_as<T, OZIMMU_ACT_NONE, PW, QW>(e, partial, bias, sums, q0, p0, lane);
+    epilogue_as<T, Out, OZIMMU_ACT_NONE, PW, QW>(e, partial, columns, sums, q0, p0, lane);
 }
 
 // one tile, or one part of its contraction
-template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT>
+template <class T, class Out, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT>
 __device__ __forceinline__ void product_tile(const Product &a, float *partial, int steps_per_split, int tiles_p, int tiles_q, int block, char *lds)
 {
     using S = ProductShape<T, BP, BQ, WP, WQ>;
@@ -505,8 +524,8 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
         }
     }
     const int q0 = tq * BQ + wq, p0 = tp * BP + wp;
-    float bias[8];
-    load_bias<T, S::kPW>(a.e, p0, lane, bias);
+    Columns<T> columns;
+    load_columns<T, Out, S::kPW>(a.e, p0, lane, columns);
     __syncthreads();                                // (the sums take the stages' place)
     float *sums = (float *)(lds + wave * S::kSums);
     const int r = lane & 15, g = lane >> 4;
@@ -523,18 +542,18 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
             }
         });
         __builtin_amdgcn_wave_barrier();
-        epilogue<T, S::kPW, S::kSQ>(a.e, partial, bias, sums, q0 + h * S::kSQ, p0, lane);
+        epilogue<T, Out, S::kPW, S::kSQ>(a.e, partial, columns, sums, q0 + h * S::kSQ, p0, lane);
         __builtin_amdgcn_wave_barrier();
     }
 }
 
-template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT>
+template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT, class Out>
 __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float *partial, int steps_per_split, int tiles_p, int tiles_q, int blocks)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     const int block = (int)(blockIdx.z * kGridRow + blockIdx.x);
     if (block >= blocks) return;
-    product_tile<T, PK, QK, BP, BQ, WP, WQ, DIRECT>(a, partial, steps_per_split, tiles_p, tiles_q, block, lds);
+    product_tile<T, Out, PK, QK, BP, BQ, WP, WQ, DIRECT>(a, partial, steps_per_split, tiles_p, tiles_q, block, lds);
 }
 
 // dx, dw and the bias gradient of a layer in one launch: each alone leaves compute units without work in its last round, or
@@ -548,20 +567,20 @@ __global__ __launch_bounds__(256) void product_pair_kernel(Product dx, Product d
     int b = (int)(blockIdx.z * kGridRow + blockIdx.x);
     if (b >= blocks) return;
     if (b < blocks_dx) {
-        product_tile<T, false, true, BP, BQ, 2, 2, true>(dx, nullptr, (dx.nk + KE - 1) / KE, (dx.e.np + BP - 1) / BP, (dx.e.nq + BQ - 1) / BQ, b, lds);
+        product_tile<T, T, false, true, BP, BQ, 2, 2, true>(dx, nullptr, (dx.nk + KE - 1) / KE, (dx.e.np + BP - 1) / BP, (dx.e.nq + BQ - 1) / BQ, b, lds);
         return;
     }
     b -= (blocks_dx + 7) & ~7;                      // (the order of tiles goes by a work-group's XCD, its number modulo 8)
     if (b < 0) return;
     if (b < blocks_dw) {
-        product_tile<T, false, false, BP, BQ, 2, 2, true>(dw, nullptr, (dw.nk + KE - 1) / KE, (dw.e.np + BP - 1) / BP, (dw.e.nq + BQ - 1) / BQ, b, lds);
+        product_tile<T, T, false, false, BP, BQ, 2, 2, true>(dw, nullptr, (dw.nk + KE - 1) / KE, (dw.e.np + BP - 1) / BP, (dw.e.nq + BQ - 1) / BQ, b, lds);
         return;
     }
     bias_grad<T>(db, b - blocks_dw, (float *)lds);
 }
 
 // the sums of the parts, in their order, and the epilogue
-template <class T>
+template <class T, class Out>
 __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, const float *partial, int splits)
 {
     const int groups = (e.np + 7) / 8;
@@ -576,21 +595,21 @@ __global__ __launch_bounds__(256) void product_join_kernel(Epilogue e, const flo
         const v4f a = *(const v4f *)(from + s * plane), b = *(const v4f *)(from + s * plane + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[i] += a[i];
-            v[4 + i] += b[i];
+            v[i] = add_sums<T>(v[i], a[i]);
+            v[4 + i] = add_sums<T>(v[4 + i], b[i]);
         }
     }
-    finish_row<T>(e, q, p, v);
+    finish_row<T, Out>(e, q, p, v);
 }
 
-template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT>
+template <class T, bool PK, bool QK, int BP, int BQ, int WP, int WQ, bool DIRECT, class Out>
 hipError_t launch_product_shape(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
     using S = ProductShape<T, BP, BQ, WP, WQ>;
     const int tiles_p = (a.e.np + BP - 1) / BP, tiles_q = (a.e.nq + BQ - 1) / BQ;
     const long long blocks = tile_order_blocks(tiles_q, tiles_p, false);
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    const auto kernel = product_kernel<T, PK, QK, BP, BQ, WP, WQ, DIRECT>;
+    const auto kernel = product_kernel<T, PK, QK, BP, BQ, WP, WQ, DIRECT, Out>;
     static std::atomic<unsigned long long> done{0};
     if (hipError_t e = allow_dynamic_lds((const void *)kernel, S::kLds, done)) return e;
     kernel<<<dim3(grid_row(blocks), plan.splits, grid_rows(blocks)), S::kThreads, S::kLds, st>>>(a, plan.splits > 1 ? partial : nullptr, plan.steps,
@@ -598,41 +617,45 @@ hipError_t launch_product_shape(const Product &a, const ProductPlan &plan, float
     return hipGetLastError();
 }
 
-template <class T, bool PK, bool QK>
+template <class T, bool PK, bool QK, class Out>
 hipError_t launch_product_order(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
     if (plan.direct) {
-        if constexpr (sizeof(T) == 2)
-            if (plan.tile == 0) return launch_product_shape<T, PK, QK, 256, 256, 2, 2, true>(a, plan, partial, st);
-        if (plan.tile == 1) return launch_product_shape<T, PK, QK, 128, 128, 2, 2, true>(a, plan, partial, st);
-        return launch_product_shape<T, PK, QK, 64, 64, 2, 2, true>(a, plan, partial, st);
+        if constexpr (sizeof(T) <= 2)
+            if (plan.tile == 0) return launch_product_shape<T, PK, QK, 256, 256, 2, 2, true, Out>(a, plan, partial, st);
+        if (plan.tile == 1) return launch_product_shape<T, PK, QK, 128, 128, 2, 2, true, Out>(a, plan, partial, st);
+        return launch_product_shape<T, PK, QK, 64, 64, 2, 2, true, Out>(a, plan, partial, st);
     }
-    if (plan.tile <= 1) return launch_product_shape<T, PK, QK, 128, 128, 2, 2, false>(a, plan, partial, st);
-    return launch_product_shape<T, PK, QK, 64, 64, 2, 2, false>(a, plan, partial, st);
+    if (plan.tile <= 1) return launch_product_shape<T, PK, QK, 128, 128, 2, 2, false, Out>(a, plan, partial, st);
+    return launch_product_shape<T, PK, QK, 64, 64, 2, 2, false, Out>(a, plan, partial, st);
 }
 
-template <class T>
+template <class T, class Out>
 hipError_t launch_product_tiles(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
-    if (a.p_k_rows && a.q_k_rows) return launch_product_order<T, true, true>(a, plan, partial, st);
-    if (a.q_k_rows) return launch_product_order<T, false, true>(a, plan, partial, st);
-    return launch_product_order<T, false, false>(a, plan, partial, st);
+    if constexpr (sizeof(T) == 1) return launch_product_order<T, true, true, Out>(a, plan, partial, st);
+    else {
+        if (a.p_k_rows && a.q_k_rows) return launch_product_order<T, true, true, Out>(a, plan, partial, st);
+        if (a.q_k_rows) return launch_product_order<T, false, true, Out>(a, plan, partial, st);
+        return launch_product_order<T, false, false, Out>(a, plan, partial, st);
+    }
 }
 
-template <class T>
+template <class T, class Out>
 hipError_t launch_join(const Product &a, const ProductPlan &plan, const float *partial, hipStream_t st)
 {
     const size_t threads = (size_t)a.e.nq * ((a.e.np + 7) / 8), groups = (threads + 255) / 256;
     if (groups > 0x7fffffff) return hipErrorInvalidValue;
-    product_join_kernel<T><<<dim3(grid_row(groups), grid_rows(groups)), 256, 0, st>>>(a.e, partial, plan.splits);
+    product_join_kernel<T, Out><<<dim3(grid_row(groups), grid_rows(groups)), 256, 0, st>>>(a.e, partial, plan.splits);
     return hipGetLastError();
 }
 
-template <class T>
+// operands of type T, results, bias and residual of type Out
+template <class T, class Out = T>
 hipError_t launch_product_type(const Product &a, const ProductPlan &plan, float *partial, hipStream_t st)
 {
-    if (hipError_t e = plan.tile == kTileFew ? launch_few_tokens<T>(a, plan, partial, st) : launch_product_tiles<T>(a, plan, partial, st)) return e;
-    return plan.splits > 1 ? launch_join<T>(a, plan, partial, st) : hipSuccess;
+    if (hipError_t e = plan.tile == kTileFew ? launch_few_tokens<T, Out>(a, plan, partial, st) : launch_product_tiles<T, Out>(a, plan, partial, st)) return e;
+    return plan.splits > 1 ? launch_join<T, Out>(a, plan, partial, st) : hipSuccess;
 }
 
 template <class T, int B>

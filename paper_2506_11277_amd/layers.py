@@ -35,6 +35,8 @@ _SIGNATURES = {
     "ozimmu_linear_grad_workspace_bytes": (_size, [_int] * 6),
     "ozimmu_linear_grad": (_int, [_int] * 4 + [_ptr, _int] * 4 + [_int] + [_ptr, _int] * 2 + [_ptr, _ptr, _size, _ptr]),
     "ozimmu_moe_workspace_bytes": (_size, [_int] * 6),
+    "ozimmu_linear8_workspace_bytes": (_size, [_int] * 4),
+    "ozimmu_linear8": (_int, [_int] * 4 + [_ptr, _int, _ptr] * 2 + [_ptr, _ptr, _int, _int, _ptr, _int, _ptr, _int, _ptr, _size, _ptr]),
     "ozimmu_quantise": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _ptr]),
     "ozimmu_rms_norm": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _c.c_double, _ptr, _int, _ptr, _int, _ptr, _int, _ptr, _ptr]),
     "ozimmu_rms_norm_grad_workspace_bytes": (_size, [_int] * 2),
@@ -456,3 +458,53 @@ def rms_norm_grad(dy, total, weight=None, eps=1e-6, add=None, dx=None, dw=None, 
     if rc != OK:
         raise OzimmuError(rc, "rms_norm_grad")
     return dx, dw
+
+
+LINEAR8_IN = 131071          # at most: sums of products of codes are exact in 32 bits
+
+
+def linear8_workspace_bytes(tokens, n_in, n_out, aligned=True):
+    """Bytes of workspace for linear8; aligned: every row of x and w starts on 16 bytes."""
+    return lib().ozimmu_linear8_workspace_bytes(*_sizes(tokens, n_in, n_out), int(aligned))
+
+
+def linear8(x, x_scale, w, w_scale, bias=None, residual=None, activation=ACT_NONE, dtype=None, pre=None, out=None, workspace=None):
+    """linear with x [tokens, n_in] and w [n_out, n_in] in 8 bits: act((x * x_scale[:, None]) @ (w * w_scale[:, None]).T + bias) + residual.
+
+    x and w: int8, with float32 scales for their rows, as quantise and rms_norm8 give them.  Everything else is of one type: that of
+    `out`, `residual`, `bias` or `pre` where given, else `dtype` (bfloat16 by default)."""
+    given = next((t for t in (out, residual, bias, pre) if t is not None), None)
+    if given is None:
+        dtype = torch.bfloat16 if dtype is None else dtype
+    elif dtype is not None and dtype != given.dtype:
+        raise ValueError(f"dtype: {given.dtype} or None expected")
+    else:
+        dtype = given.dtype
+    kind, index = _TYPES.get(dtype), x.get_device()
+    if kind is None or not x.is_cuda:
+        raise ValueError("linear8: CUDA tensors and a result in bfloat16, float16 or float32 expected")
+    try:
+        (tokens, n_in), (n_out, _) = x.shape, w.shape
+    except ValueError:
+        raise ValueError("x and w: matrices expected") from None
+    if n_in > LINEAR8_IN:
+        raise ValueError(f"linear8: at most {LINEAR8_IN} input features expected, got {n_in}")
+    ldx, ldw = _ld_codes(x, tokens, n_in, index, "x"), _ld_codes(w, n_out, n_in, index, "w")
+    px, pw = _scale(x_scale, tokens, index, "x_scale"), _scale(w_scale, n_out, index, "w_scale")
+    if out is None:
+        out = torch.empty((tokens, n_out), dtype=dtype, device=x.device)
+    ldy = _ld(out, tokens, n_out, out, "out")
+    if out.get_device() != index:
+        raise ValueError(f"out: {dtype} on {x.device} expected")
+    pbias = None if bias is None else _vector(bias, n_out, out, "bias")
+    ldr = 0 if residual is None else _ld(residual, tokens, n_out, out, "residual")
+    ldp = 0 if pre is None else _ld(pre, tokens, n_out, out, "pre")
+    L = _lib or lib()
+    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear8_workspace_bytes(tokens, n_in, n_out, _aligned(x, ldx, w, ldw))
+                                  if workspace is None else 0, x.device)
+    rc = L.ozimmu_linear8(tokens, n_in, n_out, kind, x.data_ptr(), ldx, px, w.data_ptr(), ldw, pw, pbias,
+                          None if residual is None else residual.data_ptr(), ldr, activation,
+                          None if pre is None else pre.data_ptr(), ldp, out.data_ptr(), ldy, ws, nbytes, _stream(index, "linear8"))
+    if rc != OK:
+        raise OzimmuError(rc, "linear8")
+    return out

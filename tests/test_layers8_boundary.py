@@ -93,3 +93,41 @@ def test_the_binding_refuses(monkeypatch):
             call()
     with pytest.raises(layers.OzimmuError):
         layers.rms_norm(x, w, eps=0.0)
+
+
+def linear8(h, tokens=4, n_in=8, n_out=8, type=0, x=F, ldx=8, xs=F, w=F, ldw=8, ws=F, bias=None, residual=None, ldr=8, act=0, pre=None, ldpre=8, y=F, ldy=8,
+            room=None, nbytes=0):
+    return h.ozimmu_linear8(tokens, n_in, n_out, type, x, ldx, xs, w, ldw, ws, bias, residual, ldr, act, pre, ldpre, y, ldy, room, nbytes, None)
+
+
+@pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(n_in=-1), dict(n_out=-1), dict(tokens=1 << 30), dict(n_in=131072, ldx=1 << 20, ldw=1 << 20), dict(type=3), dict(type=8),
+                                   dict(act=5), dict(act=-1), dict(x=None), dict(w=None), dict(y=None), dict(xs=None), dict(ws=None), dict(xs=ODD), dict(ws=ODD), dict(ldx=7), dict(ldw=7),
+                                   dict(ldy=7), dict(y=ODD), dict(bias=ODD), dict(residual=F, ldr=7), dict(residual=ODD), dict(pre=F, ldpre=7), dict(pre=ODD)])
+def test_linear8_refuses(handle, wrong):
+    assert linear8(handle, **wrong) == BAD
+
+
+def test_linear8_workspace(handle):
+    need = handle.ozimmu_linear8_workspace_bytes
+    assert need(-1, 1, 1, 1) == 0 and need(1, 131072, 1, 1) == 0 and need(0, 0, 0, 1) == 0 and need(1 << 30, 1, 1, 1) == 0
+    sizes = [(t, i, o) for t in (1, 64, 65, 300, 1531, 8192) for i in (1, 1001, 8192, 65536) for o in (1, 777, 2048, 8192)]
+    some = [s for s in sizes if need(*s, 1) > 0 and s[1] % 16 == 0]
+    assert some
+    t, i, o = some[0]
+    assert linear8(handle, t, i, o, ldx=i, ldw=i, ldy=o) == BAD
+    assert linear8(handle, t, i, o, ldx=i, ldw=i, ldy=o, room=F, nbytes=need(t, i, o, 1) - 1) == BAD
+    assert linear8(handle, t, i, o, ldx=i, ldw=i, ldy=o, room=ctypes.c_void_p((1 << 20) + 128), nbytes=1 << 40) == BAD
+    assert need(4096, 4096, 4096, 0) >= need(4096, 4096, 4096, 1) + 2 * 4096 * 4096        # room for copies of x and w
+    assert linear8(handle, tokens=0, x=None, xs=None, y=None) == OK and linear8(handle, n_out=0, w=None, ws=None, y=None) == OK
+
+
+def test_the_binding_refuses_operands_of_linear8(monkeypatch):
+    from paper_2506_11277_amd import layers
+    x, s = bf16(4, 8, dtype=torch.int8), bf16(4, dtype=torch.float32)
+    with pytest.raises(ValueError):
+        layers.linear8(x, s, x, s)                         # not CUDA tensors
+    with pytest.raises(ValueError):
+        layers.linear8_workspace_bytes(1 << 32, 8, 8)
+    for dtype in (torch.float64, torch.int8):
+        with pytest.raises(ValueError):
+            layers.linear8(x, s, x, s, dtype=dtype)
