@@ -172,6 +172,19 @@ int ozimmu_linear8(int tokens, int n_in, int n_out, int type, const int8_t *x, i
                    const float *w_scale, const void *bias, const void *residual, int ldr, int activation, void *pre, int ldpre,
                    void *y, int ldy, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * ozimmu_linear_grad with operands that the forward pass kept in 8 bits.  x, w and pre each are of `type` where their scale is NULL, and int8_t
+ * with x_scale [tokens], w_scale [n_out], pre_scale [tokens] otherwise, standing for code * scale.  (The rounding to 8 bits is
+ * taken as the identity.)  dz = dy * act'(pre) from the unrounded values of pre; for the products dz and the values of x and w are rounded to `type`
+ * once (float16: values beyond 65504 become infinities); db is summed from the unrounded dz.
+ * Workspace: as for ozimmu_linear_grad, with room for the values of x and w that are in 8 bits (x8, w8 = 1); `aligned` of dy and of x and w that
+ * are not.
+ */
+size_t ozimmu_linear8_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation, int aligned, int x8, int w8);
+int ozimmu_linear8_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const float *x_scale,
+                        const void *w, int ldw, const float *w_scale, const void *pre, int ldpre, const float *pre_scale, int activation,
+                        void *dx, int lddx, void *dw, int lddw, void *db, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,21 @@ __device__ __forceinline__ void load8(const T *p, int n, bool wide, float (&v)[8
     }
 }
 
+// ... held in 8 bits, with their row's scale
+__device__ __forceinline__ void load8(const int8_t *p, int n, float scale, float (&v)[8])
+{
+    if (n >= 8) {
+        typedef int8_t V __attribute__((ext_vector_type(8)));
+        V x;
+        __builtin_memcpy(&x, p, 8);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)x[i] * scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] * scale : 0.0f;
+    }
+}
+
 template <class T>
 __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
 {
@@ -34,7 +49,8 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
             float d[8], z[8];
             load8((const T *)a.dy + (size_t)r * a.lddy + c, n, a.wide, d);
             if (a.act) {
-                load8((const T *)a.pre + (size_t)r * a.ldpre + c, n, a.wide, z);
+                if (a.pre_scale) load8((const int8_t *)a.pre + (size_t)r * a.ldpre + c, n, a.pre_scale[r], z);
+                else load8((const T *)a.pre + (size_t)r * a.ldpre + c, n, a.wide, z);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) d[i] *= activation_slope<T>(a.act, z[i]);
             }

@@ -31,6 +31,7 @@ struct PadCopy {
     void *to;
     long long rows;
     int cols, ld, ldto;
+    const float *scale;                    // of the rows, where `from` is held in 8 bits; else null
 };
 struct PadCopies {
     PadCopy c[2];                          // rows = 0: none
@@ -53,6 +54,7 @@ struct GradInput {
     void *dz;                              // null: only the sums
     float *sums;                           // [ceil(tokens / rows)][n_out], null: none
     int lddy, ldpre, lddz, tokens, n_out, rows, act, wide;
+    const float *pre_scale;                // of the rows of pre, where it is held in 8 bits; else null
 };
 hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st);
 hipError_t launch_bias_grad(const BiasGrad &b, int type, hipStream_t st);

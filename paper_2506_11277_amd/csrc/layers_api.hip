@@ -131,7 +131,7 @@ ProductPlan route_product(Product &a, int type, int result, bool k_rows, char *s
     if (a.nk == 0 || space == nullptr || space_bytes < p_bytes + q_bytes || direct.us + 6 + 2 * (p_bytes + q_bytes) / 4e6 >= other.us) return other;
     auto copy = [&](PadCopy &c, const void *&x, int &ld, bool rows_along_k, int &rows, int &nk, char *to) {
         int &along = rows_along_k ? nk : rows;
-        c = PadCopy{x, to, rows_along_k ? rows : nk, along, ld, up(along, size)};
+        c = PadCopy{x, to, rows_along_k ? rows : nk, along, ld, up(along, size), nullptr};
         x = to;
         ld = along = c.ldto;
     };
@@ -171,26 +171,27 @@ LinearWorkspace linear_workspace(int tokens, int n_in, int n_out, int type, bool
     return w;
 }
 
-// parts of the workspace of ozimmu_linear_grad
+// parts of the workspace of ozimmu_linear_grad and ozimmu_linear8_grad; x8, w8: held in 8 bits, and always copied
 struct GradWorkspace {
     size_t dz, sums, partial, copies_x, copies_w, total;
-    bool has_dz, has_copies;
+    bool has_dz, has_x, has_w;
     int lddz;
 };
-GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int activation, bool aligned)
+GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int activation, bool aligned, bool x8 = false, bool w8 = false)
 {
     GradWorkspace w{};
     const size_t size = element_bytes(type);
     aligned = aligned && n_in * size % 16 == 0 && n_out * size % 16 == 0;
     w.lddz = up8(n_out);
     w.has_dz = activation != OZIMMU_ACT_NONE || !aligned;
-    w.has_copies = !aligned;
+    w.has_x = x8 || !aligned;
+    w.has_w = w8 || !aligned;
     w.sums = w.has_dz ? padded((size_t)tokens * w.lddz * size) : 0;
     w.partial = w.sums + padded((size_t)((tokens + grad_rows(tokens, n_out) - 1) / grad_rows(tokens, n_out)) * n_out * 4);
     const size_t dx = either_partial_bytes(n_in, tokens, n_out, type, false), dw = either_partial_bytes(n_in, n_out, tokens, type, false);
     w.copies_x = w.partial + (dx > dw ? dx : dw);
-    w.copies_w = w.copies_x + (w.has_copies ? padded((size_t)tokens * up8(n_in) * size) : 0);
-    w.total = w.copies_w + (w.has_copies ? padded((size_t)n_out * up8(n_in) * size) : 0);
+    w.copies_w = w.copies_x + (w.has_x ? padded((size_t)tokens * up8(n_in) * size) : 0);
+    w.total = w.copies_w + (w.has_w ? padded((size_t)n_out * up8(n_in) * size) : 0);
     return w;
 }
 
@@ -230,6 +231,112 @@ int linear(int tokens, int n_in, int n_out, int type, int result, const void *x,
                          : result == OZIMMU_F16  ? launch_product8_f16(a, plan, partial, st)
                                                  : launch_product8_f32(a, plan, partial, st);
     return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+}
+
+
+// ozimmu_linear_grad and ozimmu_linear8_grad: x, w and pre of `type`, or held in 8 bits where they have scales
+int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const float *x_scale, const void *w, int ldw,
+                const float *w_scale, const void *pre, int ldpre, const float *pre_scale, int activation, void *dx, int lddx, void *dw, int lddw,
+                void *db, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU || bad_sizes(tokens, n_in, n_out)) return OZIMMU_BAD_ARG;
+    const size_t size = element_bytes(type);
+    if (bad_rows(tokens, n_out, dy, lddy, size) || (activation && bad_rows(tokens, n_out, pre, ldpre, pre_scale ? 1 : size)) || (uintptr_t)db % size) return OZIMMU_BAD_ARG;
+    if (dx && (bad_rows(tokens, n_in, dx, lddx, size) || bad_rows(n_out, n_in, w, ldw, w_scale ? 1 : size))) return OZIMMU_BAD_ARG;
+    if (dw && (bad_rows(n_out, n_in, dw, lddw, size) || bad_rows(tokens, n_in, x, ldx, x_scale ? 1 : size))) return OZIMMU_BAD_ARG;
+    const bool x8 = x_scale != nullptr, w8 = w_scale != nullptr;
+    GradWorkspace ws = grad_workspace(tokens, n_in, n_out, type, activation, true, x8, w8);
+    if (bad_workspace(workspace, workspace_bytes, ws.total)) return OZIMMU_BAD_ARG;
+    if (n_out == 0 && !dx) return OZIMMU_OK;
+    const hipStream_t st = (hipStream_t)stream;
+    char *const base = (char *)workspace;
+    // (dy of no activation is read as it is where it can be copied directly, or there is no room for dz)
+    const bool dy_fits = direct_operand(dy, lddy, n_out, size);
+    if (!dy_fits || (dx && !w8 && !direct_operand(w, ldw, n_in, size)) || (dw && !x8 && !direct_operand(x, ldx, n_in, size))) {
+        const GradWorkspace wider = grad_workspace(tokens, n_in, n_out, type, activation, false, x8, w8);
+        if (workspace_bytes >= wider.total) ws = wider;
+    }
+
+    const bool own_dz = n_out > 0 && (dx || dw) && (activation || (ws.has_dz && !dy_fits));
+    const void *dz = dy;
+    int lddz = lddy, dz_cols = n_out;
+    const int rows = grad_rows(tokens, n_out);
+    if (n_out > 0 && (db || own_dz)) {
+        GradInput g{};
+        g.dy = dy;
+        g.pre = activation ? pre : nullptr;
+        g.dz = own_dz ? base + ws.dz : nullptr;
+        g.sums = db ? (float *)(base + ws.sums) : nullptr;
+        g.lddy = lddy;
+        g.ldpre = ldpre;
+        g.lddz = ws.lddz;
+        g.tokens = tokens;
+        g.n_out = n_out;
+        g.rows = rows;
+        g.act = activation;
+        g.pre_scale = activation ? pre_scale : nullptr;
+        g.wide = on16(dy, lddy, size) && (!activation || pre_scale || on16(pre, ldpre, size));
+        if (launch_grad_input(g, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    }
+    if (own_dz) {
+        dz = base + ws.dz;
+        lddz = dz_cols = ws.lddz;
+    }
+    const BiasGrad bias{(const float *)(base + ws.sums), db, (tokens + rows - 1) / rows, n_out};
+    float *partial = (float *)(base + ws.partial);
+    Product x_grad{}, w_grad{};
+    x_grad.P = w;
+    x_grad.ldp = ldw;
+    x_grad.p_rows = n_in;
+    x_grad.p_nk = n_out;
+    x_grad.Q = dz;
+    x_grad.ldq = lddz;
+    x_grad.q_k_rows = true;
+    x_grad.q_rows = tokens;
+    x_grad.q_nk = dz_cols;
+    x_grad.nk = n_out;
+    x_grad.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
+    w_grad.P = x;
+    w_grad.ldp = ldx;
+    w_grad.p_rows = n_in;
+    w_grad.p_nk = tokens;
+    w_grad.Q = dz;
+    w_grad.ldq = lddz;
+    w_grad.q_rows = dz_cols;
+    w_grad.q_nk = tokens;
+    w_grad.nk = tokens;
+    w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
+    PadCopies x_copies{}, w_copies{}, copies{};
+    ProductPlan x_plan{}, w_plan{};
+    const bool form_dx = dx && tokens > 0 && n_in > 0, form_dw = dw && n_out > 0 && n_in > 0;
+    // what is held in 8 bits is copied as the values it stands for
+    auto expand = [&](Product &a, const float *scale, int rows_, char *to) {
+        const PadCopy c{a.P, to, rows_, n_in, a.ldp, up8(n_in), scale};
+        a.P = to;
+        a.ldp = a.p_rows = c.ldto;
+        return c;
+    };
+    PadCopy w_values{}, x_values{};
+    if (form_dx && w8) w_values = expand(x_grad, w_scale, n_out, base + ws.copies_w);
+    if (form_dw && x8) x_values = expand(w_grad, x_scale, tokens, base + ws.copies_x);
+    // (of each product P alone can want a copy here: dz is the workspace's, or dy where there is no room for either)
+    if (form_dx) x_plan = route_product(x_grad, type, type, false, ws.has_w && !w8 ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies);
+    if (form_dw) w_plan = route_product(w_grad, type, type, false, ws.has_x && !x8 ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
+    copies.c[0] = w8 ? w_values : x_copies.c[0];
+    copies.c[1] = x8 ? x_values : w_copies.c[0];
+    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    const bool both = form_dx && form_dw && n_out > 0 && tokens > 0 && x_plan.direct && w_plan.direct;
+    const int pair = both ? plan_pair(x_grad, x_plan, w_grad, w_plan, type, db != nullptr) : -1;
+    if (pair >= 0) {
+        const hipError_t e = type == OZIMMU_BF16  ? launch_pair_bf16(x_grad, w_grad, bias, pair, st)
+                             : type == OZIMMU_F16 ? launch_pair_f16(x_grad, w_grad, bias, pair, st)
+                                                  : launch_pair_f32(x_grad, w_grad, bias, pair, st);
+        return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
+    }
+    if (launch_bias_grad(bias, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (form_dx && launch_product(x_grad, x_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (form_dw && launch_product(w_grad, w_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    return OZIMMU_OK;
 }
 
 }  // namespace
@@ -300,92 +407,23 @@ int ozimmu_linear_grad(int tokens, int n_in, int n_out, int type, const void *dy
                        int ldw, const void *pre, int ldpre, int activation, void *dx, int lddx, void *dw, int lddw, void *db,
                        void *workspace, size_t workspace_bytes, void *stream)
 {
-    if (bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU || bad_sizes(tokens, n_in, n_out)) return OZIMMU_BAD_ARG;
-    const size_t size = element_bytes(type);
-    if (bad_rows(tokens, n_out, dy, lddy, size) || (activation && bad_rows(tokens, n_out, pre, ldpre, size)) || (uintptr_t)db % size) return OZIMMU_BAD_ARG;
-    if (dx && (bad_rows(tokens, n_in, dx, lddx, size) || bad_rows(n_out, n_in, w, ldw, size))) return OZIMMU_BAD_ARG;
-    if (dw && (bad_rows(n_out, n_in, dw, lddw, size) || bad_rows(tokens, n_in, x, ldx, size))) return OZIMMU_BAD_ARG;
-    GradWorkspace ws = grad_workspace(tokens, n_in, n_out, type, activation, true);
-    if (bad_workspace(workspace, workspace_bytes, ws.total)) return OZIMMU_BAD_ARG;
-    if (n_out == 0 && !dx) return OZIMMU_OK;
-    const hipStream_t st = (hipStream_t)stream;
-    char *const base = (char *)workspace;
-    // (dy of no activation is read as it is where it can be copied directly, or there is no room for dz)
-    const bool dy_fits = direct_operand(dy, lddy, n_out, size);
-    if (!dy_fits || (dx && !direct_operand(w, ldw, n_in, size)) || (dw && !direct_operand(x, ldx, n_in, size))) {
-        const GradWorkspace wider = grad_workspace(tokens, n_in, n_out, type, activation, false);
-        if (workspace_bytes >= wider.total) ws = wider;
-    }
+    return linear_grad(tokens, n_in, n_out, type, dy, lddy, x, ldx, nullptr, w, ldw, nullptr, pre, ldpre, nullptr, activation, dx, lddx, dw, lddw, db,
+                       workspace, workspace_bytes, stream);
+}
 
-    const bool own_dz = n_out > 0 && (dx || dw) && (activation || (ws.has_dz && !dy_fits));
-    const void *dz = dy;
-    int lddz = lddy, dz_cols = n_out;
-    const int rows = grad_rows(tokens, n_out);
-    if (n_out > 0 && (db || own_dz)) {
-        GradInput g{};
-        g.dy = dy;
-        g.pre = activation ? pre : nullptr;
-        g.dz = own_dz ? base + ws.dz : nullptr;
-        g.sums = db ? (float *)(base + ws.sums) : nullptr;
-        g.lddy = lddy;
-        g.ldpre = ldpre;
-        g.lddz = ws.lddz;
-        g.tokens = tokens;
-        g.n_out = n_out;
-        g.rows = rows;
-        g.act = activation;
-        g.wide = on16(dy, lddy, size) && (!activation || on16(pre, ldpre, size));
-        if (launch_grad_input(g, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    }
-    if (own_dz) {
-        dz = base + ws.dz;
-        lddz = dz_cols = ws.lddz;
-    }
-    const BiasGrad bias{(const float *)(base + ws.sums), db, (tokens + rows - 1) / rows, n_out};
-    float *partial = (float *)(base + ws.partial);
-    Product x_grad{}, w_grad{};
-    x_grad.P = w;
-    x_grad.ldp = ldw;
-    x_grad.p_rows = n_in;
-    x_grad.p_nk = n_out;
-    x_grad.Q = dz;
-    x_grad.ldq = lddz;
-    x_grad.q_k_rows = true;
-    x_grad.q_rows = tokens;
-    x_grad.q_nk = dz_cols;
-    x_grad.nk = n_out;
-    x_grad.e = Epilogue{nullptr, nullptr, nullptr, dx, 0, 0, lddx, n_in, tokens, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
-    w_grad.P = x;
-    w_grad.ldp = ldx;
-    w_grad.p_rows = n_in;
-    w_grad.p_nk = tokens;
-    w_grad.Q = dz;
-    w_grad.ldq = lddz;
-    w_grad.q_rows = dz_cols;
-    w_grad.q_nk = tokens;
-    w_grad.nk = tokens;
-    w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
-    PadCopies x_copies{}, w_copies{}, copies{};
-    ProductPlan x_plan{}, w_plan{};
-    const bool form_dx = dx && tokens > 0 && n_in > 0, form_dw = dw && n_out > 0 && n_in > 0;
-    // (of each product P alone can want a copy here: dz is the workspace's, or dy where there is no room for either)
-    if (form_dx) x_plan = route_product(x_grad, type, type, false, ws.has_copies ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies);
-    if (form_dw) w_plan = route_product(w_grad, type, type, false, ws.has_copies ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
-    copies.c[0] = x_copies.c[0];
-    copies.c[1] = w_copies.c[0];
-    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    const bool both = form_dx && form_dw && n_out > 0 && tokens > 0 && x_plan.direct && w_plan.direct;
-    const int pair = both ? plan_pair(x_grad, x_plan, w_grad, w_plan, type, db != nullptr) : -1;
-    if (pair >= 0) {
-        const hipError_t e = type == OZIMMU_BF16  ? launch_pair_bf16(x_grad, w_grad, bias, pair, st)
-                             : type == OZIMMU_F16 ? launch_pair_f16(x_grad, w_grad, bias, pair, st)
-                                                  : launch_pair_f32(x_grad, w_grad, bias, pair, st);
-        return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
-    }
-    if (launch_bias_grad(bias, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    if (form_dx && launch_product(x_grad, x_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    if (form_dw && launch_product(w_grad, w_plan, type, partial, st) != hipSuccess) return OZIMMU_HIP_ERROR;
-    return OZIMMU_OK;
+size_t ozimmu_linear8_grad_workspace_bytes(int tokens, int n_in, int n_out, int type, int activation, int aligned, int x8, int w8)
+{
+    if (bad_sizes(tokens, n_in, n_out) || bad_type(type) || activation < OZIMMU_ACT_NONE || activation > OZIMMU_ACT_SILU) return 0;
+    return grad_workspace(tokens, n_in, n_out, type, activation, aligned != 0, x8 != 0, w8 != 0).total;
+}
+
+int ozimmu_linear8_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const float *x_scale,
+                        const void *w, int ldw, const float *w_scale, const void *pre, int ldpre, const float *pre_scale, int activation,
+                        void *dx, int lddx, void *dw, int lddw, void *db, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if ((uintptr_t)x_scale % 4 || (uintptr_t)w_scale % 4 || (uintptr_t)pre_scale % 4) return OZIMMU_BAD_ARG;
+    return linear_grad(tokens, n_in, n_out, type, dy, lddy, x, ldx, x_scale, w, ldw, w_scale, pre, ldpre, pre_scale, activation, dx, lddx, dw, lddw, db,
+                       workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

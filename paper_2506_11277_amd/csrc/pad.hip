@@ -1,4 +1,5 @@
-// Copies of operands whose rows are not on 16 bytes, or do not end with a chunk of 16: aligned rows, zeros behind them.
+// Copies of operands whose rows are not on 16 bytes, or do not end with a chunk of 16: aligned rows, zeros behind them; and of operands
+// that are held in 8 bits with a scale for each row, as the values they stand for, rounded to the type of the product.
 //
 // Bound by memory: read once, written once, a chunk a thread.  Up to two operands in a launch.
 #include "layers.h"
@@ -19,7 +20,26 @@ __global__ __launch_bounds__(256) void pad_kernel(PadCopies a)
     const int chunks = c.ldto / E;
     const long long row = i / chunks;
     const int k = (int)(i - row * chunks) * E;
-    *(v4u *)((T *)c.to + row * c.ldto + k) = load_chunk((const T *)c.from + row * c.ld + k, c.cols - k);
+    T *const to = (T *)c.to + row * c.ldto + k;
+    if constexpr (sizeof(T) > 1)
+        if (c.scale) {
+            const int8_t *const from = (const int8_t *)c.from + row * c.ld + k;
+            const float scale = c.scale[row];
+            float v[E];
+            if (k + E <= c.cols) {
+                typedef int8_t V __attribute__((ext_vector_type(E)));
+                V x;
+                __builtin_memcpy(&x, from, E);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = (float)x[e] * scale;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = k + e < c.cols ? (float)from[e] * scale : 0.0f;
+            }
+            store_row(to, v);
+            return;
+        }
+    *(v4u *)to = load_chunk((const T *)c.from + row * c.ld + k, c.cols - k);
 }
 
 }  // namespace

@@ -37,6 +37,8 @@ _SIGNATURES = {
     "ozimmu_moe_workspace_bytes": (_size, [_int] * 6),
     "ozimmu_linear8_workspace_bytes": (_size, [_int] * 4),
     "ozimmu_linear8": (_int, [_int] * 4 + [_ptr, _int, _ptr] * 2 + [_ptr, _ptr, _int, _int, _ptr, _int, _ptr, _int, _ptr, _size, _ptr]),
+    "ozimmu_linear8_grad_workspace_bytes": (_size, [_int] * 8),
+    "ozimmu_linear8_grad": (_int, [_int] * 4 + [_ptr, _int] + [_ptr, _int, _ptr] * 3 + [_int] + [_ptr, _int] * 2 + [_ptr, _ptr, _size, _ptr]),
     "ozimmu_quantise": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _ptr]),
     "ozimmu_rms_norm": (_int, [_int] * 3 + [_ptr, _int, _ptr, _int, _ptr, _c.c_double, _ptr, _int, _ptr, _int, _ptr, _int, _ptr, _ptr]),
     "ozimmu_rms_norm_grad_workspace_bytes": (_size, [_int] * 2),
@@ -508,3 +510,58 @@ def linear8(x, x_scale, w, w_scale, bias=None, residual=None, activation=ACT_NON
     if rc != OK:
         raise OzimmuError(rc, "linear8")
     return out
+
+
+def linear8_grad_workspace_bytes(tokens, n_in, n_out, dtype, activation=ACT_NONE, aligned=True, x8=True, w8=False):
+    """Bytes of workspace for linear8_grad; x8, w8: which of x and w are in 8 bits; aligned: every row of dy, and of x and w that are
+    not, starts on 16 bytes."""
+    return lib().ozimmu_linear8_grad_workspace_bytes(*_sizes(tokens, n_in, n_out), _TYPES[dtype], activation, int(aligned), int(x8), int(w8))
+
+
+def linear8_grad(dy, x, w, pre=None, activation=ACT_NONE, x_scale=None, w_scale=None, pre_scale=None, bias=True, dx=None, dw=None, db=None,
+                 want=("dx", "dw"), workspace=None):
+    """Gradients (dx, dw, db) of linear8, or of linear with operands kept in 8 bits for them, from dy [tokens, n_out].
+
+    x [tokens, n_in], w [n_out, n_in] and pre [tokens, n_out] each are of dy's type, or int8 with a float32 scale for every row,
+    as quantise and rms_norm8 give them.  The rest is linear_grad's."""
+    kind, index = _type_of(dy, "dy"), dy.get_device()
+    try:
+        (tokens, n_out), (_, n_in) = dy.shape, x.shape
+    except ValueError:
+        raise ValueError("dy and x: matrices expected") from None
+
+    def held(t, scale, rows, cols, what):
+        """(row stride, scales) of an operand of either kind."""
+        if scale is None:
+            return _ld(t, rows, cols, dy, what), None
+        return _ld_codes(t, rows, cols, index, what), _scale(scale, rows, index, what + "_scale")
+
+    lddy = _ld(dy, tokens, n_out, dy, "dy")
+    ldx, pxs = held(x, x_scale, tokens, n_in, "x")
+    ldw, pws = held(w, w_scale, n_out, n_in, "w")
+    if activation != ACT_NONE and pre is None:
+        raise ValueError("pre: the values before the activation are needed")
+    ldp, pps = held(pre, pre_scale, tokens, n_out, "pre") if activation != ACT_NONE else (0, None)
+
+    def result(given, name, shape):
+        if name not in want:
+            return None
+        return torch.empty(shape, dtype=dy.dtype, device=dy.device) if given is None else given
+
+    dx, dw = result(dx, "dx", (tokens, n_in)), result(dw, "dw", (n_out, n_in))
+    db = (torch.empty(n_out, dtype=dy.dtype, device=dy.device) if db is None else db) if bias else None
+    lddx = 0 if dx is None else _ld(dx, tokens, n_in, dy, "dx")
+    lddw = 0 if dw is None else _ld(dw, n_out, n_in, dy, "dw")
+    pdb = None if db is None else _vector(db, n_out, dy, "db")
+    plain = [v for t, ld, scale in ((x, ldx, pxs), (w, ldw, pws)) if scale is None for v in (t, ld)]
+    L = _lib or lib()
+    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear8_grad_workspace_bytes(tokens, n_in, n_out, kind, activation, _aligned(dy, lddy, *plain),
+                                                                                  pxs is not None, pws is not None)
+                                  if workspace is None else 0, dy.device)
+    rc = L.ozimmu_linear8_grad(tokens, n_in, n_out, kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, pxs, w.data_ptr(), ldw, pws,
+                               pre.data_ptr() if activation != ACT_NONE else None, ldp, pps, activation,
+                               None if dx is None else dx.data_ptr(), lddx, None if dw is None else dw.data_ptr(), lddw, pdb,
+                               ws, nbytes, _stream(index, "linear8_grad"))
+    if rc != OK:
+        raise OzimmuError(rc, "linear8_grad")
+    return dx, dw, db

@@ -1,5 +1,6 @@
 """CPU-side checks of the operators on rows in 8 bits: refused arguments, sizes of workspaces, what the binding refuses."""
 import ctypes
+import itertools
 import os
 
 import pytest
@@ -131,3 +132,47 @@ def test_the_binding_refuses_operands_of_linear8(monkeypatch):
     for dtype in (torch.float64, torch.int8):
         with pytest.raises(ValueError):
             layers.linear8(x, s, x, s, dtype=dtype)
+
+
+def linear8_grad(h, tokens=4, n_in=8, n_out=8, type=0, dy=F, lddy=8, x=F, ldx=8, xs=F, w=F, ldw=8, ws=None, pre=F, ldpre=8, ps=F, act=2, dx=F, lddx=8, dw=F, lddw=8,
+                 db=F, room=F, nbytes=1 << 40):
+    return h.ozimmu_linear8_grad(tokens, n_in, n_out, type, dy, lddy, x, ldx, xs, w, ldw, ws, pre, ldpre, ps, act, dx, lddx, dw, lddw, db, room, nbytes, None)
+
+
+@pytest.mark.parametrize("wrong", [dict(tokens=-1), dict(n_in=-1), dict(n_out=1 << 30), dict(type=3), dict(type=8), dict(act=5), dict(dy=None), dict(dy=ODD), dict(lddy=7), dict(x=None),
+                                   dict(x=ODD, xs=None), dict(ldx=7), dict(xs=ODD), dict(w=None), dict(w=ODD), dict(ldw=7), dict(ws=ODD), dict(pre=None), dict(pre=ODD, ps=None), dict(ldpre=7),
+                                   dict(ps=ODD), dict(dx=ODD), dict(lddx=7), dict(dw=ODD), dict(lddw=7), dict(db=ODD), dict(room=None), dict(nbytes=0),
+                                   dict(room=ctypes.c_void_p((1 << 20) + 128))])
+def test_linear8_grad_refuses(handle, wrong):
+    assert linear8_grad(handle, **wrong) == BAD
+
+
+def test_linear8_grad_workspace(handle):
+    need, plain = handle.ozimmu_linear8_grad_workspace_bytes, handle.ozimmu_linear_grad_workspace_bytes
+    assert need(-1, 1, 1, 0, 0, 1, 1, 1) == 0 and need(1, 1, 1, 9, 0, 1, 1, 1) == 0 and need(1, 1, 1, 0, 7, 1, 1, 1) == 0
+    for tokens, n_in, n_out in itertools.product((1, 65, 1531), (8, 1001, 4096), (8, 777, 2048)):
+        for kind, size in ((0, 2), (1, 2), (2, 4)):
+            for act, aligned in itertools.product((0, 2), (0, 1)):
+                base = plain(tokens, n_in, n_out, kind, act, aligned)
+                assert need(tokens, n_in, n_out, kind, act, aligned, 0, 0) == base
+                both = need(tokens, n_in, n_out, kind, act, aligned, 1, 1)
+                assert both >= base and both >= size * n_in * (tokens + n_out)
+                assert base <= need(tokens, n_in, n_out, kind, act, aligned, 1, 0) <= both
+                given = dict(tokens=tokens, n_in=n_in, n_out=n_out, type=kind, act=act, lddy=n_out, ldx=n_in, ldw=n_in, ldpre=n_out, lddx=n_in, lddw=n_in, ws=F)
+                assert linear8_grad(handle, **given, nbytes=need(tokens, n_in, n_out, kind, act, 1, 1, 1) - 1) == BAD
+
+
+def test_the_binding_refuses_operands_of_linear8_grad(monkeypatch):
+    from paper_2506_11277_amd import layers
+    monkeypatch.setattr(layers, "_type_of", lambda x, what: layers._TYPES[x.dtype])
+    monkeypatch.setattr(layers, "_stream", lambda index, what: None)
+    dy, w, x = bf16(4, 6), bf16(6, 8), bf16(4, 8)
+    x8, s, p8 = bf16(4, 8, dtype=torch.int8), bf16(4, dtype=torch.float32), bf16(4, 6, dtype=torch.int8)
+    for call in (lambda: layers.linear8_grad(dy, x8, w), lambda: layers.linear8_grad(dy, x, w, x_scale=s), lambda: layers.linear8_grad(dy, x8, w, x_scale=s[:3]),
+                 lambda: layers.linear8_grad(dy, x8, w, x_scale=s.double()), lambda: layers.linear8_grad(dy, x8, w, w_scale=s, x_scale=s),
+                 lambda: layers.linear8_grad(dy, x8, w, None, layers.ACT_GELU, x_scale=s), lambda: layers.linear8_grad(dy, x8, w, p8, layers.ACT_GELU, x_scale=s),
+                 lambda: layers.linear8_grad(dy, x8, w, dy, layers.ACT_GELU, x_scale=s, pre_scale=s), lambda: layers.linear8_grad(dy, x8, w, p8[:, :5], layers.ACT_GELU, x_scale=s, pre_scale=s),
+                 lambda: layers.linear8_grad(dy, x8, w[:, :7], x_scale=s), lambda: layers.linear8_grad(dy, x8, w, x_scale=s, dx=bf16(4, 7)),
+                 lambda: layers.linear8_grad_workspace_bytes(8, 1 << 32, 8, torch.bfloat16)):
+        with pytest.raises(ValueError):
+            call()
