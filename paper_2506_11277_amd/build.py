@@ -14,7 +14,7 @@ HEADERS = [os.path.join(CSRC, "oz_common.h"), os.path.join(CSRC, "gemm_dev.h"), 
 # what only the feed-forward operators' sources include
 LAYER_SOURCES = SOURCES[SOURCES.index("layers_api.hip"):]
 LAYER_HEADERS = [os.path.join(CSRC, "layers.h"), os.path.join(CSRC, "layers_dev.h"), os.path.join(CSRC, "product_dev.h"),
-                 os.path.join(CSRC, "stream_dev.h"), os.path.join(CSRC, "few_dev.h"), os.path.join(CSRC, "norm_dev.h"),
+                 os.path.join(CSRC, "stream_dev.h"), os.path.join(CSRC, "few_dev.h"), os.path.join(CSRC, "norm_dev.h"), os.path.join(CSRC, "pad_dev.h"),
                  os.path.join(HERE, "..", "include", "ozimmu_layers.h")]
 
 HIPCC_FLAGS = [

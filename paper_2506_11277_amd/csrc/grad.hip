@@ -4,7 +4,7 @@
 // owns 512 columns of grad_rows() tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
 // work-group of tokens, with the products of dx and dw or in a kernel of their own, always in the same order.
 // 8192 x 8192 bf16 with gelu, 403 MB: 74 us, 5.4 TB/s (the library's erf: 110).
-#include "layers.h"
+#include "pad_dev.h"
 
 namespace oz {
 namespace {
@@ -35,17 +35,26 @@ __device__ __forceinline__ void load8(const int8_t *p, int n, float scale, float
     }
 }
 
+// dz of operands in 16 bits, x or w of which is held in 8: dz m[t] n[o] with the m and n of their scales' (split_scale), which leaves
+// the operands exact and the products' rows to be divided by m[t] (dx) and n[o] (dw).
 template <class T>
-__global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
+__device__ __forceinline__ void grad_input(const GradInput &a, int strip, int group, float (*part)[512])
 {
-    __shared__ float part[4][512];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int c = blockIdx.x * 512 + lane * 8, n = a.n_out - c;
-    const int first = blockIdx.y * a.rows, last = first + a.rows < a.tokens ? first + a.rows : a.tokens;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int c = strip * 512 + lane * 8, n = a.n_out - c;
+    const long long first = (long long)group * a.rows, last = first + a.rows < a.tokens ? first + a.rows : a.tokens;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, factor[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        factor[i] = 1.0f;
+        if (a.w_scale && i < n) {
+            factor[i] = split_scale(a.w_scale[c + i]).m;
+            if (group == 0 && wave == 0) a.w_inverse[c + i] = 1.0f / factor[i];
+        }
+    }
     if (n > 0)
 #pragma unroll 2
-        for (int r = first + wave; r < last; r += 4) {
+        for (long long r = first + wave; r < last; r += 4) {
             float d[8], z[8];
             load8((const T *)a.dy + (size_t)r * a.lddy + c, n, a.wide, d);
             if (a.act) {
@@ -57,6 +66,15 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += d[i];
             if (a.dz) {
+                if (a.x_scale) {
+                    const float m = split_scale(a.x_scale[r]).m;
+                    if (strip == 0 && lane == 0) a.x_inverse[r] = 1.0f / m;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] *= m * factor[i];
+                } else if (a.w_scale) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i] *= factor[i];
+                }
                 T *to = (T *)a.dz + (size_t)r * a.lddz + c;
                 store_row(to, d);                           // (rows of dz are the workspace's, on 16 bytes, zeros behind them)
             }
@@ -65,8 +83,18 @@ __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a)
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[wave][lane * 8 + i] = sum[i];
     __syncthreads();
-    for (int i = threadIdx.x; i < 512 && blockIdx.x * 512 + i < a.n_out; i += 256)
-        a.sums[(size_t)blockIdx.y * a.n_out + blockIdx.x * 512 + i] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+    for (int i = threadIdx.x; i < 512 && strip * 512 + i < a.n_out; i += 256)
+        a.sums[(size_t)group * a.n_out + strip * 512 + i] = (part[0][i] + part[1][i]) + (part[2][i] + part[3][i]);
+}
+
+// ... and the copies that the products want, in one launch
+template <class T>
+__global__ __launch_bounds__(256) void grad_input_kernel(GradInput a, PadCopies copies, int strips, long long blocks)
+{
+    __shared__ float part[4][512];
+    const long long b = (long long)blockIdx.y * kGridRow + blockIdx.x;
+    if (b < blocks) grad_input<T>(a, (int)(b % strips), (int)(b / strips), part);
+    else pad_chunk<T>(copies, (b - blocks) * 256 + threadIdx.x);
 }
 
 template <class T>
@@ -77,20 +105,20 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(BiasGrad b)
 }
 
 template <class T>
-hipError_t launch(const GradInput &g, hipStream_t st)
+hipError_t launch(const GradInput &g, const PadCopies &copies, int type, hipStream_t st)
 {
-    const int groups = (g.tokens + g.rows - 1) / g.rows;
-    if (groups == 0) return hipSuccess;
-    if (groups > 65535) return hipErrorInvalidValue;
-    grad_input_kernel<T><<<dim3((g.n_out + 511) / 512, groups), 256, 0, st>>>(g);
+    const int strips = (int)((g.n_out + 511LL) / 512);
+    const long long blocks = g.dz || g.sums ? (long long)strips * ((g.tokens + (long long)g.rows - 1) / g.rows) : 0, all = blocks + pad_groups(copies, type);
+    if (all == 0) return hipSuccess;
+    grad_input_kernel<T><<<dim3(grid_row(all), grid_rows(all)), 256, 0, st>>>(g, copies, strips, blocks);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st)
+hipError_t launch_grad_input(const GradInput &g, const PadCopies &copies, int type, hipStream_t st)
 {
-    return type == OZIMMU_BF16 ? launch<bf16>(g, st) : type == OZIMMU_F16 ? launch<f16>(g, st) : launch<float>(g, st);
+    return type == OZIMMU_BF16 ? launch<bf16>(g, copies, type, st) : type == OZIMMU_F16 ? launch<f16>(g, copies, type, st) : launch<float>(g, copies, type, st);
 }
 
 hipError_t launch_bias_grad(const BiasGrad &b, int type, hipStream_t st)

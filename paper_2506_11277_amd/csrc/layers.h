@@ -55,8 +55,12 @@ struct GradInput {
     float *sums;                           // [ceil(tokens / rows)][n_out], null: none
     int lddy, ldpre, lddz, tokens, n_out, rows, act, wide;
     const float *pre_scale;                // of the rows of pre, where it is held in 8 bits; else null
+    // scales whose m goes into dz, null: none; 1 / m of the tokens and of the output features
+    const float *x_scale, *w_scale;
+    float *x_inverse, *w_inverse;
 };
-hipError_t launch_grad_input(const GradInput &g, int type, hipStream_t st);
+// (neither dz nor sums: the copies alone)
+hipError_t launch_grad_input(const GradInput &g, const PadCopies &copies, int type, hipStream_t st);
 hipError_t launch_bias_grad(const BiasGrad &b, int type, hipStream_t st);
 
 // a mixture-of-experts layer on a few tokens (moe.hip)

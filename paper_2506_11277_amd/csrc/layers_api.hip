@@ -173,8 +173,8 @@ LinearWorkspace linear_workspace(int tokens, int n_in, int n_out, int type, bool
 
 // parts of the workspace of ozimmu_linear_grad and ozimmu_linear8_grad; x8, w8: held in 8 bits, and always copied
 struct GradWorkspace {
-    size_t dz, sums, partial, copies_x, copies_w, total;
-    bool has_dz, has_x, has_w;
+    size_t dz, sums, inverse_x, inverse_w, partial, copies_x, copies_w, total;
+    bool has_dz, has_x, has_w, split;          // split: scales go into dz and the results' rows by parts (split_scale)
     int lddz;
 };
 GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int activation, bool aligned, bool x8 = false, bool w8 = false)
@@ -183,11 +183,14 @@ GradWorkspace grad_workspace(int tokens, int n_in, int n_out, int type, int acti
     const size_t size = element_bytes(type);
     aligned = aligned && n_in * size % 16 == 0 && n_out * size % 16 == 0;
     w.lddz = up8(n_out);
-    w.has_dz = activation != OZIMMU_ACT_NONE || !aligned;
+    w.split = (x8 || w8) && size == 2;
+    w.has_dz = activation != OZIMMU_ACT_NONE || !aligned || w.split;
     w.has_x = x8 || !aligned;
     w.has_w = w8 || !aligned;
     w.sums = w.has_dz ? padded((size_t)tokens * w.lddz * size) : 0;
-    w.partial = w.sums + padded((size_t)((tokens + grad_rows(tokens, n_out) - 1) / grad_rows(tokens, n_out)) * n_out * 4);
+    w.inverse_x = w.sums + padded((size_t)((tokens + grad_rows(tokens, n_out) - 1) / grad_rows(tokens, n_out)) * n_out * 4);
+    w.inverse_w = w.inverse_x + (w.split && x8 ? padded((size_t)tokens * 4) : 0);
+    w.partial = w.inverse_w + (w.split && w8 ? padded((size_t)n_out * 4) : 0);
     const size_t dx = either_partial_bytes(n_in, tokens, n_out, type, false), dw = either_partial_bytes(n_in, n_out, tokens, type, false);
     w.copies_x = w.partial + (dx > dw ? dx : dw);
     w.copies_w = w.copies_x + (w.has_x ? padded((size_t)tokens * up8(n_in) * size) : 0);
@@ -233,7 +236,6 @@ int linear(int tokens, int n_in, int n_out, int type, int result, const void *x,
     return e == hipSuccess ? OZIMMU_OK : OZIMMU_HIP_ERROR;
 }
 
-
 // ozimmu_linear_grad and ozimmu_linear8_grad: x, w and pre of `type`, or held in 8 bits where they have scales
 int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int lddy, const void *x, int ldx, const float *x_scale, const void *w, int ldw,
                 const float *w_scale, const void *pre, int ldpre, const float *pre_scale, int activation, void *dx, int lddx, void *dw, int lddw,
@@ -257,12 +259,14 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
         if (workspace_bytes >= wider.total) ws = wider;
     }
 
-    const bool own_dz = n_out > 0 && (dx || dw) && (activation || (ws.has_dz && !dy_fits));
+    // (also where only one of dx and dw is wanted: either has the same bits alone)
+    const bool split_x = ws.split && x8, split_w = ws.split && w8;
+    const bool own_dz = n_out > 0 && (dx || dw) && (activation || split_x || split_w || (ws.has_dz && !dy_fits));
     const void *dz = dy;
     int lddz = lddy, dz_cols = n_out;
     const int rows = grad_rows(tokens, n_out);
+    GradInput g{};
     if (n_out > 0 && (db || own_dz)) {
-        GradInput g{};
         g.dy = dy;
         g.pre = activation ? pre : nullptr;
         g.dz = own_dz ? base + ws.dz : nullptr;
@@ -276,7 +280,14 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
         g.act = activation;
         g.pre_scale = activation ? pre_scale : nullptr;
         g.wide = on16(dy, lddy, size) && (!activation || pre_scale || on16(pre, ldpre, size));
-        if (launch_grad_input(g, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+        if (own_dz && split_x) {
+            g.x_scale = x_scale;
+            g.x_inverse = (float *)(base + ws.inverse_x);
+        }
+        if (own_dz && split_w) {
+            g.w_scale = w_scale;
+            g.w_inverse = (float *)(base + ws.inverse_w);
+        }
     }
     if (own_dz) {
         dz = base + ws.dz;
@@ -306,6 +317,8 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
     w_grad.q_nk = tokens;
     w_grad.nk = tokens;
     w_grad.e = Epilogue{nullptr, nullptr, nullptr, dw, 0, 0, lddw, n_in, n_out, OZIMMU_ACT_NONE, nullptr, nullptr, 0};
+    x_grad.e.q_scale = g.x_inverse;
+    w_grad.e.q_scale = tokens > 0 ? g.w_inverse : nullptr;         // (which a token's launch writes)
     PadCopies x_copies{}, w_copies{}, copies{};
     ProductPlan x_plan{}, w_plan{};
     const bool form_dx = dx && tokens > 0 && n_in > 0, form_dw = dw && n_out > 0 && n_in > 0;
@@ -324,7 +337,7 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
     if (form_dw) w_plan = route_product(w_grad, type, type, false, ws.has_x && !x8 ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
     copies.c[0] = w8 ? w_values : x_copies.c[0];
     copies.c[1] = x8 ? x_values : w_copies.c[0];
-    if (launch_pad(copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
+    if (launch_grad_input(g, copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;
     const bool both = form_dx && form_dw && n_out > 0 && tokens > 0 && x_plan.direct && w_plan.direct;
     const int pair = both ? plan_pair(x_grad, x_plan, w_grad, w_plan, type, db != nullptr) : -1;
     if (pair >= 0) {

@@ -165,7 +165,8 @@ struct Epilogue {
     int ldr, ldpre, ldo;
     int np, nq;
     int act;
-    const float *q_scale, *p_scale;       // operands of 8 bits: the rows' scales; sum * q_scale[q] * p_scale[p] takes the sum's place
+    // operands of 8 bits: the rows' scales, sum * q_scale[q] * p_scale[p] takes the sum's place; gradients: sum * q_scale[q], where it is not null
+    const float *q_scale, *p_scale;
     int wide;                             // every row of 8 entries that starts at a multiple of 8 is aligned to its size, up to 16 bytes
 };
 
@@ -205,12 +206,12 @@ __device__ __forceinline__ void stream_row(T *p, const float (&v)[N])
     }
 }
 
-// The sum of operands of type T, scaled: the whole number to the nearest float, two products.
+// The sum of operands of type T, scaled: of 8 bits the whole number to the nearest float, two products.
 template <class T>
 __device__ __forceinline__ float scaled(float sum, float q_scale, float p_scale)
 {
     if constexpr (sizeof(T) == 1) return (float)__float_as_int(sum) * q_scale * p_scale;
-    else return sum;
+    else return sum * q_scale;
 }
 
 // N = 8 (p a multiple of 8) entries of row q: sums of operands of type S, results of type T
@@ -221,6 +222,10 @@ __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, floa
         const float x = e.q_scale[q];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = scaled<S>(v[i], x, p + i < e.np ? e.p_scale[p + i] : 0.0f);
+    } else if (e.q_scale) {
+        const float x = e.q_scale[q];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= x;
     }
     if (e.wide && p + 8 <= e.np) {
         float t[8];
@@ -257,6 +262,17 @@ __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, floa
             ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)x;
         }
     }
+}
+
+// A scale as m 2^e, 1 <= m < 2, and its sign with the power: code * power is exact in 16 bits (8 binary digits; float16: where it is in its range),
+// so that of an operand held in 8 bits only m has to go elsewhere.  Scales that are 0 or not finite stay whole.
+struct SplitScale {
+    float m, power;
+};
+__device__ __forceinline__ SplitScale split_scale(float s)
+{
+    if (s == 0.0f || !(fabsf(s) < __uint_as_float(0x7f800000u))) return SplitScale{1.0f, s};
+    return SplitScale{2.0f * fabsf(__builtin_amdgcn_frexp_mantf(s)), __builtin_ldexpf(s < 0.0f ? -1.0f : 1.0f, __builtin_amdgcn_frexp_expf(s) - 1)};
 }
 
 // ---- launchers, one set per element type (product_bf16.hip, product_f16.hip, product_f32.hip)

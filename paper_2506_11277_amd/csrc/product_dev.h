@@ -264,8 +264,8 @@ __device__ __forceinline__ void load_columns(const Epilogue &e, int p0, int lane
     }
 }
 
-// rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time
-template <class T, class Out, int ACT, int PW, int QW>
+// rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time.  QS: rows may have a scale
+template <class T, class Out, bool QS, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, R = QW / ROWS < 4 ? QW / ROWS : 4;
@@ -291,10 +291,12 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
                 if (q0 + s + y * ROWS < e.nq) store_row(partial + ((size_t)blockIdx.y * e.nq + q0 + s + y * ROWS) * ldn + p, v[y]);
             continue;
         }
-        float x[sizeof(T) == 1 ? R : 1];
-        if constexpr (sizeof(T) == 1)
+        float x[R];
 #pragma unroll
-            for (int y = 0; y < R; ++y) x[y] = q0 + s + y * ROWS < e.nq ? e.q_scale[q0 + s + y * ROWS] : 0.0f;
+        for (int y = 0; y < R; ++y) {
+            x[y] = 1.0f;
+            if (QS && (sizeof(T) == 1 || e.q_scale) && q0 + s + y * ROWS < e.nq) x[y] = e.q_scale[q0 + s + y * ROWS];
+        }
         if (e.residual)
 #pragma unroll
             for (int y = 0; y < R; ++y)
@@ -304,7 +306,7 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
             const int q = q0 + s + y * ROWS;
             if (q >= e.nq) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[y][i] = scaled<T>(v[y][i], x[sizeof(T) == 1 ? y : 0], columns.scale[sizeof(T) == 1 ? i : 0]) + columns.bias[i];
+            for (int i = 0; i < 8; ++i) v[y][i] = scaled<T>(v[y][i], x[y], columns.scale[sizeof(T) == 1 ? i : 0]) + columns.bias[i];
             if (e.pre) write((Out *)e.pre + (size_t)q * e.ldpre + p, v[y]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[y][i] = activate<Out>(ACT, v[y][i]);
@@ -319,7 +321,7 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
 // ... entry by entry, where rows are not aligned or end within 8 entries: consecutive lanes take consecutive entries, four
 // rows at a time; all 16 of a lane in a 64 x 64 tile (1531 x 1008 x 777 f16 with a residual 11.8 us against 12.2; in a 128 x 128
 // tile more than four are slower, 4097 x 1024 x 4095 f16 166 us against 155)
-template <class T, class Out, int ACT, int PW, int QW>
+template <class T, class Out, bool QS, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float *sums, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, W = PW < 64 ? PW : 64, ROWS = 64 / W, R = PW == 32 ? 16 : 4;
@@ -335,7 +337,7 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
 #pragma unroll
             for (int y = 0; y < R; ++y) {
                 const int q = q0 + s + y * ROWS;
-                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], sizeof(T) == 1 && q < e.nq ? e.q_scale[q] : 0.0f, p_scale) + bias;
+                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], QS && (sizeof(T) == 1 || e.q_scale) && q < e.nq ? e.q_scale[q] : 1.0f, p_scale) + bias;
                 res[y] = e.residual && q < e.nq ? (float)((const Out *)e.residual)[(size_t)q * e.ldr + p] : 0.0f;
             }
 #pragma unroll
@@ -351,23 +353,23 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
     }
 }
 
-template <class T, class Out, int ACT, int PW, int QW>
+template <class T, class Out, bool QS, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
 {
-    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, Out, ACT, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-    else epilogue_entries<T, Out, ACT, PW, QW>(e, sums, q0, p0, lane);
+    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, Out, QS, ACT, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+    else epilogue_entries<T, Out, QS, ACT, PW, QW>(e, sums, q0, p0, lane);
 }
 
-template <class T, class Out, int PW, int QW>
+template <class T, class Out, bool QS, int PW, int QW>
 __device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
 {
     switch (e.act) {                                // (decided once: a lane's entries decide nothing)
-        case OZIMMU_ACT_RELU: return epilogue_as<T, Out, OZIMMU_ACT_RELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU: return epilogue_as<T, Out, OZIMMU_ACT_GELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, Out, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-        case OZIMMU_ACT_SILU: return epilogue_as<T, Out, OZIMMU_ACT_SILU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_RELU: return epilogue_as<T, Out, QS, OZIMMU_ACT_RELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU: return epilogue_as<T, Out, QS, OZIMMU_ACT_GELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, Out, QS, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_SILU: return epilogue_as<T, Out, QS, OZIMMU_ACT_SILU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
     }
-    epilogue_as<T, Out, OZIMMU_ACT_NONE, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+    epilogue_as<T, Out, QS, OZIMMU_ACT_NONE, PW, QW>(e, partial, columns, sums, q0, p0, lane);
 }
 
 // one tile, or one part of its contraction
@@ -542,7 +544,7 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
             }
         });
         __builtin_amdgcn_wave_barrier();
-        epilogue<T, Out, S::kPW, S::kSQ>(a.e, partial, columns, sums, q0 + h * S::kSQ, p0, lane);
+        epilogue<T, Out, sizeof(T) == 1 || !PK, S::kPW, S::kSQ>(a.e, partial, columns, sums, q0 + h * S::kSQ, p0, lane);
         __builtin_amdgcn_wave_barrier();
     }
 }

@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 
 from paper_2506_11277_amd import layers
 from tests.eight_reference import guarded_codes
-from tests.layers_reference import ROUND, TYPES, U32, act, guarded, product_bound, rounded, slope, sum_bound, untouched, within
+from tests.layers_reference import LEAST, ROUND, TYPES, U32, act, guarded, product_bound, rounded, slope, sum_bound, untouched, within
 
 ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 HELD = [(True, False, True), (True, True, True), (True, False, False), (False, True, False), (False, False, True), (False, False, False)]   # x, w, pre
@@ -42,16 +42,16 @@ def check(got, dy, x, w, pre, name, kind, held):
     dx, dw, db = got
     G = dy.double()
     dz = G * slope(name, pre)
-    # pre's product with its scale and the slope in 32 bits, then one rounding of dz for the products
+    # pre's product with its scale and the slope in 32 bits, then one rounding of dz for the products (behind two products with parts of scales)
     sb = 0 if name in ("none", "relu") else 32 * U32 * G.abs() * (1 + pre.abs()) ** 2
-    zb = sb + (0 if name == "none" else rounded(dz, dtype))
-    # what is held in 8 bits: the product with the scale in 32 bits, and its rounding to the type of the product
-    xb, wb = ((U32 * v.abs() + rounded(v, dtype)) * (1 + u) if h else None for v, h in ((x, held[0]), (w, held[1])))
+    zb = sb + (0 if name == "none" and (kind == "f32" or not (held[0] or held[1])) else rounded(dz, dtype) + 4 * U32 * dz.abs())
+    # what is held in 8 bits: in 32 bits the product with the scale, in 16 nothing but float16's least numbers (times the scale's other part, below 2)
+    xb, wb = ((U32 * v.abs() if kind == "f32" else torch.full_like(v, 2 * LEAST[dtype])) if h else None for v, h in ((x, held[0]), (w, held[1])))
     for out, P, Q, PB, QB, what in ((dx, dz, w.t(), zb, None if wb is None else wb.t(), "dx"), (dw, dz.t(), x.t(), zb.t() if torch.is_tensor(zb) else zb, None if xb is None else xb.t(), "dw")):
         if out is None:
             continue
         want = torch.matmul(P, Q.t())
-        bound = product_bound(P, Q, 2 * U32)
+        bound = product_bound(P, Q, 2 * U32) + 4 * U32 * want.abs()
         if torch.is_tensor(PB):
             bound = bound + torch.matmul(PB, Q.abs().t())
         if QB is not None:
@@ -136,6 +136,29 @@ def test_a_scale_that_is_not_finite():
     assert bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(dw).all()) and bool(torch.isnan(db).all())
     keep = [i for i in range(40) if i != 3]
     assert torch.equal(dx[keep], got[0][keep])
+
+
+def test_scales_of_any_size():
+    # zeros, powers of two, scales below the normal numbers and negative ones stand for what they are; codes of -128 too
+    gen = generator(3)
+    x8, w8 = (torch.randint(-128, 128, (rows, 40), dtype=torch.int8, device="cuda", generator=gen) for rows in (70, 24))
+    xs, ws = torch.rand(70, device="cuda", generator=gen) + 0.5, torch.rand(24, device="cuda", generator=gen) - 0.5
+    xs[0], xs[1], xs[2], xs[3], xs[4], xs[5] = 0.0, 1.0, 2.0 ** -30, -3.0, 2.0 ** -140, 1e30
+    ws[0], ws[1] = 0.0, 2.0 ** 20
+    for kind in ("bf16", "f32"):
+        dy = torch.randn(70, 24, device="cuda", generator=gen).to(TYPES[kind])
+        X, W = x8.double() * xs.double()[:, None], w8.double() * ws.double()[:, None]
+        check(layers.linear8_grad(dy, x8, w8, x_scale=xs, w_scale=ws), dy, X, W, torch.zeros(70, 24, device="cuda").double(), "none", kind, (True, True, False))
+
+
+def test_no_tokens_and_no_features():
+    for kind in TYPES:
+        one = torch.ones(24, device="cuda")
+        w8 = torch.ones(24, 40, dtype=torch.int8, device="cuda")
+        dx, dw, db = layers.linear8_grad(torch.empty(0, 24, dtype=TYPES[kind], device="cuda"), torch.empty(0, 40, dtype=torch.int8, device="cuda"), w8, x_scale=one[:0], w_scale=one)
+        assert dx.shape == (0, 40) and bool((dw == 0).all()) and bool((db == 0).all())
+        dx, dw, db = layers.linear8_grad(torch.empty(24, 0, dtype=TYPES[kind], device="cuda"), w8, w8[:0], x_scale=one, w_scale=one[:0])
+        assert bool((dx == 0).all()) and dw.shape == (0, 40) and db.shape == (0,)
 
 
 class Block:
