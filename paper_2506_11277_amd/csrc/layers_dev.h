@@ -132,6 +132,30 @@ __device__ __forceinline__ float activate(int act, float z)
     return z;
 }
 
+// ... of a product of operands S.  Where these are of 8 bits the product takes half as long, and 67 million gelus of results in 16 bits a quarter
+// of its time (8192 x 4096 x 8192: 276 us, 237 without).  There Phi(-|z|) = 2^p(|z|) with one polynomial, fitted for the least error of p up to 5: 4e-6
+// of the value up to 4, 1e-5 up to 6, and 6e-7 of y at most; beyond, p runs away to minus infinity, faster than the logarithm.
+// y = max(z, 0) - |z| Phi(-|z|) (an infinite |z| is taken as a large one, or 0 would have to outweigh it).
+template <class S, class T>
+__device__ __forceinline__ float activate_sum(int act, float z)
+{
+    if constexpr (sizeof(S) == 1 && sizeof(T) == 2) {
+        if (act == OZIMMU_ACT_GELU) {
+            const float x = fabsf(z);
+            float p = -1.8195439679402625e-06f;
+            p = __builtin_fmaf(p, x, 6.133275019237772e-05f);
+            p = __builtin_fmaf(p, x, -0.00092875468544662f);
+            p = __builtin_fmaf(p, x, 0.00850219652056694f);
+            p = __builtin_fmaf(p, x, -0.053950950503349304f);
+            p = __builtin_fmaf(p, x, -0.4584710896015167f);
+            p = __builtin_fmaf(p, x, -1.1512492895126343f);
+            p = __builtin_fmaf(p, x, -0.9999953508377075f);
+            return __builtin_fmaf(-fminf(x, 0x1p100f), __builtin_amdgcn_exp2f(p), fmaxf(z, 0.0f));
+        }
+    }
+    return activate<T>(act, z);
+}
+
 // ... and their slopes
 template <class T>
 __device__ __forceinline__ float activation_slope(int act, float z)
@@ -206,38 +230,42 @@ __device__ __forceinline__ void stream_row(T *p, const float (&v)[N])
     }
 }
 
-// The sum of operands of type T, scaled: of 8 bits the whole number to the nearest float, two products.
+// The sum of operands of type T, scaled, and the bias: of 8 bits the whole number to the nearest float, its product with the token's scale, and that
+// with the feature's together with the bias, each rounded once.
 template <class T>
-__device__ __forceinline__ float scaled(float sum, float q_scale, float p_scale)
+__device__ __forceinline__ float scaled(float sum, float q_scale, float p_scale, float bias)
 {
-    if constexpr (sizeof(T) == 1) return (float)__float_as_int(sum) * q_scale * p_scale;
-    else return sum * q_scale;
+    if constexpr (sizeof(T) == 1) return __builtin_fmaf((float)__float_as_int(sum) * q_scale, p_scale, bias);
+    else return sum * q_scale + bias;
 }
 
 // N = 8 (p a multiple of 8) entries of row q: sums of operands of type S, results of type T
 template <class S, class T = S>
 __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, float (&v)[8])
 {
-    if constexpr (sizeof(S) == 1) {
-        const float x = e.q_scale[q];
+    if constexpr (sizeof(S) > 1)
+        if (e.q_scale) {
+            const float x = e.q_scale[q];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = scaled<S>(v[i], x, p + i < e.np ? e.p_scale[p + i] : 0.0f);
-    } else if (e.q_scale) {
-        const float x = e.q_scale[q];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= x;
-    }
+            for (int i = 0; i < 8; ++i) v[i] *= x;
+        }
+    const float x = sizeof(S) == 1 ? e.q_scale[q] : 1.0f;
     if (e.wide && p + 8 <= e.np) {
-        float t[8];
-        if (e.bias) {
-            load_row((const T *)e.bias + p, t);
+        float t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (e.bias) load_row((const T *)e.bias + p, t);
+        if constexpr (sizeof(S) == 1) {
+            float scale[8];
+            load_row(e.p_scale + p, scale);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = scaled<S>(v[i], x, scale[i], t[i]);
+        } else if (e.bias) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += t[i];
         }
         if (e.pre) store_row((T *)e.pre + (size_t)q * e.ldpre + p, v);
         if (e.act)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate<T>(e.act, v[i]);
+            for (int i = 0; i < 8; ++i) v[i] = activate_sum<S, T>(e.act, v[i]);
         if (e.residual) {
             load_row((const T *)e.residual + (size_t)q * e.ldr + p, t);
 #pragma unroll
@@ -255,11 +283,12 @@ __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, floa
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (p + i >= e.np) continue;
-            float x = v[i] + b[i];
-            if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)x;
-            x = activate<T>(e.act, x);
-            if (e.residual) x += r[i];
-            ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)x;
+            float z = v[i] + b[i];
+            if constexpr (sizeof(S) == 1) z = scaled<S>(v[i], x, e.p_scale[p + i], b[i]);
+            if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)z;
+            z = activate_sum<S, T>(e.act, z);
+            if (e.residual) z += r[i];
+            ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)z;
         }
     }
 }

@@ -306,10 +306,10 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
             const int q = q0 + s + y * ROWS;
             if (q >= e.nq) continue;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[y][i] = scaled<T>(v[y][i], x[y], columns.scale[sizeof(T) == 1 ? i : 0]) + columns.bias[i];
+            for (int i = 0; i < 8; ++i) v[y][i] = scaled<T>(v[y][i], x[y], columns.scale[sizeof(T) == 1 ? i : 0], columns.bias[i]);
             if (e.pre) write((Out *)e.pre + (size_t)q * e.ldpre + p, v[y]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[y][i] = activate<Out>(ACT, v[y][i]);
+            for (int i = 0; i < 8; ++i) v[y][i] = activate_sum<T, Out>(ACT, v[y][i]);
             if (e.residual)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[y][i] += res[y][i];
@@ -337,7 +337,7 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
 #pragma unroll
             for (int y = 0; y < R; ++y) {
                 const int q = q0 + s + y * ROWS;
-                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], QS && (sizeof(T) == 1 || e.q_scale) && q < e.nq ? e.q_scale[q] : 1.0f, p_scale) + bias;
+                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], QS && (sizeof(T) == 1 || e.q_scale) && q < e.nq ? e.q_scale[q] : 1.0f, p_scale, bias);
                 res[y] = e.residual && q < e.nq ? (float)((const Out *)e.residual)[(size_t)q * e.ldr + p] : 0.0f;
             }
 #pragma unroll
@@ -345,7 +345,7 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
                 const int q = q0 + s + y * ROWS;
                 if (q >= e.nq) continue;
                 if (e.pre) ((Out *)e.pre)[(size_t)q * e.ldpre + p] = (Out)v[y];
-                float x = activate<Out>(ACT, v[y]);
+                float x = activate_sum<T, Out>(ACT, v[y]);
                 if (e.residual) x += res[y];
                 ((Out *)e.out)[(size_t)q * e.ldo + p] = (Out)x;
             }

@@ -55,8 +55,11 @@ def check(x, xs, w, ws, bias, residual, name, y, pre):
     if pre is not None:
         within(pre, z, zb + rounded(z, dtype) + ROUND[dtype] * zb, "pre")
     a = act(name, z)
-    # the slope of every activation is below 1.13; evaluated in 32 bits, whose exponential is off by a few units times its argument
+    # the slope of every activation is below 1.13; evaluated in 32 bits, whose exponential is off by a few units times its argument; gelu in 16 bits
+    # by a polynomial: |z| Phi(-|z|) to 4e-6 up to 4 and 1e-5 up to 6, behind which it is below 6e-9
     ab = 1.2 * zb + (0 if name in ("none", "relu") else 16 * U32 * (a.abs() + z.abs() * (1 + z.abs()).clamp_max(8)))
+    if name == "gelu" and dtype is not torch.float32:
+        ab = ab + torch.where(z.abs() <= 4, 4e-6, 1e-5) * (z.abs() * torch.special.ndtr(-z.abs())) + 6e-9 * (z.abs() > 6)
     Y = a if residual is None else a + residual.double()
     ab = ab + (0 if residual is None else U32 * (Y.abs() + ab))
     within(y, Y, ab + rounded(Y, dtype) + ROUND[dtype] * ab, "y")
@@ -202,3 +205,23 @@ def test_other_streams_give_the_same_bits():
                 results.append(layers.linear8(x, xs, w, ws))
     torch.cuda.synchronize()
     assert all(torch.equal(y, want) for y in results)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("name", ACTS)
+def test_activations_over_their_range(name, kind):
+    # one product a sum: z = 2^-7 (-127 ... 127) times scales that reach from 2^-10 to 2^8, and infinities and NaN
+    x = torch.arange(-127, 128, device="cuda", dtype=torch.int16).to(torch.int8)[:, None].contiguous()
+    w = torch.full((64, 1), 64, dtype=torch.int8, device="cuda")
+    xs, ws = torch.full((255,), 2.0 ** -13, device="cuda"), torch.exp2(torch.linspace(-10, 8, 64, device="cuda"))
+    y = layers.linear8(x, xs, w, ws, activation=layers.ACTIVATIONS[name], dtype=TYPES[kind])
+    check(x, xs, w, ws, None, None, name, y, None)
+    for value in (float("inf"), -float("inf"), float("nan"), 1e30, -1e30):
+        bias = torch.full((64,), value, device="cuda").to(TYPES[kind])
+        y = layers.linear8(x, xs, w, ws, bias, activation=layers.ACTIVATIONS[name], dtype=TYPES[kind])
+        if value != value:
+            assert bool(torch.isnan(y).all())
+        elif value > 0 or name == "none":
+            assert torch.equal(y, bias.expand_as(y))
+        else:                                   # 0 from below, or 0 times infinity
+            assert bool(((y == 0) | torch.isnan(y)).all())
