@@ -92,7 +92,9 @@ struct ProductShape {
     static constexpr int kSQ = kQW < 64 ? kQW : 64;                     // epilogue: q of a wavefront's part at a time
     static constexpr int kSumsLd = kPW + 4, kSums = kSQ * kSumsLd * 4;
     static constexpr int kStages = kAlone ? 2 : 4;
-    static constexpr int kLds = kStages * kStage > kWaves * kSums ? kStages * kStage : kWaves * kSums;
+    // behind stages and sums, for operands of 8 bits: the rows' scales of Q (load_rows)
+    static constexpr int kRows = kStages * kStage > kWaves * kSums ? kStages * kStage : kWaves * kSums;
+    static constexpr int kLds = kRows + (sizeof(T) == 1 ? BQ * 4 : 0);
     static_assert(kLds <= kLdsBytes, "LDS");
 };
 
@@ -266,7 +268,7 @@ __device__ __forceinline__ void load_columns(const Epilogue &e, int p0, int lane
 
 // rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time.  QS: rows may have a scale
 template <class T, class Out, bool QS, int ACT, int PW, int QW>
-__device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
+__device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, const float *rows, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, R = QW / ROWS < 4 ? QW / ROWS : 4;
     static_assert(QW % (ROWS * R) == 0, "");
@@ -295,7 +297,8 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
 #pragma unroll
         for (int y = 0; y < R; ++y) {
             x[y] = 1.0f;
-            if (QS && (sizeof(T) == 1 || e.q_scale) && q0 + s + y * ROWS < e.nq) x[y] = e.q_scale[q0 + s + y * ROWS];
+            if (sizeof(T) == 1) x[y] = rows[s + y * ROWS];
+            else if (QS && e.q_scale && q0 + s + y * ROWS < e.nq) x[y] = e.q_scale[q0 + s + y * ROWS];
         }
         if (e.residual)
 #pragma unroll
@@ -354,22 +357,22 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
 }
 
 template <class T, class Out, bool QS, int ACT, int PW, int QW>
-__device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
+__device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, const float *rows, int q0, int p0, int lane)
 {
-    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, Out, QS, ACT, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+    if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, Out, QS, ACT, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
     else epilogue_entries<T, Out, QS, ACT, PW, QW>(e, sums, q0, p0, lane);
 }
 
 template <class T, class Out, bool QS, int PW, int QW>
-__device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, int q0, int p0, int lane)
+__device__ __forceinline__ void epilogue(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, const float *rows, int q0, int p0, int lane)
 {
     switch (e.act) {                                // (decided once: a lane's entries decide nothing)
-        case OZIMMU_ACT_RELU: return epilogue_as<T, Out, QS, OZIMMU_ACT_RELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU: return epilogue_as<T, Out, QS, OZIMMU_ACT_GELU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, Out, QS, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, columns, sums, q0, p0, lane);
-        case OZIMMU_ACT_SILU: return epilogue_as<T, Out, QS, OZIMMU_ACT_SILU, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+        case OZIMMU_ACT_RELU: return epilogue_as<T, Out, QS, OZIMMU_ACT_RELU, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
+        case OZIMMU_ACT_GELU: return epilogue_as<T, Out, QS, OZIMMU_ACT_GELU, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
+        case OZIMMU_ACT_GELU_TANH: return epilogue_as<T, Out, QS, OZIMMU_ACT_GELU_TANH, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
+        case OZIMMU_ACT_SILU: return epilogue_as<T, Out, QS, OZIMMU_ACT_SILU, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
     }
-    epilogue_as<T, Out, QS, OZIMMU_ACT_NONE, PW, QW>(e, partial, columns, sums, q0, p0, lane);
+    epilogue_as<T, Out, QS, OZIMMU_ACT_NONE, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
 }
 
 // one tile, or one part of its contraction
@@ -388,6 +391,13 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
     P.init(a.P, a.ldp, a.p_rows, tp * BP, a.p_nk, wave, lane);
     Q.init(a.Q, a.ldq, a.q_rows, tq * BQ, a.q_nk, wave, lane);
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+
+    // (a load in the epilogue waits for all stores before it)
+    if constexpr (sizeof(T) == 1) {
+        static_assert(BQ <= S::kThreads, "a row a thread");
+        const int t = threadIdx.x;
+        if (t < BQ) ((float *)(lds + S::kRows))[t] = tq * BQ + t < a.e.nq ? a.e.q_scale[tq * BQ + t] : 0.0f;
+    }
 
     v4f acc[FP][FQ];
     auto clear = [&]() {
@@ -530,6 +540,7 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
     load_columns<T, Out, S::kPW>(a.e, p0, lane, columns);
     __syncthreads();                                // (the sums take the stages' place)
     float *sums = (float *)(lds + wave * S::kSums);
+    const float *rows = sizeof(T) == 1 ? (const float *)(lds + S::kRows) + wq : nullptr;
     const int r = lane & 15, g = lane >> 4;
 #pragma nounroll
     for (int h = 0; h < S::kQW / S::kSQ; ++h) {
@@ -544,7 +555,7 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
             }
         });
         __builtin_amdgcn_wave_barrier();
-        epilogue<T, Out, sizeof(T) == 1 || !PK, S::kPW, S::kSQ>(a.e, partial, columns, sums, q0 + h * S::kSQ, p0, lane);
+        epilogue<T, Out, sizeof(T) == 1 || !PK, S::kPW, S::kSQ>(a.e, partial, columns, sums, rows + h * S::kSQ, q0 + h * S::kSQ, p0, lane);
         __builtin_amdgcn_wave_barrier();
     }
 }
