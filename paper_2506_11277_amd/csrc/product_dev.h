@@ -72,14 +72,16 @@ __device__ __forceinline__ void mma_row(v4u p, const v4u (&q)[FQ], v4f (&c)[FQ])
             for (int j = 0; j < FQ; ++j) asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+v"(c[j]) : "v"(p[e]), "v"(q[j][e]));
     }
 }
-// the wait states between a matrix instruction and another use of its result, which the compiler does not see through the asm
-template <bool ACC, int N>
+// the wait states between a matrix instruction and another use of its result, which the compiler does not see through the asm: once, behind
+// the last of them (WAIT), and for what came before it the place alone
+template <bool ACC, bool WAIT, int N>
 __device__ __forceinline__ void settle(v4f (&c)[N])
 {
 #pragma unroll
     for (int j = 0; j < N; j += 2) {
-        if constexpr (ACC) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(c[j]), "+a"(c[j + 1]));
-        else asm volatile("s_nop 15\n\ts_nop 15" : "+v"(c[j]), "+v"(c[j + 1]));
+        if (WAIT && j == 0) asm volatile("s_nop 15\n\ts_nop 15");
+        if constexpr (ACC) asm volatile("" : "+a"(c[j]), "+a"(c[j + 1]));
+        else asm volatile("" : "+v"(c[j]), "+v"(c[j + 1]));
     }
 }
 
@@ -270,7 +272,7 @@ __device__ __forceinline__ void load_columns(const Epilogue &e, int p0, int lane
 template <class T, class Out, bool QS, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, const float *rows, int q0, int p0, int lane)
 {
-    constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, R = QW / ROWS < 4 ? QW / ROWS : 4;
+    constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, MOST = sizeof(T) == 1 ? 8 : 4, R = QW / ROWS < MOST ? QW / ROWS : MOST;
     static_assert(QW % (ROWS * R) == 0, "");
     const int col = lane % LANES * 8, p = p0 + col;
     if (p >= e.np) return;
@@ -504,7 +506,7 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
         }
         half(first, reads, now, nothing);
         half(second, none, 0, nothing);
-        static_for<0, FP>([&](auto I) __attribute__((always_inline)) { settle<(S::kAlone && I < FP - 1)>(acc[I]); });
+        static_for<0, FP>([&](auto I) __attribute__((always_inline)) { settle<(S::kAlone && I < FP - 1), I == 0>(acc[I]); });
     } else {
         // the chunks of a step are loaded two steps ahead (one: 24 us for 1531 x 1001 x 777 f16)
         auto load = [&](int t, auto X) __attribute__((always_inline)) {
