@@ -20,12 +20,15 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(Product a, f
     const bool on[1] = {(lane & 15) < a.e.nq};
     const T *const x[1] = {(const T *)a.Q + (size_t)(on[0] ? lane & 15 : 0) * a.ldq};
     v4f acc[1][1] = {{v4f{0, 0, 0, 0}}};
+    const int q = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8, p = p0 + c;
+    const bool finishes = q < 16 && q < a.e.nq && p < a.e.np;
+    RowVectors<O> with;                             // (their loads beside the weight's, not behind the sums)
+    if (sizeof(T) == 1 && finishes && !partial) with.load(a.e, q, p);
     const int all = (a.nk + KE - 1) / KE, first = blockIdx.y * steps_per_split, last = all < first + steps_per_split ? all : first + steps_per_split;
     stream_products<T, 1, 1, U>(acc, w, x, on, first + wave, last, kFewWaves, a.nk, lane);
     put_sums(sums[wave], acc[0][0], lane);
     __syncthreads();
-    const int q = threadIdx.x >> 1, c = (threadIdx.x & 1) * 8, p = p0 + c;
-    if (q >= 16 || q >= a.e.nq || p >= a.e.np) return;
+    if (!finishes) return;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
     for (int s = 0; s < kFewWaves; ++s) {
@@ -34,6 +37,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_tokens_kernel(Product a, f
         for (int e = 0; e < 8; ++e) v[e] = add_sums<T>(v[e], from[e]);
     }
     if (partial) store_row(partial + ((size_t)blockIdx.y * a.e.nq + q) * ((a.e.np + 7) & ~7) + p, v);
+    else if constexpr (sizeof(T) == 1) finish_row<T, O>(a.e, q, p, v, with);
     else finish_row<T, O>(a.e, q, p, v);
 }
 
@@ -44,7 +48,8 @@ hipError_t launch_few_tokens(const Product &a, const ProductPlan &plan, float *p
     const dim3 grid(grid_row(groups), plan.splits, grid_rows(groups));
     float *const to = plan.splits > 1 ? partial : nullptr;
     // (steps whose loads a wavefront issues together: no more than it has)
-    if (plan.steps > 2 * kFewWaves) few_tokens_kernel<T, O, 4><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
+    if (sizeof(T) == 1 && plan.steps <= kFewWaves) few_tokens_kernel<T, O, 1><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
+    else if (plan.steps > 2 * kFewWaves) few_tokens_kernel<T, O, 4><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
     else few_tokens_kernel<T, O, 2><<<grid, 64 * kFewWaves, 0, st>>>(a, to, plan.steps);
     return hipGetLastError();
 }

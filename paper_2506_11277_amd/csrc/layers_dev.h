@@ -239,58 +239,95 @@ __device__ __forceinline__ float scaled(float sum, float q_scale, float p_scale,
     else return sum * q_scale + bias;
 }
 
-// N = 8 (p a multiple of 8) entries of row q: sums of operands of type S, results of type T
-template <class S, class T = S>
-__device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, float (&v)[8])
-{
-    if constexpr (sizeof(S) > 1)
-        if (e.q_scale) {
-            const float x = e.q_scale[q];
+// What 8 entries of a row want of the scales and the bias (operands of 8 bits): loaded early, or in finish_row
+template <class T>
+struct RowVectors {
+    float x, scale[8], bias[8];
+    __device__ __forceinline__ void load(const Epilogue &e, int q, int p)
+    {
+        x = e.q_scale[q];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= x;
-        }
-    const float x = sizeof(S) == 1 ? e.q_scale[q] : 1.0f;
-    if (e.wide && p + 8 <= e.np) {
-        float t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (e.bias) load_row((const T *)e.bias + p, t);
-        if constexpr (sizeof(S) == 1) {
-            float scale[8];
+        for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
+        if (e.wide && p + 8 <= e.np) {
             load_row(e.p_scale + p, scale);
+            if (e.bias) load_row((const T *)e.bias + p, bias);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = scaled<S>(v[i], x, scale[i], t[i]);
-        } else if (e.bias) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += t[i];
+            for (int i = 0; i < 8; ++i) {
+                scale[i] = p + i < e.np ? e.p_scale[p + i] : 0.0f;
+                if (e.bias && p + i < e.np) bias[i] = (float)((const T *)e.bias)[p + i];
+            }
         }
+    }
+};
+
+// The values before the activation, `pre` and what follows, of N = 8 (p a multiple of 8) entries of row q: sums of operands of type S.
+template <class S, class T>
+__device__ __forceinline__ void finish_values(const Epilogue &e, int q, int p, float (&v)[8])
+{
+    if (e.wide && p + 8 <= e.np) {
         if (e.pre) store_row((T *)e.pre + (size_t)q * e.ldpre + p, v);
         if (e.act)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = activate_sum<S, T>(e.act, v[i]);
         if (e.residual) {
+            float t[8];
             load_row((const T *)e.residual + (size_t)q * e.ldr + p, t);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += t[i];
         }
         store_row((T *)e.out + (size_t)q * e.ldo + p, v);
     } else {
-        float b[8], r[8];                           // (all loads before the first store, which might be to the same place)
+        float r[8];                                 // (all loads before the first store, which might be to the same place)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const bool in = p + i < e.np;
-            b[i] = in && e.bias ? (float)((const T *)e.bias)[p + i] : 0.0f;
-            r[i] = in && e.residual ? (float)((const T *)e.residual)[(size_t)q * e.ldr + p + i] : 0.0f;
-        }
+        for (int i = 0; i < 8; ++i) r[i] = p + i < e.np && e.residual ? (float)((const T *)e.residual)[(size_t)q * e.ldr + p + i] : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (p + i >= e.np) continue;
-            float z = v[i] + b[i];
-            if constexpr (sizeof(S) == 1) z = scaled<S>(v[i], x, e.p_scale[p + i], b[i]);
-            if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)z;
-            z = activate_sum<S, T>(e.act, z);
+            if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)v[i];
+            float z = activate_sum<S, T>(e.act, v[i]);
             if (e.residual) z += r[i];
             ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)z;
         }
     }
+}
+
+template <class S, class T>
+__device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, float (&v)[8], const RowVectors<T> &with)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = scaled<S>(v[i], with.x, with.scale[i], with.bias[i]);
+    finish_values<S, T>(e, q, p, v);
+}
+
+// N = 8 (p a multiple of 8) entries of row q: sums of operands of type S, results of type T
+template <class S, class T = S>
+__device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, float (&v)[8])
+{
+    if constexpr (sizeof(S) == 1) {
+        RowVectors<T> with;
+        with.load(e, q, p);
+        finish_row<S, T>(e, q, p, v, with);
+        return;
+    }
+    if (e.q_scale) {
+        const float x = e.q_scale[q];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= x;
+    }
+    if (e.bias) {
+        if (e.wide && p + 8 <= e.np) {
+            float t[8];
+            load_row((const T *)e.bias + p, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += t[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (p + i < e.np) v[i] += (float)((const T *)e.bias)[p + i];
+        }
+    }
+    finish_values<S, T>(e, q, p, v);
 }
 
 // A scale as m 2^e, 1 <= m < 2, and its sign with the power: code * power is exact in 16 bits (8 binary digits; float16: where it is in its range),
