@@ -75,6 +75,30 @@ __device__ __forceinline__ v4u load_chunk(const T *p, int n)
     return r.v;
 }
 
+// ... of a row whose entries in front of p number `before`: those of 8 bits that end within a chunk are taken with the 16 bytes that end where the row
+// does, where it is as long, and moved (sixteen loads of a byte otherwise)
+template <class T>
+__device__ __forceinline__ v4u load_chunk(const T *p, int n, int before)
+{
+    if constexpr (sizeof(T) == 1) {
+        if (n <= 0) return v4u{0, 0, 0, 0};
+        if (before + n >= 16) {
+            const int beyond = n < 16 ? 16 - n : 0, shift = 8 * beyond;
+            unsigned long long x[2];
+            __builtin_memcpy(x, p - beyond, 16);
+            if (shift >= 64) {
+                x[0] = x[1] >> (shift - 64);
+                x[1] = 0;
+            } else if (shift > 0) {
+                x[0] = (x[0] >> shift) | (x[1] << (64 - shift));
+                x[1] >>= shift;
+            }
+            return v4u{(unsigned)x[0], (unsigned)(x[0] >> 32), (unsigned)x[1], (unsigned)(x[1] >> 32)};
+        }
+    }
+    return load_chunk(p, n);
+}
+
 // Activations, in 32 bits.  Operands of 32 bits take the library's exponential, error function and division; those of 16
 // bits the instructions for 2^x and 1 / x (two units off at most) and a polynomial, whose errors are a hundredth of the
 // rounding that follows: 8192 x 8192 values of an epilogue with the library's erf cost 110 us, so 40.

@@ -36,7 +36,7 @@ __device__ __forceinline__ void pad_chunk(const PadCopies &a, long long i)
             store_row(to, v);
             return;
         }
-    *(v4u *)to = load_chunk((const T *)c.from + row * c.ld + k, c.cols - k);
+    *(v4u *)to = load_chunk((const T *)c.from + row * c.ld + k, c.cols - k, k);
 }
 
 // work-groups of 256

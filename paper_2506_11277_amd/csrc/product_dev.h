@@ -200,7 +200,7 @@ struct Operand {
             slot(i, wave, lane, r, c);
             if constexpr (K_ROWS) {
                 const int row = row0 + r < rows ? row0 + r : rows - 1, k = k0 + c * E;
-                reg[S][i] = load_chunk(base + (size_t)row * ld + k, nk - k);
+                reg[S][i] = load_chunk(base + (size_t)row * ld + k, nk - k, k);
             } else {
                 const int k = k0 + r, col = row0 + c * E;
                 reg[S][i] = load_chunk(base + (size_t)k * ld + col, k < nk ? rows - col : 0);

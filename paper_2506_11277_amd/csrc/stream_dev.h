@@ -41,9 +41,9 @@ __device__ __forceinline__ void stream_products(v4f (&acc)[NW][NX], const T *con
                 for (int s = 0; s < 2; ++s) {
                     const int k = (t + u * stride) * KE + s * 4 * E + g, n = t + u * stride < last ? nk - k : 0;
 #pragma unroll
-                    for (int i = 0; i < NW; ++i) a[u][s][i] = load_chunk(w[i] + k, n);
+                    for (int i = 0; i < NW; ++i) a[u][s][i] = load_chunk(w[i] + k, n, k);
 #pragma unroll
-                    for (int j = 0; j < NX; ++j) b[u][s][j] = load_chunk(x[j] + k, on[j] ? n : 0);
+                    for (int j = 0; j < NX; ++j) b[u][s][j] = load_chunk(x[j] + k, on[j] ? n : 0, k);
                 }
         }
 #pragma unroll
