@@ -279,7 +279,6 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
         g.rows = rows;
         g.act = activation;
         g.pre_scale = activation ? pre_scale : nullptr;
-        g.wide = on16(dy, lddy, size) && (!activation || pre_scale || on16(pre, ldpre, size));
         if (own_dz && split_x) {
             g.x_scale = x_scale;
             g.x_inverse = (float *)(base + ws.inverse_x);

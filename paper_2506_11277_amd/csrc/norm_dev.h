@@ -1,4 +1,4 @@
-// What the kernels over whole rows share (norm.hip): a row in registers, sums and maxima over it, rows in 8 bits.
+// What the kernels over whole rows share (norm.hip, norm_grad.hip, grad.hip): eight elements at a time, a row in registers, sums and maxima over it, rows in 8 bits.
 #pragma once
 #include "layers.h"
 
@@ -15,7 +15,7 @@ struct Eight {
             __builtin_memcpy(&v, p, sizeof v);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0.0f;
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0;
         }
     }
     __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }

@@ -215,22 +215,23 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormGradArgs a, 
     }
 }
 
-// dw: the partial sums' rows, 64 columns a work-group, its wavefronts every sixteenth row
+// dw: the partial sums' rows, 32 columns a work-group, half a wavefront every 32nd row
+constexpr int kJoinColumns = 32;
 template <class T>
 __global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float *sums, T *dw, int rows, int width)
 {
-    __shared__ float part[16][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long c = ((long long)blockIdx.y * kGridRow + blockIdx.x) * 64 + lane;
+    __shared__ float part[32][kJoinColumns];
+    const int group = threadIdx.x / kJoinColumns, t = threadIdx.x % kJoinColumns;
+    const long long c = ((long long)blockIdx.y * kGridRow + blockIdx.x) * kJoinColumns + t;
     float s = 0.0f;
     if (c < width)
 #pragma unroll 8
-        for (int r = wave; r < rows; r += 16) s += sums[(size_t)r * width + c];
-    part[wave][lane] = s;
+        for (int r = group; r < rows; r += 32) s += sums[(size_t)r * width + c];
+    part[group][t] = s;
     __syncthreads();
-    if (wave == 0 && c < width) {
+    if (group == 0 && c < width) {
 #pragma unroll
-        for (int w = 1; w < 16; ++w) s += part[w][lane];
+        for (int g = 1; g < 32; ++g) s += part[g][t];
         dw[c] = (T)s;
     }
 }
@@ -276,7 +277,7 @@ hipError_t launch(const NormGradArgs &a, hipStream_t st)
         }
     }
     if (e != hipSuccess || !a.dw) return e;
-    const long long groups = (a.width + 63LL) / 64;
+    const long long groups = (a.width + kJoinColumns - 1LL) / kJoinColumns;
     norm_grad_join_kernel<T><<<dim3(grid_row(groups), grid_rows(groups)), 1024, 0, st>>>(a.sums, (T *)a.dw, a.rows > 0 ? plan.parts : 0, a.width);
     return hipGetLastError();
 }

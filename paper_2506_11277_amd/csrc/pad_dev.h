@@ -15,7 +15,7 @@ __device__ __forceinline__ void pad_chunk(const PadCopies &a, long long i)
     const PadCopy &c = a.c[second];
     if (second) i -= first;
     const int chunks = c.ldto / E;
-    const long long row = i / chunks;
+    const long long row = i >> 32 ? i / chunks : (long long)((unsigned)i / (unsigned)chunks);      // (64-bit division: as long as the copy)
     const int k = (int)(i - row * chunks) * E;
     T *const to = (T *)c.to + row * c.ldto + k;
     if constexpr (sizeof(T) > 1)
