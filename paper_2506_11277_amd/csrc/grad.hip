@@ -3,95 +3,67 @@
 // Bound by memory: dy and pre are read once, dz is written once; the column sums ride along in registers.  A work-group
 // owns 512 columns of grad_rows() tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
 // work-group of tokens, with the products of dx and dw or in a kernel of their own, always in the same order.
-// 8192 x 8192 bf16 with gelu, 403 MB: 74 us, 5.4 TB/s (the library's erf: 110).
+// 8192 x 8192 bf16 with gelu, 403 MB: 77 us, 5.2 TB/s (the library's erf: 110); from 8 bits, with 8192 x 4096 of x to bf16 beside it, 435 MB: 85 us.
 #include "norm_dev.h"
 #include "pad_dev.h"
 
 namespace oz {
 namespace {
 
-// Rows first + wave, ... of a work-group's columns.  (ACT and EIGHT decided once: with a decision for each value, and loads behind decisions, the launch
-// takes 7.9 us instead of 5.5 for 500 x 384 f32, silu, and its copies.)
+// Rows first, first + 4, ... of a lane's 8 columns from c on, `n` of them there.  (With a decision on the activation for each value, and loads behind
+// decisions, the launch takes 7.9 us instead of 6.0 for 500 x 384 f32, silu, and its copies; two rows at a time 80 us instead of 77 for 8192 x 8192 bf16.)
 //
-// dz of operands in 16 bits, x or w of which is held in 8: dz m[t] n[o] with the m and n of their scales (split_scale), which leaves
+// dz of operands in 16 bits, x or w of which is held in 8 (SPLIT): dz m[t] n[o] with the m and n of their scales (split_scale), which leaves
 // the operands exact and the products' rows to be divided by m[t] (dx) and n[o] (dw).
-template <class T, int ACT, bool EIGHT>
-__device__ __forceinline__ void grad_rows_of(const GradInput &a, long long first, long long last, bool first_strip, int lane, int c, int n, const float (&factor)[8], float (&sum)[8])
+template <class T, int ACT, bool EIGHT, bool SPLIT>
+__device__ __forceinline__ void grad_rows_of(const GradInput &a, long long first, long long last, bool writes_inverse, int c, int n, const float (&factor)[8], float (&sum)[8])
 {
-    constexpr int R = 2;
-    for (long long r0 = first; r0 < last; r0 += 4 * R) {
-        // (as they are in memory: as floats they would leave fewer wavefronts a SIMD)
-        Eight<T> dy[R];
-        Eight<std::conditional_t<EIGHT, int8_t, T>> pre[R];
-        float m[R], z_scale[R];
-#pragma unroll
-        for (int y = 0; y < R; ++y) {
-            const long long r = r0 + 4 * y < last ? r0 + 4 * y : r0;
-            dy[y].load((const T *)a.dy + (size_t)r * a.lddy + c, n);
-            if constexpr (ACT != OZIMMU_ACT_NONE) {
-                pre[y].load((const std::conditional_t<EIGHT, int8_t, T> *)a.pre + (size_t)r * a.ldpre + c, n);
-                if constexpr (EIGHT) z_scale[y] = a.pre_scale[r];
-            }
-            m[y] = a.x_scale ? a.x_scale[r] : 1.0f;
+    typedef std::conditional_t<EIGHT, int8_t, T> Pre;
+    for (long long r = first; r < last; r += 4) {
+        Eight<T> dy;
+        Eight<Pre> pre;
+        float scale = 1.0f, m = 1.0f, d[8];
+        dy.load((const T *)a.dy + (size_t)r * a.lddy + c, n);
+        if constexpr (ACT != OZIMMU_ACT_NONE) {
+            pre.load((const Pre *)a.pre + (size_t)r * a.ldpre + c, n);
+            if constexpr (EIGHT) scale = a.pre_scale[r];
         }
+        if (SPLIT && a.x_scale) m = split_scale(a.x_scale[r]).m;
 #pragma unroll
-        for (int y = 0; y < R; ++y) {
-            const long long r = r0 + 4 * y;
-            if (r >= last) break;
-            float d[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                d[i] = dy[y][i];
-                if constexpr (ACT != OZIMMU_ACT_NONE) d[i] *= activation_slope<T>(ACT, EIGHT ? pre[y][i] * z_scale[y] : pre[y][i]);
-                sum[i] += d[i];
-            }
-            if (!a.dz) continue;
-            if (a.x_scale) {
-                const float f = split_scale(m[y]).m;
-                if (first_strip && lane == 0) a.x_inverse[r] = 1.0f / f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= f * factor[i];
-            } else if (a.w_scale) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= factor[i];
-            }
-            T *to = (T *)a.dz + (size_t)r * a.lddz + c;
-            store_row(to, d);                            // (rows of dz are the workspace's, on 16 bytes, zeros behind them)
+        for (int i = 0; i < 8; ++i) {
+            d[i] = dy[i];
+            if constexpr (ACT != OZIMMU_ACT_NONE) d[i] *= activation_slope<T>(ACT, EIGHT ? pre[i] * scale : pre[i]);
+            sum[i] += d[i];
+            if constexpr (SPLIT) d[i] *= m * factor[i];
         }
+        if (SPLIT && a.x_scale && writes_inverse) a.x_inverse[r] = 1.0f / m;
+        if (n < 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i >= n) d[i] = 0.0f;                    // (0 times an infinite scale is none)
+        // (rows of dz are the workspace's, on 16 bytes, zeros behind them)
+        if (a.dz) store_row((T *)a.dz + (size_t)r * a.lddz + c, d);
     }
 }
 
-template <class T, bool EIGHT>
-__device__ __forceinline__ void grad_rows_as(const GradInput &a, long long first, long long last, bool first_strip, int lane, int c, int n, const float (&factor)[8], float (&sum)[8])
-{
-    switch (a.act) {
-        case OZIMMU_ACT_RELU: return grad_rows_of<T, OZIMMU_ACT_RELU, EIGHT>(a, first, last, first_strip, lane, c, n, factor, sum);
-        case OZIMMU_ACT_GELU: return grad_rows_of<T, OZIMMU_ACT_GELU, EIGHT>(a, first, last, first_strip, lane, c, n, factor, sum);
-        case OZIMMU_ACT_GELU_TANH: return grad_rows_of<T, OZIMMU_ACT_GELU_TANH, EIGHT>(a, first, last, first_strip, lane, c, n, factor, sum);
-        case OZIMMU_ACT_SILU: return grad_rows_of<T, OZIMMU_ACT_SILU, EIGHT>(a, first, last, first_strip, lane, c, n, factor, sum);
-    }
-    grad_rows_of<T, OZIMMU_ACT_NONE, EIGHT>(a, first, last, first_strip, lane, c, n, factor, sum);
-}
-
-template <class T>
+template <class T, int ACT, bool EIGHT, bool SPLIT>
 __device__ __forceinline__ void grad_input(const GradInput &a, int strip, int group, float (*part)[512])
 {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    // (the rows are a wavefront's: their addresses are scalars)
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int c = strip * 512 + lane * 8, n = a.n_out - c;
     const long long first = (long long)group * a.rows, last = first + a.rows < a.tokens ? first + a.rows : a.tokens;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, factor[8];
+    if constexpr (SPLIT) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) factor[i] = a.w_scale && i < n ? a.w_scale[c + i] : 1.0f;
-    if (a.w_scale)
+        for (int i = 0; i < 8; ++i) factor[i] = a.w_scale && i < n ? a.w_scale[c + i] : 1.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             factor[i] = split_scale(factor[i]).m;
-            if (i < n && group == 0 && wave == 0) a.w_inverse[c + i] = 1.0f / factor[i];
+            if (a.w_scale && i < n && group == 0 && wave == 0) a.w_inverse[c + i] = 1.0f / factor[i];
         }
-    if (n > 0) {
-        if (a.pre_scale) grad_rows_as<T, true>(a, first + wave, last, strip == 0, lane, c, n, factor, sum);
-        else grad_rows_as<T, false>(a, first + wave, last, strip == 0, lane, c, n, factor, sum);
     }
+    if (n > 0) grad_rows_of<T, ACT, EIGHT, SPLIT>(a, first + wave, last, strip == 0 && lane == 0, c, n, factor, sum);
     if (!a.sums) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[wave][lane * 8 + i] = sum[i];
@@ -101,12 +73,12 @@ __device__ __forceinline__ void grad_input(const GradInput &a, int strip, int gr
 }
 
 // ... and the copies that the products want, in one launch
-template <class T>
+template <class T, int ACT, bool EIGHT, bool SPLIT>
 __global__ __launch_bounds__(256) void grad_input_kernel(GradInput a, PadCopies copies, int strips, long long blocks)
 {
     __shared__ float part[4][512];
     const long long b = (long long)blockIdx.y * kGridRow + blockIdx.x;
-    if (b < blocks) grad_input<T>(a, (int)((unsigned)b % (unsigned)strips), (int)((unsigned)b / (unsigned)strips), part);
+    if (b < blocks) grad_input<T, ACT, EIGHT, SPLIT>(a, (int)((unsigned)b % (unsigned)strips), (int)((unsigned)b / (unsigned)strips), part);
     else pad_chunk<T>(copies, (b - blocks) * 256 + threadIdx.x);
 }
 
@@ -117,6 +89,20 @@ __global__ __launch_bounds__(256) void bias_grad_kernel(BiasGrad b)
     bias_grad<T>(b, (int)(blockIdx.y * kGridRow + blockIdx.x), part);
 }
 
+template <class T, bool EIGHT, bool SPLIT>
+hipError_t launch_as(const GradInput &g, const PadCopies &copies, int strips, long long blocks, long long all, hipStream_t st)
+{
+    const dim3 grid(grid_row(all), grid_rows(all));
+    switch (g.act) {
+        case OZIMMU_ACT_RELU: grad_input_kernel<T, OZIMMU_ACT_RELU, EIGHT, SPLIT><<<grid, 256, 0, st>>>(g, copies, strips, blocks); break;
+        case OZIMMU_ACT_GELU: grad_input_kernel<T, OZIMMU_ACT_GELU, EIGHT, SPLIT><<<grid, 256, 0, st>>>(g, copies, strips, blocks); break;
+        case OZIMMU_ACT_GELU_TANH: grad_input_kernel<T, OZIMMU_ACT_GELU_TANH, EIGHT, SPLIT><<<grid, 256, 0, st>>>(g, copies, strips, blocks); break;
+        case OZIMMU_ACT_SILU: grad_input_kernel<T, OZIMMU_ACT_SILU, EIGHT, SPLIT><<<grid, 256, 0, st>>>(g, copies, strips, blocks); break;
+        default: grad_input_kernel<T, OZIMMU_ACT_NONE, false, SPLIT><<<grid, 256, 0, st>>>(g, copies, strips, blocks);
+    }
+    return hipGetLastError();
+}
+
 template <class T>
 hipError_t launch(const GradInput &g, const PadCopies &copies, int type, hipStream_t st)
 {
@@ -124,8 +110,11 @@ hipError_t launch(const GradInput &g, const PadCopies &copies, int type, hipStre
     const long long blocks = g.dz || g.sums ? (long long)strips * ((g.tokens + (long long)g.rows - 1) / g.rows) : 0, all = blocks + pad_groups(copies, type);
     if (all == 0) return hipSuccess;
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    grad_input_kernel<T><<<dim3(grid_row(all), grid_rows(all)), 256, 0, st>>>(g, copies, strips, blocks);
-    return hipGetLastError();
+    // (scales go into dz in 16 bits only)
+    if constexpr (sizeof(T) == 2)
+        if (g.x_scale || g.w_scale)
+            return g.pre_scale ? launch_as<T, true, true>(g, copies, strips, blocks, all, st) : launch_as<T, false, true>(g, copies, strips, blocks, all, st);
+    return g.pre_scale ? launch_as<T, true, false>(g, copies, strips, blocks, all, st) : launch_as<T, false, false>(g, copies, strips, blocks, all, st);
 }
 
 }  // namespace

@@ -16,7 +16,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
     constexpr int ROWS = L < 256 ? 256 / L : 1;
     __shared__ SumAndTop slots[2][L / 64];
     const int t = L < 256 ? threadIdx.x & (L - 1) : threadIdx.x;
-    const long long row = ((long long)blockIdx.y * kGridRow + blockIdx.x) * ROWS + (L < 256 ? threadIdx.x / L : 0);
+    const long long row = ((long long)blockIdx.y * kGridRow + blockIdx.x) * ROWS + (L < 256 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : 0);
     if (row >= a.rows) return;
     const T *x = (const T *)a.x + (size_t)row * a.ldx, *res = a.residual ? (const T *)a.residual + (size_t)row * a.ldr : nullptr;
     const T *w = (const T *)a.weight;

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_grad_kernel(NormGradAr
     constexpr int ROWS = L < 256 ? 256 / L : 1;
     __shared__ TwoSums slots[3][L / 64];
     __shared__ float part[L < 256 ? 256 * 8 : 1];
-    const int t = L < 256 ? threadIdx.x & (L - 1) : threadIdx.x, which = L < 256 ? threadIdx.x / L : 0;
+    const int t = L < 256 ? threadIdx.x & (L - 1) : threadIdx.x, which = L < 256 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : 0;
     float dw[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -194,7 +194,7 @@ template <class T>
 __global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormGradArgs a, int group)
 {
     __shared__ float part[4][512];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = blockIdx.x * 512 + lane * 8;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = blockIdx.x * 512 + lane * 8;
     const long long first = (long long)blockIdx.y * group, last = first + group < a.rows ? first + group : a.rows;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (c < a.width)
