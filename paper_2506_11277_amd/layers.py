@@ -350,32 +350,29 @@ def moe(x, router, w_in, w_out, top_k, normalise=True, out=None, chosen=None, ga
     return out, chosen, gates
 
 
-def _matrix(x, what):
-    if x.dim() != 2:
+def _first(x, what):
+    """(type, shape, device, row stride) of the matrix that the others of a call go by."""
+    kind, shape = _type_of(x, what), x.shape
+    if len(shape) != 2:
         raise ValueError(f"{what}: a matrix expected")
-    return x.shape
+    return kind, shape, x.get_device(), _ld(x, shape[0], shape[1], x, what)
 
 
-def _codes(out, scale, rows, cols, like):
-    """(codes, their row stride, scales) of rows in 8 bits: given tensors or new ones."""
-    index = like.get_device()
-    if out is None:
-        out = torch.empty((rows, cols), dtype=torch.int8, device=like.device)
-    if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=like.device)
-    return out, _ld_codes(out, rows, cols, index, "out"), scale, _scale(scale, rows, index, "scale")
+def _like(x, shape, dtype, index, what):
+    """Row stride of a [rows, cols] device tensor of this type, as _ld; the plain case first (a third of the time)."""
+    if x.dtype is dtype and x.shape == shape and x.get_device() == index:
+        return (shape[1] or 1) if x.is_contiguous() and not (shape[0] | shape[1]) >> 30 else _ld(x, shape[0], shape[1], x, what)
+    raise ValueError(f"{what}: {list(shape)} of {dtype} on cuda:{index} expected")
 
 
-def _ld_codes(x, rows, cols, index, what):
-    if x.dtype is not torch.int8 or x.get_device() != index:
-        raise ValueError(f"{what}: int8 on cuda:{index} expected")
-    return _ld(x, rows, cols, x, what)
+def _line(x, n, dtype, index, what):
+    """Address of a contiguous vector."""
+    if x.dtype is dtype and x.shape == (n,) and x.get_device() == index and x.is_contiguous():
+        return x.data_ptr()
+    raise ValueError(f"{what}: contiguous [{n}] of {dtype} on cuda:{index} expected")
 
 
-def _scale(x, n, index, what):
-    if x.shape != (n,) or x.dtype is not torch.float32 or x.get_device() != index or (n > 1 and x.stride(0) != 1):
-        raise ValueError(f"{what}: contiguous [{n}] of float32 on cuda:{index} expected")
-    return x.data_ptr()
+_int8, _float32 = torch.int8, torch.float32
 
 
 def quantise(x, out=None, scale=None):
@@ -383,11 +380,14 @@ def quantise(x, out=None, scale=None):
 
     scale is the row's largest magnitude / 127, codes are rounded to nearest; a row with a value that is not finite has
     a scale of NaN.  Asynchronous on the current stream."""
-    kind = _type_of(x, "x")
-    rows, cols = _matrix(x, "x")
-    ldx = _ld(x, rows, cols, x, "x")
-    out, ldc, scale, pscale = _codes(out, scale, rows, cols, x)
-    rc = (_lib or lib()).ozimmu_quantise(rows, cols, kind, x.data_ptr(), ldx, out.data_ptr(), ldc, pscale, _stream(x.get_device(), "quantise"))
+    kind, shape, index, ldx = _first(x, "x")
+    rows, cols = shape
+    if out is None:
+        out = torch.empty(shape, dtype=_int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=_float32, device=x.device)
+    rc = (_lib or lib()).ozimmu_quantise(rows, cols, kind, x.data_ptr(), ldx, out.data_ptr(), _like(out, shape, _int8, index, "out"),
+                                         _line(scale, rows, _float32, index, "scale"), _stream(index, "quantise"))
     if rc != OK:
         raise OzimmuError(rc, "quantise")
     return out, scale
@@ -395,27 +395,29 @@ def quantise(x, out=None, scale=None):
 
 def _norm(x, weight, residual, eps, total, y, codes, scale, what):
     """The norm's call: (tensors that it made or was given)."""
-    kind = _type_of(x, "x")
-    tokens, width = _matrix(x, "x")
-    ldx = _ld(x, tokens, width, x, "x")
-    pw = None if weight is None else _vector(weight, width, x, "weight")
+    kind, shape, index, ldx = _first(x, "x")
+    (tokens, width), dtype = shape, x.dtype
+    pw = None if weight is None else _line(weight, width, dtype, index, "weight")
     ldr = ldt = ldy = ldc = 0
     py = pc = ps = pt = pr = None
     if residual is not None:
-        ldr, pr = _ld(residual, tokens, width, x, "residual"), residual.data_ptr()
+        ldr, pr = _like(residual, shape, dtype, index, "residual"), residual.data_ptr()
         if total is None:
-            total = torch.empty((tokens, width), dtype=x.dtype, device=x.device)
+            total = torch.empty(shape, dtype=dtype, device=x.device)
     if total is not None:
-        ldt, pt = _ld(total, tokens, width, x, "total"), total.data_ptr()
+        ldt, pt = _like(total, shape, dtype, index, "total"), total.data_ptr()
     if what == "rms_norm":
         if y is None:
-            y = torch.empty((tokens, width), dtype=x.dtype, device=x.device)
-        ldy, py = _ld(y, tokens, width, x, "out"), y.data_ptr()
+            y = torch.empty(shape, dtype=dtype, device=x.device)
+        ldy, py = _like(y, shape, dtype, index, "out"), y.data_ptr()
     else:
-        codes, ldc, scale, ps = _codes(codes, scale, tokens, width, x)
-        pc = codes.data_ptr()
+        if codes is None:
+            codes = torch.empty(shape, dtype=_int8, device=x.device)
+        if scale is None:
+            scale = torch.empty(tokens, dtype=_float32, device=x.device)
+        ldc, pc, ps = _like(codes, shape, _int8, index, "out"), codes.data_ptr(), _line(scale, tokens, _float32, index, "scale")
     rc = (_lib or lib()).ozimmu_rms_norm(tokens, width, kind, x.data_ptr(), ldx, pr, ldr, pw, eps, pt, ldt, py, ldy, pc, ldc, ps,
-                                         _stream(x.get_device(), what))
+                                         _stream(index, what))
     if rc != OK:
         raise OzimmuError(rc, what)
     return y, codes, scale, x if total is None else total
@@ -444,19 +446,19 @@ def rms_norm_grad(dy, total, weight=None, eps=1e-6, add=None, dx=None, dw=None, 
 
     dx is the gradient of x and of the residual; `add` [tokens, width], the gradient that reaches `total` from elsewhere, is added to
     it, and dx may be dy, total or add itself.  Of dx and dw those in `want` are formed, the others are None."""
-    kind = _type_of(dy, "dy")
-    tokens, width = _matrix(dy, "dy")
-    lddy, ldh = _ld(dy, tokens, width, dy, "dy"), _ld(total, tokens, width, dy, "total")
-    pw = None if weight is None else _vector(weight, width, dy, "weight")
-    lda = 0 if add is None else _ld(add, tokens, width, dy, "add")
-    dx = None if "dx" not in want else torch.empty((tokens, width), dtype=dy.dtype, device=dy.device) if dx is None else dx
-    dw = None if "dw" not in want else torch.empty(width, dtype=dy.dtype, device=dy.device) if dw is None else dw
-    lddx = 0 if dx is None else _ld(dx, tokens, width, dy, "dx")
-    pdw = None if dw is None else _vector(dw, width, dy, "dw")
+    kind, shape, index, lddy = _first(dy, "dy")
+    (tokens, width), dtype = shape, dy.dtype
+    ldh = _like(total, shape, dtype, index, "total")
+    pw = None if weight is None else _line(weight, width, dtype, index, "weight")
+    lda = 0 if add is None else _like(add, shape, dtype, index, "add")
+    dx = None if "dx" not in want else torch.empty(shape, dtype=dtype, device=dy.device) if dx is None else dx
+    dw = None if "dw" not in want else torch.empty(width, dtype=dtype, device=dy.device) if dw is None else dw
+    lddx = 0 if dx is None else _like(dx, shape, dtype, index, "dx")
+    pdw = None if dw is None else _line(dw, width, dtype, index, "dw")
     L = _lib or lib()
     keep, ws, nbytes = _workspace(workspace, L.ozimmu_rms_norm_grad_workspace_bytes(tokens, width) if workspace is None and dw is not None else 0, dy.device)
     rc = L.ozimmu_rms_norm_grad(tokens, width, kind, dy.data_ptr(), lddy, total.data_ptr(), ldh, pw, eps, None if add is None else add.data_ptr(), lda,
-                                None if dx is None else dx.data_ptr(), lddx, pdw, ws, nbytes, _stream(dy.get_device(), "rms_norm_grad"))
+                                None if dx is None else dx.data_ptr(), lddx, pdw, ws, nbytes, _stream(index, "rms_norm_grad"))
     if rc != OK:
         raise OzimmuError(rc, "rms_norm_grad")
     return dx, dw
@@ -475,13 +477,13 @@ def linear8(x, x_scale, w, w_scale, bias=None, residual=None, activation=ACT_NON
 
     x and w: int8, with float32 scales for their rows, as quantise and rms_norm8 give them.  Everything else is of one type: that of
     `out`, `residual`, `bias` or `pre` where given, else `dtype` (bfloat16 by default)."""
-    given = next((t for t in (out, residual, bias, pre) if t is not None), None)
+    given = out if out is not None else residual if residual is not None else bias if bias is not None else pre
     if given is None:
         dtype = torch.bfloat16 if dtype is None else dtype
-    elif dtype is not None and dtype != given.dtype:
-        raise ValueError(f"dtype: {given.dtype} or None expected")
-    else:
+    elif dtype is None:
         dtype = given.dtype
+    elif dtype != given.dtype:
+        raise ValueError(f"dtype: {given.dtype} or None expected")
     kind, index = _TYPES.get(dtype), x.get_device()
     if kind is None or not x.is_cuda:
         raise ValueError("linear8: CUDA tensors and a result in bfloat16, float16 or float32 expected")
@@ -491,16 +493,15 @@ def linear8(x, x_scale, w, w_scale, bias=None, residual=None, activation=ACT_NON
         raise ValueError("x and w: matrices expected") from None
     if n_in > LINEAR8_IN:
         raise ValueError(f"linear8: at most {LINEAR8_IN} input features expected, got {n_in}")
-    ldx, ldw = _ld_codes(x, tokens, n_in, index, "x"), _ld_codes(w, n_out, n_in, index, "w")
-    px, pw = _scale(x_scale, tokens, index, "x_scale"), _scale(w_scale, n_out, index, "w_scale")
+    ldx, ldw = _like(x, x.shape, _int8, index, "x"), _like(w, (n_out, n_in), _int8, index, "w")
+    px, pw = _line(x_scale, tokens, _float32, index, "x_scale"), _line(w_scale, n_out, _float32, index, "w_scale")
+    shape = (tokens, n_out)
     if out is None:
-        out = torch.empty((tokens, n_out), dtype=dtype, device=x.device)
-    ldy = _ld(out, tokens, n_out, out, "out")
-    if out.get_device() != index:
-        raise ValueError(f"out: {dtype} on {x.device} expected")
-    pbias = None if bias is None else _vector(bias, n_out, out, "bias")
-    ldr = 0 if residual is None else _ld(residual, tokens, n_out, out, "residual")
-    ldp = 0 if pre is None else _ld(pre, tokens, n_out, out, "pre")
+        out = torch.empty(shape, dtype=dtype, device=x.device)
+    ldy = _like(out, shape, dtype, index, "out")
+    pbias = None if bias is None else _line(bias, n_out, dtype, index, "bias")
+    ldr = 0 if residual is None else _like(residual, shape, dtype, index, "residual")
+    ldp = 0 if pre is None else _like(pre, shape, dtype, index, "pre")
     L = _lib or lib()
     keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear8_workspace_bytes(tokens, n_in, n_out, _aligned(x, ldx, w, ldw))
                                   if workspace is None else 0, x.device)
@@ -530,13 +531,15 @@ def linear8_grad(dy, x, w, pre=None, activation=ACT_NONE, x_scale=None, w_scale=
     except ValueError:
         raise ValueError("dy and x: matrices expected") from None
 
+    dtype = dy.dtype
+
     def held(t, scale, rows, cols, what):
         """(row stride, scales) of an operand of either kind."""
         if scale is None:
-            return _ld(t, rows, cols, dy, what), None
-        return _ld_codes(t, rows, cols, index, what), _scale(scale, rows, index, what + "_scale")
+            return _like(t, (rows, cols), dtype, index, what), None
+        return _like(t, (rows, cols), _int8, index, what), _line(scale, rows, _float32, index, what + "_scale")
 
-    lddy = _ld(dy, tokens, n_out, dy, "dy")
+    lddy = _like(dy, (tokens, n_out), dtype, index, "dy")
     ldx, pxs = held(x, x_scale, tokens, n_in, "x")
     ldw, pws = held(w, w_scale, n_out, n_in, "w")
     if activation != ACT_NONE and pre is None:
@@ -546,13 +549,13 @@ def linear8_grad(dy, x, w, pre=None, activation=ACT_NONE, x_scale=None, w_scale=
     def result(given, name, shape):
         if name not in want:
             return None
-        return torch.empty(shape, dtype=dy.dtype, device=dy.device) if given is None else given
+        return torch.empty(shape, dtype=dtype, device=dy.device) if given is None else given
 
     dx, dw = result(dx, "dx", (tokens, n_in)), result(dw, "dw", (n_out, n_in))
-    db = (torch.empty(n_out, dtype=dy.dtype, device=dy.device) if db is None else db) if bias else None
-    lddx = 0 if dx is None else _ld(dx, tokens, n_in, dy, "dx")
-    lddw = 0 if dw is None else _ld(dw, n_out, n_in, dy, "dw")
-    pdb = None if db is None else _vector(db, n_out, dy, "db")
+    db = (torch.empty(n_out, dtype=dtype, device=dy.device) if db is None else db) if bias else None
+    lddx = 0 if dx is None else _like(dx, (tokens, n_in), dtype, index, "dx")
+    lddw = 0 if dw is None else _like(dw, (n_out, n_in), dtype, index, "dw")
+    pdb = None if db is None else _line(db, n_out, dtype, index, "db")
     plain = [v for t, ld, scale in ((x, ldx, pxs), (w, ldw, pws)) if scale is None for v in (t, ld)]
     L = _lib or lib()
     keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear8_grad_workspace_bytes(tokens, n_in, n_out, kind, activation, _aligned(dy, lddy, *plain),

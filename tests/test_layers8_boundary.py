@@ -176,3 +176,18 @@ def test_the_binding_refuses_operands_of_linear8_grad(monkeypatch):
                  lambda: layers.linear8_grad_workspace_bytes(8, 1 << 32, 8, torch.bfloat16)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("rows,cols,ld", [(2, 8, (1 << 32) + 8), (2, 8, 1 << 31), (2, (1 << 32) + 8, (1 << 32) + 8), ((1 << 32) + 2, 8, 8), (1, 1 << 30, 1 << 30), (1 << 30, 1, 1)])
+def test_sizes_that_an_int_cannot_hold_are_refused(rows, cols, ld):
+    from paper_2506_11277_amd import layers
+    x = torch.empty_strided((rows, cols), (ld, 1), dtype=torch.int8, device="meta")
+    with pytest.raises(ValueError):
+        layers._like(x, x.shape, torch.int8, x.get_device(), "x")
+
+
+def test_sizes_up_to_the_largest_are_taken():
+    from paper_2506_11277_amd import layers
+    for rows, cols, ld in ((2, MOST, (1 << 31) - 1), (MOST, 1, 1), (0, MOST, MOST), (1, 8, 1 << 40), (5, 7, 7), (5, 7, 9)):
+        x = torch.empty_strided((rows, cols), (ld, 1), dtype=torch.int8, device="meta")
+        assert layers._like(x, x.shape, torch.int8, x.get_device(), "x") == (ld if rows > 1 else cols)
