@@ -114,14 +114,15 @@ struct NormGradPlan {
 };
 inline NormGradPlan plan_norm_grad(int rows, int width)
 {
-    constexpr int kMostParts = 512;
+    // (and no more than 1024 rows one behind the other in a sum of 32 bits)
     NormGradPlan p{width <= 16384, 0, 64};
+    constexpr int kMostParts = 512, kMostRows = 1024;
     if (p.in_registers) {
-        const int each = width <= 1024 ? 4 : 1, groups = (int)((rows + each - 1LL) / each);
-        p.parts = groups < kMostParts ? groups : kMostParts;
+        const int each = width <= 1024 ? 4 : 1, groups = (int)((rows + each - 1LL) / each), least = (int)((groups + kMostRows - 1LL) / kMostRows);
+        p.parts = groups < kMostParts ? groups : least > kMostParts ? least : kMostParts;
     } else {
-        const int least = (int)((rows + kMostParts - 1LL) / kMostParts);
-        if (least > p.group) p.group = least;
+        const int even = (int)((rows + kMostParts - 1LL) / kMostParts);
+        if (even > p.group) p.group = even < 4 * kMostRows ? even : 4 * kMostRows;
         p.parts = (int)((rows + p.group - 1LL) / p.group);
     }
     return p;

@@ -400,10 +400,10 @@ __device__ __forceinline__ void bias_grad(const BiasGrad &b, int block, float *p
 }
 
 // HIP takes less than 2^32 work-items along a dimension of a grid: rows of at most kGridRow work-groups (of up to 512; a multiple of
-// the XCDs), one behind the other along y or z.
-constexpr unsigned kGridRow = 1u << 22;
-inline unsigned grid_row(long long groups) { return groups < kGridRow ? (unsigned)groups : kGridRow; }
-inline unsigned grid_rows(long long groups) { return (unsigned)((groups + kGridRow - 1) / kGridRow); }
+// the XCDs), one behind the other along y or z; half as many (kGridRow1024) of larger ones.
+constexpr unsigned kGridRow = 1u << 22, kGridRow1024 = kGridRow / 2;
+inline unsigned grid_row(long long groups, unsigned row = kGridRow) { return groups < row ? (unsigned)groups : row; }
+inline unsigned grid_rows(long long groups, unsigned row = kGridRow) { return (unsigned)((groups + row - 1) / row); }
 
 enum Tile { kTile256, kTile128, kTile64, kTileFew };      // edge; few_tokens_kernel
 struct ProductPlan {

@@ -16,7 +16,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
     constexpr int ROWS = L < 256 ? 256 / L : 1;
     __shared__ SumAndTop slots[2][L / 64];
     const int t = L < 256 ? threadIdx.x & (L - 1) : threadIdx.x;
-    const long long row = ((long long)blockIdx.y * kGridRow + blockIdx.x) * ROWS + (L < 256 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : 0);
+    const long long row = ((long long)blockIdx.y * (L > 512 ? kGridRow1024 : kGridRow) + blockIdx.x) * ROWS + (L < 256 ? __builtin_amdgcn_readfirstlane(threadIdx.x / L) : 0);
     if (row >= a.rows) return;
     const T *x = (const T *)a.x + (size_t)row * a.ldx, *res = a.residual ? (const T *)a.residual + (size_t)row * a.ldr : nullptr;
     const T *w = (const T *)a.weight;
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 {
     constexpr int L = 1024;
     __shared__ SumAndTop slots[2][L / 64];
-    const long long row = (long long)blockIdx.y * kGridRow + blockIdx.x;
+    const long long row = (long long)blockIdx.y * kGridRow1024 + blockIdx.x;
     if (row >= a.rows) return;
     const T *x = (const T *)a.x + (size_t)row * a.ldx, *res = a.residual ? (const T *)a.residual + (size_t)row * a.ldr : nullptr;
     const T *w = (const T *)a.weight;
@@ -128,16 +128,17 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
         float sum = 0.0f;
         unsigned top = 0;
         for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
-            float h[8];
+            float h[8], part = 0.0f;
             Eight<T> rw;
             values(at, h, rw);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float v = h[i] * factor;
-                sum = __builtin_fmaf(v, v, sum);
+                part = __builtin_fmaf(v, v, part);
                 const unsigned m = magnitude(v * rw[i]);
                 top = m > top ? m : top;
             }
+            sum += part;
         }
         return over_row<L>(sum, top, to);
     };
@@ -177,7 +178,8 @@ hipError_t launch_rows(const NormArgs &a, hipStream_t st)
 {
     constexpr int ROWS = L < 256 ? 256 / L : 1;
     const long long groups = ((long long)a.rows + ROWS - 1) / ROWS;
-    norm_kernel<T, L, C><<<dim3(grid_row(groups), grid_rows(groups)), L < 256 ? 256 : L, 0, st>>>(a);
+    constexpr unsigned line = L > 512 ? kGridRow1024 : kGridRow;
+    norm_kernel<T, L, C><<<dim3(grid_row(groups, line), grid_rows(groups, line)), L < 256 ? 256 : L, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -191,7 +193,7 @@ hipError_t launch(const NormArgs &a, hipStream_t st)
     if (a.width <= 4096) return launch_rows<T, 256, 2>(a, st);
     if (a.width <= 8192) return launch_rows<T, 256, 4>(a, st);
     if (a.width <= 16384) return launch_rows<T, 1024, 2>(a, st);
-    norm_long_kernel<T><<<dim3(grid_row(a.rows), grid_rows(a.rows)), 1024, 0, st>>>(a);
+    norm_long_kernel<T><<<dim3(grid_row(a.rows, kGridRow1024), grid_rows(a.rows, kGridRow1024)), 1024, 0, st>>>(a);
     return hipGetLastError();
 }
 

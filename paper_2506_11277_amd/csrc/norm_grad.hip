@@ -140,7 +140,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a)
 {
     constexpr int L = 1024;
     __shared__ TwoSums slots[2][L / 64];
-    const long long row = (long long)blockIdx.y * kGridRow + blockIdx.x;
+    const long long row = (long long)blockIdx.y * kGridRow1024 + blockIdx.x;
     if (row >= a.rows) return;
     const T *hs = (const T *)a.h + (size_t)row * a.ldh, *ds = (const T *)a.dy + (size_t)row * a.lddy, *w = (const T *)a.weight;
     const T *add = a.add ? (const T *)a.add + (size_t)row * a.ldadd : nullptr;
@@ -158,14 +158,16 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a)
     auto statistics = [&](float factor, TwoSums *to) __attribute__((always_inline)) {
         float squares = 0.0f, products = 0.0f;
         for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
-            float h[8], g[8];
+            float h[8], g[8], a = 0.0f, b = 0.0f;
             values(at, h, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float v = h[i] * factor;
-                squares = __builtin_fmaf(v, v, squares);
-                products = __builtin_fmaf(g[i], v, products);
+                a = __builtin_fmaf(v, v, a);
+                b = __builtin_fmaf(g[i], v, b);
             }
+            squares += a;
+            products += b;
         }
         return sums_over_row<L>(squares, products, to);
     };
@@ -222,7 +224,7 @@ __global__ __launch_bounds__(1024) void norm_grad_join_kernel(const float *sums,
 {
     __shared__ float part[32][kJoinColumns];
     const int group = threadIdx.x / kJoinColumns, t = threadIdx.x % kJoinColumns;
-    const long long c = ((long long)blockIdx.y * kGridRow + blockIdx.x) * kJoinColumns + t;
+    const long long c = ((long long)blockIdx.y * kGridRow1024 + blockIdx.x) * kJoinColumns + t;
     float s = 0.0f;
     if (c < width)
 #pragma unroll 8
@@ -258,7 +260,7 @@ hipError_t launch(const NormGradArgs &a, hipStream_t st)
                                   : launch_rows<T, 1024, 2>(a, plan.parts, st);
         } else {
             // (where dx takes the place of what the columns are summed from, it is formed behind them)
-            const dim3 grid(grid_row(a.rows), grid_rows(a.rows));
+            const dim3 grid(grid_row(a.rows, kGridRow1024), grid_rows(a.rows, kGridRow1024));
             const bool behind = a.sums && a.dx && (a.dx == a.dy || a.dx == a.h);
             NormGradArgs b = a;
             if (behind) b.dx = nullptr;
@@ -278,7 +280,7 @@ hipError_t launch(const NormGradArgs &a, hipStream_t st)
     }
     if (e != hipSuccess || !a.dw) return e;
     const long long groups = (a.width + kJoinColumns - 1LL) / kJoinColumns;
-    norm_grad_join_kernel<T><<<dim3(grid_row(groups), grid_rows(groups)), 1024, 0, st>>>(a.sums, (T *)a.dw, a.rows > 0 ? plan.parts : 0, a.width);
+    norm_grad_join_kernel<T><<<dim3(grid_row(groups, kGridRow1024), grid_rows(groups, kGridRow1024)), 1024, 0, st>>>(a.sums, (T *)a.dw, a.rows > 0 ? plan.parts : 0, a.width);
     return hipGetLastError();
 }
 

@@ -40,8 +40,8 @@ def codes_untouched(view, buf):
 
 
 def depth(width):
-    """Additions that a value of a row passes on its way into the row's sum: at most 64 of a thread (of a longer row: width /
-    1024 and a group of 8), 6 among lanes, 16 among wavefronts."""
+    """Additions that a value of a row passes on its way into the row's sum: at most 64 of a thread (of a longer row less than width /
+    1024, and a group of 8), 6 among lanes, 16 among wavefronts."""
     return max(64, width // 1024 + 8) + 22
 
 

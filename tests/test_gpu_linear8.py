@@ -225,3 +225,24 @@ def test_activations_over_their_range(name, kind):
             assert torch.equal(y, bias.expand_as(y))
         else:                                   # 0 from below, or 0 times infinity
             assert bool(((y == 0) | torch.isnan(y)).all())
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("shape", [(1, 100, 40), (40, 0, 100), (300, 0, 24), (300, 100, 264), (3, 2000, 264)])
+def test_scales_bias_and_operands_at_any_alignment(shape, kind):
+    # (scales off 16 bytes, a bias off its rows', operands that start at any byte)
+    tokens, n_in, n_out = shape
+    x, xs, w, ws = operands(*shape, 0, 6)
+    bias, residual = others(tokens, n_out, kind, 0, 3)
+    want = layers.linear8(x, xs, w, ws, bias, residual, layers.ACT_GELU)
+    check(x, xs, w, ws, bias, residual, "gelu", want, None)
+
+    def moved(t, by):
+        buf = torch.empty(t.numel() + by, dtype=t.dtype, device="cuda")
+        view = buf[by:].view(t.shape)
+        return view.copy_(t)
+
+    for by in (1, 2, 3, 7):
+        y = layers.linear8(moved(x, by), moved(xs, by), moved(w, by), moved(ws, by), moved(bias, by), moved(residual, by), layers.ACT_GELU,
+                           out=moved(torch.empty_like(want), by))
+        assert torch.equal(y, want)

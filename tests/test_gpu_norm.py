@@ -284,3 +284,29 @@ def test_calls_in_a_graph_and_on_two_streams():
                 results.append(layers.rms_norm_grad(x, total, weight, add=res))
     torch.cuda.synchronize()
     assert all(torch.equal(a, dx) and torch.equal(b, dw) for a, b in results)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("width", [100, 2056, 20000])
+def test_tensors_at_any_alignment(width, kind):
+    x, res, dy = (values((5, width), kind, i) for i in range(3))
+    weight = values((width,), kind, 3)
+    want = layers.rms_norm8(x, weight, res) + layers.rms_norm(x, weight, res)[:1] + layers.rms_norm_grad(dy, x, weight, add=res)
+
+    def moved(t, by):
+        view = torch.empty(t.numel() + by, dtype=t.dtype, device="cuda")[by:].view(t.shape)
+        return view.copy_(t)
+
+    for by in (1, 3):
+        a, b, d, w = (moved(t, by) for t in (x, res, dy, weight))
+        empty = [moved(torch.empty_like(t), by) for t in want]
+        got = layers.rms_norm8(a, w, b, out=empty[0], scale=empty[1], total=empty[2]) + layers.rms_norm(a, w, b, out=empty[3])[:1]
+        got = got + layers.rms_norm_grad(d, a, w, add=b, dx=empty[4], dw=empty[5])
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_one_tensor_for_several_arguments():
+    # x that is its own residual, dy that is h: inputs may be the same
+    x, weight = values((9, 300), "bf16", 1), values((300,), "bf16", 3)
+    assert all(torch.equal(a, b) for a, b in zip(layers.rms_norm8(x, weight, x), layers.rms_norm8(x, weight, x.clone())))
+    assert all(torch.equal(a, b) for a, b in zip(layers.rms_norm_grad(x, x, weight, add=x), layers.rms_norm_grad(x, x.clone(), weight, add=x.clone())))

@@ -65,7 +65,8 @@ def test_norm_grad_workspace(handle):
     assert need(-1, 8) == 0 and need(8, 1 << 30) == 0 and need(0, 8) == 0 and need(8, 0) == 0
     for tokens in (1, 5, 1000, 1 << 20, MOST):
         for width in (1, 1001, 4096, 16384, 16385, 1 << 20):
-            assert 4 * width <= need(tokens, width) <= 1024 * 4 * (width + 64) + 8 * (tokens + 32)
+            # 512 parts, or one of every 1024 rows; and two numbers a row
+            assert 4 * width <= need(tokens, width) <= 4 * width * max(512, tokens // 1024 + 1) + 8 * tokens + 1024
             assert norm_grad(handle, tokens, width, lddy=width, ldh=width, lddx=width, nbytes=need(tokens, width) - 1) == BAD
     assert norm_grad(handle, width=0) == OK and norm_grad(handle, dx=None, dw=None, ws=None, nbytes=0) == OK
 
