@@ -4,7 +4,6 @@
 // owns 512 columns of grad_rows() tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
 // work-group of tokens, with the products of dx and dw or in a kernel of their own, always in the same order.
 // 8192 x 8192 bf16 with gelu, 403 MB: 77 us, 5.2 TB/s (the library's erf: 110); from 8 bits, with 8192 x 4096 of x to bf16 beside it, 435 MB: 85 us.
-#include "norm_dev.h"
 #include "pad_dev.h"
 
 namespace oz {

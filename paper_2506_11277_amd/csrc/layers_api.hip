@@ -110,8 +110,8 @@ inline size_t copy_bytes(const Product &a, bool of_p, size_t size)
 }
 
 // The plan of a product, and the copies that it wants first (`space`: where they go; null: there is no room, or too little).
-// type: of the operands, result: of what the epilogue reads and writes.
-ProductPlan route_product(Product &a, int type, int result, bool k_rows, char *space, size_t space_bytes, PadCopies &copies)
+// type: of the operands, result: of what the epilogue reads and writes, launch_us: what a launch for copies costs.
+ProductPlan route_product(Product &a, int type, int result, bool k_rows, char *space, size_t space_bytes, PadCopies &copies, double launch_us = 6)
 {
     const size_t size = element_bytes(type), out = element_bytes(result);
     Epilogue &e = a.e;
@@ -128,7 +128,7 @@ ProductPlan route_product(Product &a, int type, int result, bool k_rows, char *s
     const size_t p_bytes = p_fits ? 0 : copy_bytes(a, true, size), q_bytes = q_fits ? 0 : copy_bytes(a, false, size);
     // The copies: a launch, and their bytes read and written at 4 TB/s.  Rows off 16 bytes, without and with them: 4096^3 f16 321 and
     // 128 us (aligned: 110), 1024 x 4096 x 1024 52 and 30, 1531 x 1000 x 776 17 either way, 200 x 1000 x 4000 15 and 19.
-    if (a.nk == 0 || space == nullptr || space_bytes < p_bytes + q_bytes || direct.us + 6 + 2 * (p_bytes + q_bytes) / 4e6 >= other.us) return other;
+    if (a.nk == 0 || space == nullptr || space_bytes < p_bytes + q_bytes || direct.us + launch_us + 2 * (p_bytes + q_bytes) / 4e6 >= other.us) return other;
     auto copy = [&](PadCopy &c, const void *&x, int &ld, bool rows_along_k, int &rows, int &nk, char *to) {
         int &along = rows_along_k ? nk : rows;
         c = PadCopy{x, to, rows_along_k ? rows : nk, along, ld, up(along, size), nullptr};
@@ -331,9 +331,11 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
     PadCopy w_values{}, x_values{};
     if (form_dx && w8) w_values = expand(x_grad, w_scale, n_out, base + ws.copies_w);
     if (form_dw && x8) x_values = expand(w_grad, x_scale, tokens, base + ws.copies_x);
+    // (what is in 8 bits has a launch, which takes other copies along: 948 x 91 -> 768 f16 38 us with w through registers, 21 with a copy)
+    const double launch_us = x8 || w8 ? 0.5 : 6;
     // (of each product P alone can want a copy here: dz is the workspace's, or dy where there is no room for either)
-    if (form_dx) x_plan = route_product(x_grad, type, type, false, ws.has_w && !w8 ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies);
-    if (form_dw) w_plan = route_product(w_grad, type, type, false, ws.has_x && !x8 ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies);
+    if (form_dx) x_plan = route_product(x_grad, type, type, false, ws.has_w && !w8 ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies, launch_us);
+    if (form_dw) w_plan = route_product(w_grad, type, type, false, ws.has_x && !x8 ? base + ws.copies_x : nullptr, ws.copies_w - ws.copies_x, w_copies, launch_us);
     copies.c[0] = w8 ? w_values : x_copies.c[0];
     copies.c[1] = x8 ? x_values : w_copies.c[0];
     if (launch_grad_input(g, copies, type, st) != hipSuccess) return OZIMMU_HIP_ERROR;

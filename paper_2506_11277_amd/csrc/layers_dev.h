@@ -254,6 +254,38 @@ __device__ __forceinline__ void stream_row(T *p, const float (&v)[N])
     }
 }
 
+// eight elements, at any alignment of their type; `n` of them there (the others 0)
+template <class T>
+struct Eight {
+    typedef T V __attribute__((ext_vector_type(8)));
+    V v;
+    __device__ __forceinline__ void load(const T *p, int n)
+    {
+        if (n >= 8) {
+            __builtin_memcpy(&v, p, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0;
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
+};
+
+template <class T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&x)[8])
+{
+    typename Eight<T>::V v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
+    if (n >= 8) {
+        __builtin_memcpy(p, &v, sizeof v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = v[i];
+    }
+}
+
 // The sum of operands of type T, scaled, and the bias: of 8 bits the whole number to the nearest float, its product with the token's scale, and that
 // with the feature's together with the bias, each rounded once.
 template <class T>
@@ -270,16 +302,24 @@ struct RowVectors {
     __device__ __forceinline__ void load(const Epilogue &e, int q, int p)
     {
         x = e.q_scale[q];
+        load_columns(e, p);
+    }
+    __device__ __forceinline__ void load_columns(const Epilogue &e, int p)
+    {
 #pragma unroll
         for (int i = 0; i < 8; ++i) bias[i] = 0.0f;
-        if (e.wide && p + 8 <= e.np) {
+        if (e.wide && p + 8 <= e.np) {              // (both loads before either's wait)
             load_row(e.p_scale + p, scale);
             if (e.bias) load_row((const T *)e.bias + p, bias);
         } else {
+            Eight<float> s;
+            Eight<T> b;
+            s.load(e.p_scale + p, e.np - p);
+            if (e.bias) b.load((const T *)e.bias + p, e.np - p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                scale[i] = p + i < e.np ? e.p_scale[p + i] : 0.0f;
-                if (e.bias && p + i < e.np) bias[i] = (float)((const T *)e.bias)[p + i];
+                scale[i] = s[i];
+                if (e.bias) bias[i] = b[i];
             }
         }
     }
@@ -289,18 +329,19 @@ struct RowVectors {
 template <class S, class T>
 __device__ __forceinline__ void finish_values(const Epilogue &e, int q, int p, float (&v)[8])
 {
-    if (e.wide && p + 8 <= e.np) {
-        if (e.pre) store_row((T *)e.pre + (size_t)q * e.ldpre + p, v);
+    if (sizeof(S) == 1 || (e.wide && p + 8 <= e.np)) {
+        // (8 entries at any alignment, or what there is of them: of operands of 8 bits; the others take aligned rows only)
+        const int n = sizeof(S) == 1 ? e.np - p : 8;
+        Eight<T> t;
+        if (e.residual) t.load((const T *)e.residual + (size_t)q * e.ldr + p, n);
+        if (e.pre) store8((T *)e.pre + (size_t)q * e.ldpre + p, n, v);
         if (e.act)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = activate_sum<S, T>(e.act, v[i]);
-        if (e.residual) {
-            float t[8];
-            load_row((const T *)e.residual + (size_t)q * e.ldr + p, t);
+        if (e.residual)
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += t[i];
-        }
-        store_row((T *)e.out + (size_t)q * e.ldo + p, v);
+        store8((T *)e.out + (size_t)q * e.ldo + p, n, v);
     } else {
         float r[8];                                 // (all loads before the first store, which might be to the same place)
 #pragma unroll

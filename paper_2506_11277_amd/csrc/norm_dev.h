@@ -1,40 +1,8 @@
-// What the kernels over whole rows share (norm.hip, norm_grad.hip, grad.hip): eight elements at a time, a row in registers, sums and maxima over it, rows in 8 bits.
+// What the kernels over whole rows share (norm.hip, norm_grad.hip): a row in registers, sums and maxima over it, rows in 8 bits.
 #pragma once
 #include "layers.h"
 
 namespace oz {
-
-// eight elements, at any alignment of their type; `n` of them there (the others 0)
-template <class T>
-struct Eight {
-    typedef T V __attribute__((ext_vector_type(8)));
-    V v;
-    __device__ __forceinline__ void load(const T *p, int n)
-    {
-        if (n >= 8) {
-            __builtin_memcpy(&v, p, sizeof v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0;
-        }
-    }
-    __device__ __forceinline__ float operator[](int i) const { return (float)v[i]; }
-};
-
-template <class T>
-__device__ __forceinline__ void store8(T *p, int n, const float (&x)[8])
-{
-    typename Eight<T>::V v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (T)x[i];
-    if (n >= 8) {
-        __builtin_memcpy(p, &v, sizeof v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) p[i] = v[i];
-    }
-}
 
 // f over the 64 lanes' values of a wavefront, the same in each: among 16 by exchanges inside the vector unit
 template <class X, class F>

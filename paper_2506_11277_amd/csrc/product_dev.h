@@ -260,24 +260,31 @@ __device__ __forceinline__ void load_columns(const Epilogue &e, int p0, int lane
     const int p = p0 + lane % (PW / 8) * 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) c.bias[i] = 0.0f;
-    if (e.bias && e.wide && p + 8 <= e.np) load_row((const Out *)e.bias + p, c.bias);
+    if (sizeof(T) > 1 && e.bias && e.wide && p + 8 <= e.np) load_row((const Out *)e.bias + p, c.bias);
     if constexpr (sizeof(T) == 1) {
+        RowVectors<Out> with;
+        with.load_columns(e, p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c.scale[i] = 0.0f;
-        if (e.wide && p + 8 <= e.np) load_row(e.p_scale + p, c.scale);
+        for (int i = 0; i < 8; ++i) {
+            c.bias[i] = with.bias[i];
+            c.scale[i] = with.scale[i];
+        }
     }
 }
 
-// rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time.  QS: rows may have a scale
-template <class T, class Out, bool QS, int ACT, int PW, int QW>
+// rows q0 ... q0 + QW - 1 of `sums`, PW + 4 floats apart; R rows of a lane at a time.  QS: rows may have a scale.
+// !WHOLE: rows at any alignment, what lies behind their last entry one by one (8-bit operands; entry by entry 1531 x 1001 -> 777 takes 18.8 us instead
+// of 14.3, 4097 x 1001 -> 4095 84 instead of 57, but what is aligned would take 221 instead of 210 this way, 8192 x 4096 -> 8192)
+template <class T, class Out, bool QS, int ACT, int PW, int QW, bool WHOLE = true>
 __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, const float *rows, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, LANES = PW / 8, ROWS = 64 / LANES, MOST = sizeof(T) == 1 ? 8 : 4, R = QW / ROWS < MOST ? QW / ROWS : MOST;
     static_assert(QW % (ROWS * R) == 0, "");
     const int col = lane % LANES * 8, p = p0 + col;
     if (p >= e.np) return;
-    auto write = [](Out *to, const float (&x)[8]) __attribute__((always_inline)) {
-        if constexpr (PW == 128) stream_row(to, x);
+    auto write = [&](Out *to, const float (&x)[8]) __attribute__((always_inline)) {
+        if constexpr (!WHOLE) store8(to, e.np - p, x);
+        else if constexpr (PW == 128) stream_row(to, x);
         else store_row(to, x);
     };
 #pragma nounroll
@@ -305,7 +312,17 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
         if (e.residual)
 #pragma unroll
             for (int y = 0; y < R; ++y)
-                if (q0 + s + y * ROWS < e.nq) load_row((const Out *)e.residual + (size_t)(q0 + s + y * ROWS) * e.ldr + p, res[y]);
+                if (q0 + s + y * ROWS < e.nq) {
+                    const Out *from = (const Out *)e.residual + (size_t)(q0 + s + y * ROWS) * e.ldr + p;
+                    if constexpr (WHOLE) {
+                        load_row(from, res[y]);
+                    } else {
+                        Eight<Out> t;
+                        t.load(from, e.np - p);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) res[y][i] = t[i];
+                    }
+                }
 #pragma unroll
         for (int y = 0; y < R; ++y) {
             const int q = q0 + s + y * ROWS;
@@ -323,7 +340,7 @@ __device__ __forceinline__ void epilogue_rows(const Epilogue &e, float *partial,
     }
 }
 
-// ... entry by entry, where rows are not aligned or end within 8 entries: consecutive lanes take consecutive entries, four
+// ... entry by entry, where rows are not aligned or end within 8 entries (operands of 16 and 32 bits): consecutive lanes take consecutive entries, four
 // rows at a time; all 16 of a lane in a 64 x 64 tile (1531 x 1008 x 777 f16 with a residual 11.8 us against 12.2; in a 128 x 128
 // tile more than four are slower, 4097 x 1024 x 4095 f16 166 us against 155)
 template <class T, class Out, bool QS, int ACT, int PW, int QW>
@@ -362,6 +379,7 @@ template <class T, class Out, bool QS, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_as(const Epilogue &e, float *partial, const Columns<T> &columns, const float *sums, const float *rows, int q0, int p0, int lane)
 {
     if (partial || (e.wide && (p0 + PW <= e.np || e.np % 8 == 0))) epilogue_rows<T, Out, QS, ACT, PW, QW>(e, partial, columns, sums, rows, q0, p0, lane);
+    else if constexpr (sizeof(T) == 1) epilogue_rows<T, Out, QS, ACT, PW, QW, false>(e, partial, columns, sums, rows, q0, p0, lane);
     else epilogue_entries<T, Out, QS, ACT, PW, QW>(e, sums, q0, p0, lane);
 }
 
