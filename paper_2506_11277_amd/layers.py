@@ -9,6 +9,7 @@ version counter.  AdamW.step does raise the counters of what it writes, so that 
 """
 import ctypes
 from array import array
+from functools import lru_cache
 from operator import attrgetter
 
 import torch
@@ -375,6 +376,22 @@ def _line(x, n, dtype, index, what):
 _int8, _float32 = torch.int8, torch.float32
 
 
+# (sizes of workspaces follow from the sizes of a call: asked for once, where the library would take 1 us of every call)
+@lru_cache(maxsize=4096)
+def _norm_grad_bytes(*sizes):
+    return lib().ozimmu_rms_norm_grad_workspace_bytes(*sizes)
+
+
+@lru_cache(maxsize=4096)
+def _linear8_bytes(*sizes):
+    return lib().ozimmu_linear8_workspace_bytes(*sizes)
+
+
+@lru_cache(maxsize=4096)
+def _linear8_grad_bytes(*sizes):
+    return lib().ozimmu_linear8_grad_workspace_bytes(*sizes)
+
+
 def quantise(x, out=None, scale=None):
     """x [rows, cols] in 8 bits: (codes, scale), int8 [rows, cols] and float32 [rows], that stand for codes * scale[:, None].
 
@@ -456,7 +473,7 @@ def rms_norm_grad(dy, total, weight=None, eps=1e-6, add=None, dx=None, dw=None, 
     lddx = 0 if dx is None else _like(dx, shape, dtype, index, "dx")
     pdw = None if dw is None else _line(dw, width, dtype, index, "dw")
     L = _lib or lib()
-    keep, ws, nbytes = _workspace(workspace, L.ozimmu_rms_norm_grad_workspace_bytes(tokens, width) if workspace is None and dw is not None else 0, dy.device)
+    keep, ws, nbytes = _workspace(workspace, _norm_grad_bytes(tokens, width) if workspace is None and dw is not None else 0, dy.device)
     rc = L.ozimmu_rms_norm_grad(tokens, width, kind, dy.data_ptr(), lddy, total.data_ptr(), ldh, pw, eps, None if add is None else add.data_ptr(), lda,
                                 None if dx is None else dx.data_ptr(), lddx, pdw, ws, nbytes, _stream(index, "rms_norm_grad"))
     if rc != OK:
@@ -503,8 +520,7 @@ def linear8(x, x_scale, w, w_scale, bias=None, residual=None, activation=ACT_NON
     ldr = 0 if residual is None else _like(residual, shape, dtype, index, "residual")
     ldp = 0 if pre is None else _like(pre, shape, dtype, index, "pre")
     L = _lib or lib()
-    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear8_workspace_bytes(tokens, n_in, n_out, _aligned(x, ldx, w, ldw))
-                                  if workspace is None else 0, x.device)
+    keep, ws, nbytes = _workspace(workspace, _linear8_bytes(tokens, n_in, n_out, _aligned(x, ldx, w, ldw)) if workspace is None else 0, x.device)
     rc = L.ozimmu_linear8(tokens, n_in, n_out, kind, x.data_ptr(), ldx, px, w.data_ptr(), ldw, pw, pbias,
                           None if residual is None else residual.data_ptr(), ldr, activation,
                           None if pre is None else pre.data_ptr(), ldp, out.data_ptr(), ldy, ws, nbytes, _stream(index, "linear8"))
@@ -558,9 +574,8 @@ def linear8_grad(dy, x, w, pre=None, activation=ACT_NONE, x_scale=None, w_scale=
     pdb = None if db is None else _line(db, n_out, dtype, index, "db")
     plain = [v for t, ld, scale in ((x, ldx, pxs), (w, ldw, pws)) if scale is None for v in (t, ld)]
     L = _lib or lib()
-    keep, ws, nbytes = _workspace(workspace, L.ozimmu_linear8_grad_workspace_bytes(tokens, n_in, n_out, kind, activation, _aligned(dy, lddy, *plain),
-                                                                                  pxs is not None, pws is not None)
-                                  if workspace is None else 0, dy.device)
+    keep, ws, nbytes = _workspace(workspace, _linear8_grad_bytes(tokens, n_in, n_out, kind, activation, _aligned(dy, lddy, *plain),
+                                                                       pxs is not None, pws is not None) if workspace is None else 0, dy.device)
     rc = L.ozimmu_linear8_grad(tokens, n_in, n_out, kind, dy.data_ptr(), lddy, x.data_ptr(), ldx, pxs, w.data_ptr(), ldw, pws,
                                pre.data_ptr() if activation != ACT_NONE else None, ldp, pps, activation,
                                None if dx is None else dx.data_ptr(), lddx, None if dw is None else dw.data_ptr(), lddw, pdb,
