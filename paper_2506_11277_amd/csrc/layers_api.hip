@@ -331,7 +331,7 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
     PadCopy w_values{}, x_values{};
     if (form_dx && w8) w_values = expand(x_grad, w_scale, n_out, base + ws.copies_w);
     if (form_dw && x8) x_values = expand(w_grad, x_scale, tokens, base + ws.copies_x);
-    // (what is in 8 bits has a launch, which takes other copies along: 948 x 91 -> 768 f16 38 us with w through registers, 21 with a copy)
+    // (what is in 8 bits has a launch, which takes other copies along: 948 x 91 -> 768 f16 38 us with w through registers, 16 with a copy)
     const double launch_us = x8 || w8 ? 0.5 : 6;
     // (of each product P alone can want a copy here: dz is the workspace's, or dy where there is no room for either)
     if (form_dx) x_plan = route_product(x_grad, type, type, false, ws.has_w && !w8 ? base + ws.copies_w : nullptr, ws.total - ws.copies_w, x_copies, launch_us);

@@ -1,6 +1,6 @@
 // The tiled matrix product of the feed-forward operators: D[q][p] = act(sum_k P Q + bias) + residual.
 //
-// A work-group owns a tile of BP x BQ entries and walks k in steps of 128 bytes of an operand's row (64 entries of 16
+// A work-group owns a tile of BP x BQ entries and walks k in steps of 128 bytes of an operand's row (128 entries of 8 bits, 64 of 16
 // bits, 32 of 32 bits).  Both operands of a step stand in LDS as BP (BQ) * 128 bytes, in a ring of two stages (256 x 256: all
 // that fits) or four: the copies of a step are issued one to three steps before its products, one barrier a step.
 //
@@ -8,6 +8,10 @@
 // and 64 written a step of 2048 cycles of matrix instructions) close behind: 8192^3 bf16 1.43 PFLOP/s, 4096^3 1.36, 8192 x 4096 x 8192
 // with a gelu and `pre` 1.2.  128 x 128 and 64 x 64 LDS: 96 and 48 KB a step of 512 and 128 cycles (2048^3 770 TFLOP/s,
 // 1024^3 260).  32 bits: the matrix instructions (2048^3 133 TFLOP/s, 4096^3 140).
+//
+// 8 bits, results in 16: a step takes as long as in 16 bits, with twice the k.  8192 x 4096 x 8192 211 us (2.6 POP/s; without an epilogue 195),
+// with gelu and `pre` 240, 16384 of k 2.9 POP/s; on operands of zeros a step takes a quarter less: power.  A tile's epilogue is 5 us of
+// vector instructions (10 with gelu), and as long goes by until its first products: four times in 8192 x 8192.
 //
 // k_rows: the entries of an operand's row are contiguous along k (activations and weights of a forward pass).  LDS row r
 //   holds its 8 chunks of 16 bytes at position chunk ^ (r / 2 % 8): the 16 rows that a matrix instruction's operand takes
@@ -94,7 +98,7 @@ struct ProductShape {
     static constexpr int kSQ = kQW < 64 ? kQW : 64;                     // epilogue: q of a wavefront's part at a time
     static constexpr int kSumsLd = kPW + 4, kSums = kSQ * kSumsLd * 4;
     static constexpr int kStages = kAlone ? 2 : 4;
-    // behind stages and sums, for operands of 8 bits: the rows' scales of Q (load_rows)
+    // behind stages and sums, for operands of 8 bits: the scales of Q's rows
     static constexpr int kRows = kStages * kStage > kWaves * kSums ? kStages * kStage : kWaves * kSums;
     static constexpr int kLds = kRows + (sizeof(T) == 1 ? BQ * 4 : 0);
     static_assert(kLds <= kLdsBytes, "LDS");
