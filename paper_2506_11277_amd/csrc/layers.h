@@ -116,12 +116,15 @@ inline NormGradPlan plan_norm_grad(int rows, int width)
 {
     // (and no more than 1024 rows one behind the other in a sum of 32 bits)
     NormGradPlan p{width <= 16384, 0, 64};
-    constexpr int kMostParts = 512, kMostRows = 1024;
+    // (one row at a time in a work-group of 256 threads: 1024 groups keep the memory busy, 16384 x 2048 bf16 54.5 us instead of 60,
+    // 30000 x 1500 109 instead of 176, but 2000 x 2000 f32 20.7 instead of 19.6)
+    constexpr int kMostRows = 1024;
+    const int most = width > 1024 && width <= 2048 && rows >= 8192 ? 1024 : 512;
     if (p.in_registers) {
         const int each = width <= 1024 ? 4 : 1, groups = (int)((rows + each - 1LL) / each), least = (int)((groups + kMostRows - 1LL) / kMostRows);
-        p.parts = groups < kMostParts ? groups : least > kMostParts ? least : kMostParts;
+        p.parts = groups < most ? groups : least > most ? least : most;
     } else {
-        const int even = (int)((rows + kMostParts - 1LL) / kMostParts);
+        const int even = (int)((rows + most - 1LL) / most);
         if (even > p.group) p.group = even < 4 * kMostRows ? even : 4 * kMostRows;
         p.parts = (int)((rows + p.group - 1LL) / p.group);
     }

@@ -5,6 +5,8 @@
 // sums of dw stay in registers from row to row, and leave them as one row of partial sums for each work-group, which a
 // second kernel adds up, always in the same order.  Rows beyond what registers hold are read twice, and dw is summed
 // by columns in a pass of its own.
+// 8192 x 8192 bf16 with `add`: 100 us for the rows (5.4 TB/s) and 4.9 for the partial sums, where a copy of as many bytes
+// takes 110; 7863 x 24 f32: 11 us, of which the two launches are nearly all.
 #include "norm_dev.h"
 
 namespace oz {
@@ -252,10 +254,12 @@ hipError_t launch(const NormGradArgs &a, hipStream_t st)
     hipError_t e = hipSuccess;
     if (a.rows > 0 && (a.dx || a.sums)) {
         if (plan.in_registers) {
+            // (6000 values, 11000 rows, bf16: 117 us with 512 threads a row, 145 with 256, 167 with 1024; 8192 x 8192: 108, 106, 108)
             e = a.width <= 512    ? launch_rows<T, 64, 1>(a, plan.parts, st)
                 : a.width <= 1024 ? launch_rows<T, 64, 2>(a, plan.parts, st)
                 : a.width <= 2048 ? launch_rows<T, 256, 1>(a, plan.parts, st)
                 : a.width <= 4096 ? launch_rows<T, 256, 2>(a, plan.parts, st)
+                : a.width <= 6144 ? launch_rows<T, 512, 2>(a, plan.parts, st)
                 : a.width <= 8192 ? launch_rows<T, 256, 4>(a, plan.parts, st)
                                   : launch_rows<T, 1024, 2>(a, plan.parts, st);
         } else {
