@@ -219,7 +219,7 @@ struct Operand {
     }
 
     // Where a lane finds its operands in a stage: fragment() of rows w0 + 16 f ... + 15 (w0: a wavefront's part, a multiple of
-    // 32) and half h of a step is read from `from`, which is reader() behind the operand's place in LDS (a multiple of 1 KB); f
+    // 16) and half h of a step is read from `from`, which is reader() behind the operand's place in LDS (a multiple of 1 KB); f
     // and the swizzle meet in one exclusive or.
     static __device__ __forceinline__ unsigned reader(int w0, int lane)
     {
@@ -488,7 +488,8 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
-        static_assert(3 * FP >= FP + FQ && L == 2 * FP, "reads and copies of a step");
+        constexpr int A = (L + FP - 1) / FP;        // copies to a row: two, of 32 x 64 three
+        static_assert(3 * FP >= FP + FQ && A <= 3, "reads and copies of a step");
         auto nothing = [](auto) __attribute__((always_inline)) {};
         // (every part of the contraction has a step)
 #pragma unroll
@@ -510,7 +511,7 @@ __device__ __forceinline__ void product_tile(const Product &a, float *partial, i
             const T *from_p = P.at((t + R) * KE), *from_q = Q.at((t + R) * KE);
             const unsigned to = lds0 + now * S::kStage;
             half(second, reads, next, [&](auto I) __attribute__((always_inline)) {
-                static_for<2 * I, 2 * I + 2>([&](auto C) __attribute__((always_inline)) {
+                static_for<A * I, A * I + A>([&](auto C) __attribute__((always_inline)) {
                     if constexpr (C < P.N) P.template copy_one<C>(from_p, to, wave);
                     else if constexpr (C < L) Q.template copy_one<C - P.N>(from_q, to + BP * 128, wave);
                 });
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void product_kernel(Product a, float 
 }
 
 // dx, dw and the bias gradient of a layer in one launch: each alone leaves compute units without work in its last round, or
-// in its only one, and costs a launch (500 x 512 x 384 f32: the call 35 us in three launches, 19 in one; 1777 x 1024 x 2304 f16: 63
+// in its only one, and costs a launch (500 x 512 x 384 f32: the call 35 us in three launches, 19 in one with 64 x 64 tiles, 15 with 32 x 64; 1777 x 1024 x 2304 f16: 63
 // and 33).
 template <class T, int BP, int BQ>
 __global__ __launch_bounds__(256) void product_pair_kernel(Product dx, Product dw, BiasGrad db, int blocks_dx, int blocks_dw, int blocks)
@@ -695,15 +696,15 @@ hipError_t launch_product_type(const Product &a, const ProductPlan &plan, float 
     return plan.splits > 1 ? launch_join<T, Out>(a, plan, partial, st) : hipSuccess;
 }
 
-template <class T, int B>
+template <class T, int BP, int BQ>
 hipError_t launch_pair_shape(const Product &dx, const Product &dw, const BiasGrad &db, hipStream_t st)
 {
-    using S = ProductShape<T, B, B, 2, 2>;
-    const long long bx = tile_order_blocks((dx.e.nq + B - 1) / B, (dx.e.np + B - 1) / B, false);
-    const long long bw = tile_order_blocks((dw.e.nq + B - 1) / B, (dw.e.np + B - 1) / B, false);
+    using S = ProductShape<T, BP, BQ, 2, 2>;
+    const long long bx = tile_order_blocks((dx.e.nq + BQ - 1) / BQ, (dx.e.np + BP - 1) / BP, false);
+    const long long bw = tile_order_blocks((dw.e.nq + BQ - 1) / BQ, (dw.e.np + BP - 1) / BP, false);
     const long long blocks = ((bx + 7) & ~7LL) + bw + bias_grad_blocks(db);
     if (blocks > 0x7fffffffLL) return hipErrorInvalidValue;
-    const auto kernel = product_pair_kernel<T, B, B>;
+    const auto kernel = product_pair_kernel<T, BP, BQ>;
     static std::atomic<unsigned long long> done{0};
     if (hipError_t e = allow_dynamic_lds((const void *)kernel, S::kLds, done)) return e;
     kernel<<<dim3(grid_row(blocks), 1, grid_rows(blocks)), S::kThreads, S::kLds, st>>>(dx, dw, db, (int)bx, (int)bw, (int)blocks);
@@ -713,7 +714,13 @@ hipError_t launch_pair_shape(const Product &dx, const Product &dw, const BiasGra
 template <class T>
 hipError_t launch_pair_type(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st)
 {
-    return tile == kTile128 ? launch_pair_shape<T, 128>(dx, dw, db, st) : launch_pair_shape<T, 64>(dx, dw, db, st);
+    if (tile == kTile128) return launch_pair_shape<T, 128, 128>(dx, dw, db, st);
+    if constexpr (sizeof(T) == 4) {
+        // (32 bits: a step's matrix instructions keep a compute unit busy, and half of the units would have none: 500 x 512 x 384 10.7 us instead of 14.6)
+        auto tiles = [](const Product &a) { return ((a.e.np + 63) / 64) * (long long)((a.e.nq + 63) / 64); };
+        if (tiles(dx) + tiles(dw) <= 128) return launch_pair_shape<T, 32, 64>(dx, dw, db, st);
+    }
+    return launch_pair_shape<T, 64, 64>(dx, dw, db, st);
 }
 
 }  // namespace oz
