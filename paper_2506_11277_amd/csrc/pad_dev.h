@@ -1,4 +1,5 @@
-// Copies of operands in front of a product, a chunk of 16 bytes a thread.
+// Copies of operands in front of a product, a chunk of 16 bytes a thread: to aligned rows, or from 8 bits.  Bound by memory; they ride in the
+// launch for dz (948 x 91 -> 768 f16 with x in 8 bits: the call 16 us, with launches of their own 38), or make one themselves.
 #pragma once
 #include "layers.h"
 

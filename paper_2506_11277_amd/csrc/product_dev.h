@@ -2,7 +2,7 @@
 //
 // A work-group owns a tile of BP x BQ entries and walks k in steps of 128 bytes of an operand's row (128 entries of 8 bits, 64 of 16
 // bits, 32 of 32 bits).  Both operands of a step stand in LDS as BP (BQ) * 128 bytes, in a ring of two stages (256 x 256: all
-// that fits) or four: the copies of a step are issued one to three steps before its products, one barrier a step.
+// that fits) or four: the copies of a step are issued one to three steps before its products, one barrier a step.  (Gradients in 32 bits also take 32 x 64.)
 //
 // What bounds it: 256 x 256 in 16 bits the matrix instructions at the clock that the board's power leaves them, with LDS (128 KB read
 // and 64 written a step of 2048 cycles of matrix instructions) close behind: 8192^3 bf16 1.43 PFLOP/s, 4096^3 1.36, 8192 x 4096 x 8192
