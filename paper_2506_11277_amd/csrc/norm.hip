@@ -12,7 +12,8 @@
 namespace oz {
 namespace {
 
-template <class T, int L, int C>
+// SHORT: rows of less than 8 values
+template <class T, int L, int C, bool SHORT>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
 {
     constexpr int ROWS = L < 256 ? 256 / L : 1;
@@ -24,22 +25,28 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
     const T *w = (const T *)a.weight;
 
     // (all loads before the first store, which may be to the residual's place)
+    auto load = [&](Eight<T> &v, const T *from, int at) __attribute__((always_inline)) {
+        if constexpr (SHORT) v.load(from + at, a.width - at);
+        else load_to_end(v, from, at, a.width);
+    };
+    auto end = [&](Eight<T> &v, int at) __attribute__((always_inline)) {
+        if constexpr (!SHORT) ends(v, at, a.width);
+    };
     Eight<T> rx[C], rr[C], rw[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int at = (c * L + t) * 8;
-        rx[c].load(x + at, a.width - at);
-    }
+    for (int c = 0; c < C; ++c) load(rx[c], x, (c * L + t) * 8);
     if (res)
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int at = (c * L + t) * 8;
-            rr[c].load(res + at, a.width - at);
-        }
+        for (int c = 0; c < C; ++c) load(rr[c], res, (c * L + t) * 8);
+    if (w)
+#pragma unroll
+        for (int c = 0; c < C; ++c) load(rw[c], w, (c * L + t) * 8);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int at = (c * L + t) * 8;
-        if (w) rw[c].load(w + at, a.width - at);
+        end(rx[c], at);
+        if (res) end(rr[c], at);
+        if (w) end(rw[c], at);
         else
 #pragma unroll
             for (int i = 0; i < 8; ++i) rw[c].v[i] = (T)1.0f;
@@ -181,7 +188,13 @@ hipError_t launch_rows(const NormArgs &a, hipStream_t st)
     constexpr int ROWS = L < 256 ? 256 / L : 1;
     const long long groups = ((long long)a.rows + ROWS - 1) / ROWS;
     constexpr unsigned line = L > 512 ? kGridRow1024 : kGridRow;
-    norm_kernel<T, L, C><<<dim3(grid_row(groups, line), grid_rows(groups, line)), L < 256 ? 256 : L, 0, st>>>(a);
+    const dim3 grid(grid_row(groups, line), grid_rows(groups, line));
+    if constexpr (L * C == 64)
+        if (a.width < 8) {
+            norm_kernel<T, L, C, true><<<grid, 256, 0, st>>>(a);
+            return hipGetLastError();
+        }
+    norm_kernel<T, L, C, false><<<grid, L < 256 ? 256 : L, 0, st>>>(a);
     return hipGetLastError();
 }
 

@@ -46,6 +46,27 @@ __device__ __forceinline__ SumAndTop over_row(float sum, unsigned top, SumAndTop
     return SumAndTop{sum, top};
 }
 
+// 8 values of a row from `at` on, of a row that has 8: at its end the 8 that end there, which ends() moves to their places, with zeros behind
+// them.  (No decision stands before the load, behind which
+// the next would wait: gradients of 8000 x 7001 bf16 130 -> 114 us, 40000 x 800 74 -> 66.)
+template <class T>
+__device__ __forceinline__ void load_to_end(Eight<T> &v, const T *row, int at, int width)
+{
+    __builtin_memcpy(&v.v, row + (at < width - 8 ? at : width - 8), sizeof v.v);
+}
+template <class T>
+__device__ __forceinline__ void ends(Eight<T> &v, int at, int width)
+{
+    const int over = at - (width - 8);
+    if (over <= 0) return;
+#pragma unroll
+    for (int by = 4; by > 0; by /= 2)
+        if (over & by)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v.v[i] = i + by < 8 ? v.v[i + by < 8 ? i + by : 0] : (T)0;
+    if (over >= 8) v.v = (T)0;
+}
+
 // Bits of |x|: ordered as the magnitudes are, infinities and then NaN above all numbers.
 __device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 constexpr unsigned kInfinity = 0x7f800000u;
