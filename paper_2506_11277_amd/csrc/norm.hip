@@ -202,14 +202,15 @@ template <class T>
 hipError_t launch(const NormArgs &a, hipStream_t st)
 {
     if (a.rows == 0) return hipSuccess;
-    // (where many rows fill the machine, fewer threads with more of a row each: 30000 x 1500 bf16 to 8 bits 63 us by wavefronts, 77 with 256
-    // threads a row, but 64 x 1500 4.9 instead of 3.9; 11000 x 6000 90 us with 512 threads, 104 with 256; 9370 values 94 us with 512, 134 with 1024;
-    // 16384 values 84.5, 94; 30000 values 99 from registers, 114 in two passes; 20000 values 104 either way)
+    // (Threads a row, bf16.  Where many rows fill the machine, as few as hold it: 30000 x 1500 to 8 bits 58 us by wavefronts, 65 with 256;
+    // 16384 x 4096 80 and the norm alone 39 with 256, 81 and 42 with 512.  Fewer rows, more threads: 1 x 4096 3.1 us with 512, 3.4 with 256; 64 x 6000
+    // 4.7 with 512, 5.8 with 256.  9370 values 86 us with 512, 131 with 1024; 16384 values 84, 98; 30000 values 96 from registers, 114 in two
+    // passes; 20000 values 102 either way.)
     if (a.width <= 512) return launch_rows<T, 64, 1>(a, st);
     if (a.width <= 1024) return launch_rows<T, 64, 2>(a, st);
     if (a.width <= 1536 && a.rows >= 2048) return launch_rows<T, 64, 3>(a, st);
     if (a.width <= 2048) return launch_rows<T, 256, 1>(a, st);
-    if (a.width <= 4096) return launch_rows<T, 256, 2>(a, st);
+    if (a.width <= 4096) return a.rows <= 256 ? launch_rows<T, 512, 1>(a, st) : launch_rows<T, 256, 2>(a, st);
     if (a.width <= 8192) return launch_rows<T, 512, 2>(a, st);
     if (a.width <= 12288) return launch_rows<T, 512, 3>(a, st);
     if (a.width <= 16384) return launch_rows<T, 512, 4>(a, st);

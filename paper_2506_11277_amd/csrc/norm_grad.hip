@@ -5,7 +5,7 @@
 // sums of dw stay in registers from row to row, and leave them as one row of partial sums for each work-group, which a
 // second kernel adds up, always in the same order.  Rows beyond what registers hold are read twice, and dw is summed
 // by columns in a pass of its own.
-// 8192 x 8192 bf16 with `add`: 100 us for the rows (5.4 TB/s) and 4.9 for the partial sums, where a copy of as many bytes
+// 8192 x 8192 bf16 with `add`: 98 us for the rows (5.5 TB/s) and 4.9 for the partial sums, where a copy of as many bytes
 // takes 110; 7863 x 24 f32: 11 us, of which the two launches are nearly all.
 #include "norm_dev.h"
 
@@ -52,7 +52,7 @@ __device__ __forceinline__ float input_grad(const RowGrad &s, float h, float g)
 
 // SHORT: rows of less than 8 values, and of 32 bits for 1024 threads, which have no registers for more.  Rows of up to 2048 values: the next one
 // is on its way while one's gradients are formed (40000 x 800 bf16 66 -> 51 us, 30000 x 1500 82 -> 77, 20000 x 512 24 -> 20; of 8192 values that
-// takes the registers of a second work-group, 107 -> 112, of 6000 107 either way).
+// takes the registers of a second work-group, 107 -> 112).
 template <class T, int L, int C, bool ADD, bool SHORT>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_grad_kernel(NormGradArgs a)
 {
@@ -308,13 +308,12 @@ hipError_t launch(const NormGradArgs &a, hipStream_t st)
     hipError_t e = hipSuccess;
     if (a.rows > 0 && (a.dx || a.sums)) {
         if (plan.in_registers) {
-            // (6000 values, 11000 rows, bf16: 117 us with 512 threads a row, 145 with 256, 167 with 1024; 8192 x 8192: 108, 106, 108)
+            // (8192 values, bf16: 104 us with 512 threads a row, 107 with 256; 7001 111, 114; 9370 132 with 1024 as with 512)
             e = a.width <= 512    ? launch_rows<T, 64, 1>(a, plan.parts, st)
                 : a.width <= 1024 ? launch_rows<T, 64, 2>(a, plan.parts, st)
                 : a.width <= 2048 ? launch_rows<T, 256, 1>(a, plan.parts, st)
                 : a.width <= 4096 ? launch_rows<T, 256, 2>(a, plan.parts, st)
-                : a.width <= 6144 ? launch_rows<T, 512, 2>(a, plan.parts, st)
-                : a.width <= 8192 ? launch_rows<T, 256, 4>(a, plan.parts, st)
+                : a.width <= 8192 ? launch_rows<T, 512, 2>(a, plan.parts, st)
                                   : launch_rows<T, 1024, 2>(a, plan.parts, st);
         } else {
             // (where dx takes the place of what the columns are summed from, it is formed behind them)

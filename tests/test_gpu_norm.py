@@ -15,7 +15,7 @@ EPS = 1e-5
 # (tokens, width): a row of a wavefront, of a work-group, of more than registers hold; ends inside a group of 8 and inside a wavefront
 SIZES = [(1, 1), (5, 2), (3, 7), (4, 8), (9, 9), (1, 64), (70, 65), (6, 511), (1, 512), (7, 513), (300, 1000), (3, 1024), (2, 1025), (33, 2048),
          (1, 2049), (5, 4095), (1, 4096), (3, 4104), (1, 8192), (2, 8200), (3, 16384), (2, 16385), (1, 20001), (2, 70000), (0, 16), (3, 0),
-         (2050, 1201), (8195, 1536), (2051, 1544), (8200, 2047), (3, 6144), (3, 6150), (2, 9001), (3, 12288), (2, 12300), (2, 24577), (3, 32768), (2, 32776)]
+         (2050, 1201), (8195, 1536), (2051, 1544), (8200, 2047), (3, 6144), (3, 6150), (2, 9001), (3, 12288), (2, 12300), (2, 24577), (3, 32768), (2, 32776), (257, 2100), (300, 4096)]
 
 
 def values(shape, kind, seed, std=1.0):
