@@ -4,8 +4,8 @@
 //
 // Bound by memory: every value is read once, into registers, and written once.  A row is a wavefront's (no barriers) or
 // a work-group's, C groups of 8 values a thread; rows beyond the largest of these are read twice, in a loop.
-// 8192 x 8192 bf16 with a residual to 8 bits: 79 us (6 TB/s; a copy of as many bytes takes 96); to 8 bits alone: 31 us, of a copy's 41;
-// one row of 4096: 2.7 us, a launch and one trip to memory.
+// 8192 x 8192 bf16 with a residual to 8 bits: 82 us, 16384 x 4096 80 (5.9 TB/s; a copy of as many bytes takes 96); to 8 bits alone: 30 us, of a copy's 41;
+// one row of 4096: 2.4 us, a launch and one trip to memory.
 // h^2 that leaves the range: h 2^-80 and r 2^80 take their places (a product with a power of two is exact).
 #include "norm_dev.h"
 
