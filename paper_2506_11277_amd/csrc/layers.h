@@ -116,10 +116,10 @@ inline NormGradPlan plan_norm_grad(int rows, int width)
 {
     // (and no more than 1024 rows one behind the other in a sum of 32 bits)
     NormGradPlan p{width <= 16384, 0, 64};
-    // (one row at a time in a work-group of 256 threads: 1024 groups keep the memory busy, 16384 x 2048 bf16 54.5 us instead of 60,
-    // 30000 x 1500 77 instead of 114, but 2000 x 2000 f32 20.7 instead of 19.6)
+    // (rows of 1025 to 1536 values leave many of 256 threads without one, and more work-groups make up for it: 30000 x 1500 bf16 77 us with 1024 parts, 94
+    // with 512, but 16384 x 2048 53.5 with 1024, 48.5 with 512)
     constexpr int kMostRows = 1024;
-    const int most = width > 1024 && width <= 2048 && rows >= 8192 ? 1024 : 512;
+    const int most = width > 1024 && width <= 1536 && rows >= 8192 ? 1024 : 512;
     if (p.in_registers) {
         const int each = width <= 1024 ? 4 : 1, groups = (int)((rows + each - 1LL) / each), least = (int)((groups + kMostRows - 1LL) / kMostRows);
         p.parts = groups < most ? groups : least > most ? least : most;
