@@ -176,9 +176,10 @@ int ozimmu_linear8(int tokens, int n_in, int n_out, int type, const int8_t *x, i
  * ozimmu_linear_grad with operands that the forward pass kept in 8 bits.  x, w and pre each are of `type` where their scale is NULL, and int8_t
  * with x_scale [tokens], w_scale [n_out], pre_scale [tokens] otherwise, standing for code * scale.  (The rounding to 8 bits is
  * taken as the identity.)  dz = dy * act'(pre) from the unrounded values of pre; db is summed from the unrounded dz.  In 16 bits dz is the
- * only operand of the products that is rounded: a scale is m 2^e, code 2^e is exact, and m (1 <= m < 2) goes into dz before it is rounded and out of the
- * sums behind (so that a float16 dz becomes an infinity from 65504, 32752 or 16376 on, as none, one or both of x and w are in 8 bits; a float16 code 2^e
- * below 2^-14 is rounded to a multiple of 2^-24).  Scales are read also where their operand is not (x without dw, w without dx).
+ * only operand of the products that is rounded: a scale is m 2^e, code 2^e is exact, and m (1/2 <= m < 1) goes into dz before it is rounded and out of the
+ * sums behind, so that dz keeps its type's range (of scales from 256 on, in bfloat16 2^120, 2^e stays 256, 2^120, and m takes the rest, for codes to stay finite;
+ * a float16 dz m below 2^-14, or code 2^e, is rounded to a multiple of 2^-24).  With OZIMMU_F32 nothing is rounded to 16 bits.  Scales are read also where
+ * their operand is not (x without dw, w without dx).
  * Workspace: as for ozimmu_linear_grad, with room for the values of x and w that are in 8 bits (x8, w8 = 1); `aligned` of dy and of x and w that
  * are not.
  */

@@ -28,7 +28,7 @@ __device__ __forceinline__ void grad_rows_of(const GradInput &a, long long first
             pre.load((const Pre *)a.pre + (size_t)r * a.ldpre + c, FULL ? 8 : n);
             if constexpr (EIGHT) scale = a.pre_scale[r];
         }
-        if (SPLIT && a.x_scale) m = split_scale(a.x_scale[r]).m;
+        if (SPLIT && a.x_scale) m = split_scale<T>(a.x_scale[r]).m;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             d[i] = dy[i];
@@ -56,10 +56,10 @@ __device__ __forceinline__ void grad_input(const GradInput &a, int strip, int gr
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0}, factor[8];
     if constexpr (SPLIT) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) factor[i] = a.w_scale && i < n ? a.w_scale[c + i] : 1.0f;
+        for (int i = 0; i < 8; ++i) factor[i] = a.w_scale && i < n ? a.w_scale[c + i] : 0.0f;       // (0: m = 1)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            factor[i] = split_scale(factor[i]).m;
+            factor[i] = split_scale<T>(factor[i]).m;
             if (a.w_scale && i < n && group == 0 && wave == 0) a.w_inverse[c + i] = 1.0f / factor[i];
         }
     }

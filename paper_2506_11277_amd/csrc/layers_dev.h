@@ -395,15 +395,20 @@ __device__ __forceinline__ void finish_row(const Epilogue &e, int q, int p, floa
     finish_values<S, T>(e, q, p, v);
 }
 
-// A scale as m 2^e, 1 <= m < 2, and its sign with the power: code * power is exact in 16 bits (8 binary digits; float16: where it is in its range),
-// so that of an operand held in 8 bits only m has to go elsewhere.  Scales that are 0 or not finite stay whole.
+// A scale as m 2^e, 1/2 <= m < 1, and its sign with the power: code * power is exact in 16 bits (8 binary digits; float16: where it is in its range),
+// so that of an operand held in 8 bits only m has to go elsewhere: into dz, which with m below 1 stays in its type's range.  (Half of that range was lost with
+// each operand in 8 bits where m was 1 to 2.)  The power is 2^8 (bfloat16: 2^120) at most, so that no code's value leaves the range, and m takes the rest of
+// larger scales.  Scales that are 0 or not finite stay whole.
 struct SplitScale {
     float m, power;
 };
+template <class T>
 __device__ __forceinline__ SplitScale split_scale(float s)
 {
+    constexpr int kMost = std::is_same_v<T, f16> ? 8 : 120;
     if (s == 0.0f || !(fabsf(s) < __uint_as_float(0x7f800000u))) return SplitScale{1.0f, s};
-    return SplitScale{2.0f * fabsf(__builtin_amdgcn_frexp_mantf(s)), __builtin_ldexpf(s < 0.0f ? -1.0f : 1.0f, __builtin_amdgcn_frexp_expf(s) - 1)};
+    const int e = __builtin_amdgcn_frexp_expf(s), over = e > kMost ? e - kMost : 0;
+    return SplitScale{__builtin_ldexpf(fabsf(__builtin_amdgcn_frexp_mantf(s)), over), __builtin_ldexpf(s < 0.0f ? -1.0f : 1.0f, e - over)};
 }
 
 // ---- launchers, one set per element type (product_bf16.hip, product_f16.hip, product_f32.hip)

@@ -22,7 +22,7 @@ __device__ __forceinline__ void pad_chunk(const PadCopies &a, long long i)
     if constexpr (sizeof(T) > 1)
         if (c.scale) {
             const int8_t *const from = (const int8_t *)c.from + row * c.ld + k;
-            const float scale = sizeof(T) == 2 ? split_scale(c.scale[row]).power : c.scale[row];
+            const float scale = sizeof(T) == 2 ? split_scale<T>(c.scale[row]).power : c.scale[row];
             float v[E];
             if (k + E <= c.cols) {
                 typedef int8_t V __attribute__((ext_vector_type(E)));

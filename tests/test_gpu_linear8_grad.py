@@ -1,5 +1,6 @@
 """ozimmu_linear8_grad against 64-bit forms, and the layers in 8 bits together: a block's step, captured, on other streams."""
 import itertools
+import math
 
 import pytest
 
@@ -256,3 +257,34 @@ def test_blocks_on_two_streams():
                 got.append(b.step())
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for i, g in enumerate(got) for p, q in zip(g, want[i % 2]))
+
+
+@pytest.mark.parametrize("held", [(True, False, True), (False, True, False), (True, True, False), (True, True, True)])
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+def test_gradients_up_to_their_types_range(kind, held):
+    # what linear_grad takes stays finite: dz up to 60000 (bfloat16: 3e38), beside scales of every m in [1, 2)
+    gen = generator(17)
+    tokens, n_in, n_out = 70, 48, 40
+    most = 6e4 if kind == "f16" else 3e38
+    dy = (torch.empty(tokens, n_out, device="cuda").uniform_(1 / 3, 1.0, generator=gen) * most).to(TYPES[kind])
+    dy[1::2] *= -1
+    x, w = (torch.empty(rows, n_in, device="cuda").uniform_(-1.0, 1.0, generator=gen) * 2.0 ** -9 for rows in (tokens, n_out))
+    x, w = (v * torch.linspace(1.0, 2.0, v.shape[0], device="cuda")[:, None] for v in (x, w))
+    (x, xs, X), (w, ws, W) = (held_rows(v, h, kind, 0) for v, h in zip((x, w), held))
+    z = torch.empty(tokens, n_out, device="cuda").uniform_(1.0, 2.0, generator=gen)
+    z, zs, Z = held_rows(z, held[2], kind, 0)
+    check(layers.linear8_grad(dy, x, w, z, layers.ACT_RELU, x_scale=xs, w_scale=ws, pre_scale=zs, bias=False), dy, X, W, Z, "relu", kind, held)
+
+
+@pytest.mark.parametrize("kind,scales", [("f16", (200.0, 1e5)), ("bf16", (2.0 ** 119, 3e38))])
+def test_codes_whose_values_leave_the_range_of_16_bits(kind, scales):
+    # the values that they stand for are finite in 64 bits (beyond 65504, or 2^128), and so are the results
+    gen = generator(18)
+    x8, w8 = (torch.randint(-128, 128, (rows, 40), dtype=torch.int8, device="cuda", generator=gen) for rows in (70, 24))
+    x8[0], w8[0] = -128, -128
+    xs, ws = (torch.empty(rows, device="cuda").uniform_(0.0, 1.0, generator=gen).mul_(math.log(scales[1] / scales[0])).exp_().mul_(scales[0]) for rows in (70, 24))
+    dy = (torch.randn(70, 24, device="cuda", generator=gen) * (2.0 ** -12 if kind == "f16" else 1e-8)).to(TYPES[kind])
+    X, W = x8.double() * xs.double()[:, None], w8.double() * ws.double()[:, None]
+    Z = torch.zeros(70, 24, device="cuda").double()
+    dx, dw, _ = layers.linear8_grad(dy, x8, w8, x_scale=xs, w_scale=ws, bias=False)
+    check((dx, dw, None), dy, X, W, Z, "none", kind, (True, True, False))
