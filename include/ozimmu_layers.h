@@ -14,7 +14,8 @@
  *     into HIP graphs (kernels only) and return one of the OZIMMU_* status codes; nothing throws or aborts.
  *   - Outputs must not overlap inputs or each other unless an entry point says so.
  *   - Sums, activations and statistics are formed in 32 bits; what is written in 16 bits is rounded to nearest once.
- *     Results are deterministic (no atomics on floating-point values; the order of every sum is fixed by the sizes).
+ *     Results are deterministic: no atomics on floating-point values; the order of every sum is fixed by the sizes, the type, which
+ *     rows start on 16 bytes, the room in the workspace and which results are asked for (dw alone may be summed in other parts than beside dx).
  *   - NaN and infinities go where the formulas take them; no entry point looks for them.
  *   - Sizes of 0 are accepted: no tokens or no output features write nothing, n_in = 0 gives products of 0.  Sizes up to
  *     2^30 - 1 (ozimmu_moe's width and hidden: 2^24), offsets in 64 bits.

@@ -259,7 +259,7 @@ int linear_grad(int tokens, int n_in, int n_out, int type, const void *dy, int l
         if (workspace_bytes >= wider.total) ws = wider;
     }
 
-    // (also where only one of dx and dw is wanted: either has the same bits alone)
+    // (also where only one of dx and dw is wanted: the products' operands are the same whichever is, and only the order of their sums goes by that)
     const bool split_x = ws.split && x8, split_w = ws.split && w8;
     const bool own_dz = n_out > 0 && (dx || dw) && (activation || split_x || split_w || (ws.has_dz && !dy_fits));
     const void *dz = dy;

@@ -181,8 +181,8 @@ def linear_grad_workspace_bytes(tokens, n_in, n_out, dtype, activation=ACT_NONE,
 def linear_grad(dy, x, w, pre=None, activation=ACT_NONE, bias=True, dx=None, dw=None, db=None, want=("dx", "dw"), workspace=None):
     """Gradients (dx, dw, db) of linear from dy [tokens, n_out], its x, w and `pre` (not needed for ACT_NONE).
 
-    db is None with bias=False; of dx and dw those in `want` are formed, the others are None.  Given tensors receive
-    the results.  The gradient of linear's residual is dy itself."""
+    db is None with bias=False; of dx and dw those in `want` are formed, the others are None (what is formed together may be summed in
+    another order than alone).  Given tensors receive the results.  The gradient of linear's residual is dy itself."""
     kind = _type_of(dy, "dy")
     try:
         (tokens, n_out), (_, n_in) = dy.shape, x.shape

@@ -288,3 +288,15 @@ def test_codes_whose_values_leave_the_range_of_16_bits(kind, scales):
     Z = torch.zeros(70, 24, device="cuda").double()
     dx, dw, _ = layers.linear8_grad(dy, x8, w8, x_scale=xs, w_scale=ws, bias=False)
     check((dx, dw, None), dy, X, W, Z, "none", kind, (True, True, False))
+
+
+@pytest.mark.parametrize("kind,shape", [("bf16", (2048, 256, 256)), ("f32", (500, 512, 384))])
+@pytest.mark.parametrize("held", HELD[:4])
+def test_gradients_asked_for_alone(kind, shape, held):
+    # alone, dx or dw may be summed in other parts than in the launch for both: the bounds hold either way, and a call repeats itself
+    _, (dy, x, w, z), given = run(shape, kind, 0, "gelu", held)
+    X, W, Z = (v.double() * s.double()[:, None] if s is not None else v.double() for v, s in ((x, given["x_scale"]), (w, given["w_scale"]), (z, given["pre_scale"])))
+    for want, bias in ((("dx",), True), (("dw",), True), (("dw",), False), (("dx", "dw"), False)):
+        got, again = (layers.linear8_grad(dy, x, w, z, want=want, bias=bias, **given) for _ in range(2))
+        check(got, dy, X, W, Z, "gelu", kind, held)
+        assert all((a is None and b is None) or torch.equal(a, b) for a, b in zip(got, again))
