@@ -159,3 +159,18 @@ def test_entries_beyond_32_bit_offsets():
     dy = values(rows, 8)
     w = values(8, 136, seed=3)
     assert all(torch.equal(a, b) for a, b in zip(layers.linear8_grad(dy, codes, w, x_scale=scale), layers.linear8_grad(dy, want[0], w, x_scale=scale)))
+
+
+@pytest.mark.parametrize("cols,line", [(1600, 1 << 22), (4104, 1 << 22), (24584, 1 << 21)])
+def test_more_rows_than_one_line_of_the_grid_of_every_kernel(cols, line):
+    # 256, 512 and 1024 threads a row, rows in registers
+    rows = line + 5
+    x = values(rows, cols)
+    print(cols, flush=True)
+    codes, scale = layers.quantise(x)
+    torch.cuda.synchronize()
+    assert bool((scale > 0).all())
+    for i, j in ((0, 8), (line // 2 - 3, line // 2 + 3), (line - 3, rows)):
+        want, top = codes_of(x[i:j].float())
+        assert torch.equal(codes[i:j].cpu(), want)
+        assert bool(((scale[i:j].double().cpu() - top).abs() <= 2 * U32 * top).all())
