@@ -110,7 +110,7 @@ int ozimmu_calibration_copy(void *dst, const void *src, size_t bytes, void *stre
  * ozimmu_debug_linear_tile: edge of the tiles in which ozimmu_linear (which = 0), or the dx (1) and dw (2) of ozimmu_linear_grad, multiply
  *   operands of these sizes and this type (of ozimmu_layers.h; with which = 0 also 8: ozimmu_linear8) whose rows all start and end on 16 bytes (aligned = 1) or do not and
  *   are not copied (0); 16 for the kernel for few tokens; which = 3: of the one launch that forms dx, dw and the bias gradient of
- *   aligned operands, 0 where they are formed in launches of their own.
+ *   aligned operands (32: tiles of 32 x 64), 0 where they are formed in launches of their own.
  *   *parts [host], may be NULL, receives the parts of the contraction.  Host only; OZIMMU_BAD_ARG (1) for other arguments.
  */
 int ozimmu_debug_linear_tile(int which, int tokens, int n_in, int n_out, int type, int aligned, int *parts);

@@ -451,7 +451,7 @@ constexpr unsigned kGridRow = 1u << 22, kGridRow1024 = kGridRow / 2;
 inline unsigned grid_row(long long groups, unsigned row = kGridRow) { return groups < row ? (unsigned)groups : row; }
 inline unsigned grid_rows(long long groups, unsigned row = kGridRow) { return (unsigned)((groups + row - 1) / row); }
 
-enum Tile { kTile256, kTile128, kTile64, kTileFew };      // edge; few_tokens_kernel
+enum Tile { kTile256, kTile128, kTile64, kTileFew, kTile32 };      // edge; few_tokens_kernel; 32 x 64 (both gradients in one launch, 32 bits)
 struct ProductPlan {
     int tile;
     int splits, steps;       // the contraction in `splits` parts of `steps` steps of 128 bytes

@@ -715,11 +715,8 @@ template <class T>
 hipError_t launch_pair_type(const Product &dx, const Product &dw, const BiasGrad &db, int tile, hipStream_t st)
 {
     if (tile == kTile128) return launch_pair_shape<T, 128, 128>(dx, dw, db, st);
-    if constexpr (sizeof(T) == 4) {
-        // (32 bits: a step's matrix instructions keep a compute unit busy, and half of the units would have none: 500 x 512 x 384 10.7 us instead of 14.6)
-        auto tiles = [](const Product &a) { return ((a.e.np + 63) / 64) * (long long)((a.e.nq + 63) / 64); };
-        if (tiles(dx) + tiles(dw) <= 128) return launch_pair_shape<T, 32, 64>(dx, dw, db, st);
-    }
+    if constexpr (sizeof(T) == 4)
+        if (tile == kTile32) return launch_pair_shape<T, 32, 64>(dx, dw, db, st);
     return launch_pair_shape<T, 64, 64>(dx, dw, db, st);
 }
 

@@ -192,3 +192,10 @@ def test_sizes_up_to_the_largest_are_taken():
     for rows, cols, ld in ((2, MOST, (1 << 31) - 1), (MOST, 1, 1), (0, MOST, MOST), (1, 8, 1 << 40), (5, 7, 7), (5, 7, 9)):
         x = torch.empty_strided((rows, cols), (ld, 1), dtype=torch.int8, device="meta")
         assert layers._like(x, x.shape, torch.int8, x.get_device(), "x") == (ld if rows > 1 else cols)
+
+
+def test_tiles_of_both_gradients(handle):
+    # 32 bits: 32 x 64 where tiles of 64 would leave half of the compute units without one
+    tile = handle.ozimmu_debug_linear_tile
+    assert [tile(3, *shape, 2, 1, None) for shape in ((500, 512, 384), (1000, 512, 384), (512, 512, 512), (512, 576, 512), (1536, 183121, 1629))] == [32, 64, 32, 64, 128]
+    assert tile(3, 500, 512, 384, 0, 1, None) == 64
