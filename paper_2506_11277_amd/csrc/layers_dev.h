@@ -350,7 +350,7 @@ __device__ __forceinline__ void finish_values(const Epilogue &e, int q, int p, f
         for (int i = 0; i < 8; ++i) {
             if (p + i >= e.np) continue;
             if (e.pre) ((T *)e.pre)[(size_t)q * e.ldpre + p + i] = (T)v[i];
-            float z = activate_sum<S, T>(e.act, v[i]);
+            float z = activate<T>(e.act, v[i]);
             if (e.residual) z += r[i];
             ((T *)e.out)[(size_t)q * e.ldo + p + i] = (T)z;
         }

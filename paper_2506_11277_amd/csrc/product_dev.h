@@ -351,19 +351,19 @@ template <class T, class Out, bool QS, int ACT, int PW, int QW>
 __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float *sums, int q0, int p0, int lane)
 {
     constexpr int LD = PW + 4, W = PW < 64 ? PW : 64, ROWS = 64 / W, R = PW == 32 ? 16 : 4;
-    static_assert(QW % (ROWS * R) == 0, "");
+    static_assert(sizeof(T) > 1 && QW % (ROWS * R) == 0, "");
 #pragma nounroll
     for (int c = lane % W; c < PW; c += W) {
         const int p = p0 + c;
         if (p >= e.np) break;
-        const float bias = e.bias ? (float)((const Out *)e.bias)[p] : 0.0f, p_scale = sizeof(T) == 1 ? e.p_scale[p] : 0.0f;
+        const float bias = e.bias ? (float)((const Out *)e.bias)[p] : 0.0f;
 #pragma nounroll
         for (int s = lane / W; s < QW && q0 + s < e.nq; s += R * ROWS) {
             float v[R], res[R];
 #pragma unroll
             for (int y = 0; y < R; ++y) {
                 const int q = q0 + s + y * ROWS;
-                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], QS && (sizeof(T) == 1 || e.q_scale) && q < e.nq ? e.q_scale[q] : 1.0f, p_scale, bias);
+                v[y] = scaled<T>(sums[(s + y * ROWS) * LD + c], QS && e.q_scale && q < e.nq ? e.q_scale[q] : 1.0f, 1.0f, bias);
                 res[y] = e.residual && q < e.nq ? (float)((const Out *)e.residual)[(size_t)q * e.ldr + p] : 0.0f;
             }
 #pragma unroll
@@ -371,7 +371,7 @@ __device__ __forceinline__ void epilogue_entries(const Epilogue &e, const float 
                 const int q = q0 + s + y * ROWS;
                 if (q >= e.nq) continue;
                 if (e.pre) ((Out *)e.pre)[(size_t)q * e.ldpre + p] = (Out)v[y];
-                float x = activate_sum<T, Out>(ACT, v[y]);
+                float x = activate<Out>(ACT, v[y]);
                 if (e.residual) x += res[y];
                 ((Out *)e.out)[(size_t)q * e.ldo + p] = (Out)x;
             }
