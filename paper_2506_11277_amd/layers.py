@@ -361,14 +361,14 @@ def _first(x, what):
 
 def _like(x, shape, dtype, index, what):
     """Row stride of a [rows, cols] device tensor of this type, as _ld; the plain case first (a third of the time)."""
-    if x.dtype is dtype and x.shape == shape and x.get_device() == index:
+    if x is not None and x.dtype is dtype and x.shape == shape and x.get_device() == index:
         return (shape[1] or 1) if x.is_contiguous() and not (shape[0] | shape[1]) >> 30 else _ld(x, shape[0], shape[1], x, what)
     raise ValueError(f"{what}: {list(shape)} of {dtype} on cuda:{index} expected")
 
 
 def _line(x, n, dtype, index, what):
     """Address of a contiguous vector."""
-    if x.dtype is dtype and x.shape == (n,) and x.get_device() == index and x.is_contiguous():
+    if x is not None and x.dtype is dtype and x.shape == (n,) and x.get_device() == index and x.is_contiguous():
         return x.data_ptr()
     raise ValueError(f"{what}: contiguous [{n}] of {dtype} on cuda:{index} expected")
 

@@ -199,3 +199,11 @@ def test_tiles_of_both_gradients(handle):
     tile = handle.ozimmu_debug_linear_tile
     assert [tile(3, *shape, 2, 1, None) for shape in ((500, 512, 384), (1000, 512, 384), (512, 512, 512), (512, 576, 512), (1536, 183121, 1629))] == [32, 64, 32, 64, 128]
     assert tile(3, 500, 512, 384, 0, 1, None) == 64
+
+
+def test_what_is_not_given_is_refused():
+    from paper_2506_11277_amd import layers
+    with pytest.raises(ValueError):
+        layers._line(None, 4, torch.float32, 0, "x_scale")
+    with pytest.raises(ValueError):
+        layers._like(None, (4, 8), torch.int8, 0, "w")
