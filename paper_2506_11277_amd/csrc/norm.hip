@@ -99,12 +99,14 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
     for (int c = 0; c < C; ++c) {
         const int at = (c * L + t) * 8;
         float p[8];
+        if (a.codes) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = h[c][i] * rw[c][i];
-        if (a.codes) store_codes(a.codes + (size_t)row * a.ldc + at, a.width - at, p, scale);
-        if (a.y) {
+            for (int i = 0; i < 8; ++i) p[i] = h[c][i] * rw[c][i];
+            store_codes(a.codes + (size_t)row * a.ldc + at, a.width - at, p, scale);
+        }
+        if (a.y) {                                              // (h r first: h w may leave the range)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] *= r;
+            for (int i = 0; i < 8; ++i) p[i] = h[c][i] * r * rw[c][i];
             store8((T *)a.y + (size_t)row * a.ldy + at, a.width - at, p);
         }
     }
@@ -167,16 +169,19 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
         Eight<T> rw;
         values(at, h, rw);                                      // (this thread's values: what total replaces, it has read)
         if (a.total) store8((T *)a.total + (size_t)row * a.ldt + at, a.width - at, h);
+        float p[8];
+        if (a.codes) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = h[i] * factor;
-            h[i] = v * rw[i];
+            for (int i = 0; i < 8; ++i) {
+                const float v = h[i] * factor;
+                p[i] = v * rw[i];
+            }
+            store_codes(a.codes + (size_t)row * a.ldc + at, a.width - at, p, scale);
         }
-        if (a.codes) store_codes(a.codes + (size_t)row * a.ldc + at, a.width - at, h, scale);
         if (a.y) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] *= r;
-            store8((T *)a.y + (size_t)row * a.ldy + at, a.width - at, h);
+            for (int i = 0; i < 8; ++i) p[i] = h[i] * factor * r * rw[i];
+            store8((T *)a.y + (size_t)row * a.ldy + at, a.width - at, p);
         }
     }
     if (a.scale && threadIdx.x == 0) a.scale[row] = scale.scale == 0.0f ? 0.0f : scale.scale * r;

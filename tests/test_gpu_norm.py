@@ -311,3 +311,14 @@ def test_one_tensor_for_several_arguments():
     x, weight = values((9, 300), "bf16", 1), values((300,), "bf16", 3)
     assert all(torch.equal(a, b) for a, b in zip(layers.rms_norm8(x, weight, x), layers.rms_norm8(x, weight, x.clone())))
     assert all(torch.equal(a, b) for a, b in zip(layers.rms_norm_grad(x, x, weight, add=x), layers.rms_norm_grad(x, x.clone(), weight, add=x.clone())))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [24, 600, 3000, 20000])
+def test_norms_of_large_and_small_weights(width, kind):
+    # h weight may leave the range of 32 bits where h r weight does not
+    for size, gain in ((1e12, 1e30), (1e20, 1e-36), (1e-3, 1e-36), (1.0, 1e37)):
+        x, weight = values((3, width), kind, 1).float().mul(size).to(TYPES[kind]), values((width,), kind, 3).float().mul(gain).to(TYPES[kind])
+        r, want = norm(x, weight, EPS)
+        y, _ = layers.rms_norm(x, weight, eps=EPS)
+        within(y, want, want.abs() * (root_error(width) + 4 * U32) + rounded(want, x.dtype) + 2.0 ** -150, "y")
