@@ -141,8 +141,8 @@ int ozimmu_quantise(int rows, int cols, int type, const void *x, int ldx, int8_t
  *   x, residual, total and y [tokens, width], weight [width], all of `type`; residual and weight may be NULL (zeros, ones).
  * Each of these may be NULL and is then not formed: total receives h; y the norm of the unrounded h; codes [tokens, width] and scale [tokens] the norm
  * in 8 bits, with t = h weight for the codes (r, which is common to the row, goes into the scale: a r / 127).
- * total may be x or residual itself (same pointer and ld).  0 < eps < infinity, as a float.  Where the squares of h leave the range of 32
- * bits the row is taken times 2^-80, so that every finite row has its norm.
+ * total may be x or residual itself (same pointer and ld).  0 < eps < infinity, as a float.  Where the mean of h^2 + eps leaves the range of 32
+ * bits the row is taken times 2^-80, so that every finite row has its norm.  (codes and scale go by h weight: where that leaves the range the scale is NaN.)
  */
 int ozimmu_rms_norm(int tokens, int width, int type, const void *x, int ldx, const void *residual, int ldr, const void *weight,
                     double eps, void *total, int ldt, void *y, int ldy, int8_t *codes, int ldc, float *scale, void *stream);

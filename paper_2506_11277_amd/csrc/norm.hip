@@ -84,15 +84,16 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_kernel(NormArgs a)
     SumAndTop s = statistics(slots[0]);
     float r = 1.0f;
     if (a.norm) {
-        r = inverse_root(s.sum, a.width, a.eps);
-        if (__builtin_expect(!(s.sum < __uint_as_float(kInfinity)), 0)) {       // (the same for the whole row)
+        float mean = mean_of(s.sum, a.width, a.eps);
+        if (__builtin_expect(!in_range(mean), 0)) {                             // (the same for the whole row)
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[c][i] *= kSmaller;
             s = statistics(slots[1]);
-            r = inverse_root(s.sum, a.width, 0.0f);
+            mean = mean_of(s.sum, a.width, a.eps, kSmaller);
         }
+        r = inverse_root(mean);
     }
     const RowScale scale = row_scale(s.top);
 #pragma unroll
@@ -156,12 +157,13 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
     SumAndTop s = statistics(slots[0], 1.0f);
     float r = 1.0f, factor = 1.0f;
     if (a.norm) {
-        r = inverse_root(s.sum, a.width, a.eps);
-        if (!(s.sum < __uint_as_float(kInfinity))) {
+        float mean = mean_of(s.sum, a.width, a.eps);
+        if (!in_range(mean)) {
             factor = kSmaller;
             s = statistics(slots[1], factor);
-            r = inverse_root(s.sum, a.width, 0.0f);
+            mean = mean_of(s.sum, a.width, a.eps, factor);
         }
+        r = inverse_root(mean);
     }
     const RowScale scale = row_scale(s.top);
     for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {

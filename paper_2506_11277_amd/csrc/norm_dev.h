@@ -113,12 +113,14 @@ __device__ __forceinline__ void store_codes(int8_t *p, int n, const float (&t)[8
     }
 }
 
-// where squares of h leave the range of 32 bits, h times this takes its place, and eps, nothing beside them, is left out
+// Where the mean of h^2, or its sum with eps, leaves the range of 32 bits, h times this takes its place, and eps times its square.
 constexpr float kSmaller = 0x1p-80f;
-// 1 / sqrt(mean of the squares + eps)
-__device__ __forceinline__ float inverse_root(float squares, int width, float eps)
+// the mean of the squares + eps, of h times `factor`
+__device__ __forceinline__ float mean_of(float squares, int width, float eps, float factor = 1.0f)
 {
-    return 1.0f / sqrtf(squares / (float)width + eps);
+    return squares / (float)width + eps * factor * factor;
 }
+__device__ __forceinline__ bool in_range(float mean) { return mean < __uint_as_float(kInfinity); }       // (a NaN is not)
+__device__ __forceinline__ float inverse_root(float mean) { return 1.0f / sqrtf(mean); }
 
 }  // namespace oz

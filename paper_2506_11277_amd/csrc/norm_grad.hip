@@ -38,9 +38,9 @@ __device__ __forceinline__ TwoSums sums_over_row(float a, float b, TwoSums *slot
 struct RowGrad {
     float r, mean, factor;
 };
-__device__ __forceinline__ RowGrad row_grad(const TwoSums &s, int width, float eps, float factor)
+__device__ __forceinline__ RowGrad row_grad(float mean, const TwoSums &s, int width, float factor)
 {
-    const float r = inverse_root(s.a, width, factor == 1.0f ? eps : 0.0f);
+    const float r = inverse_root(mean);
     return RowGrad{r, s.b * r / (float)width, factor};
 }
 // (r of h itself is r factor; g and n are of ordinary size, whatever h is)
@@ -119,11 +119,13 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void norm_grad_kernel(NormGradAr
         // (two sets of slots in turn: a row's are read before anyone is behind the next row's barrier)
         RowGrad s;
         const TwoSums first = statistics(1.0f, slots[turn]);
-        if (__builtin_expect(first.a < __uint_as_float(kInfinity), 1)) {
-            s = row_grad(first, a.width, a.eps, 1.0f);
+        const float mean = mean_of(first.a, a.width, a.eps);
+        if (__builtin_expect(in_range(mean), 1)) {
+            s = row_grad(mean, first, a.width, 1.0f);
         } else {
             if constexpr (L > 64) __syncthreads();
-            s = row_grad(statistics(kSmaller, slots[2]), a.width, a.eps, kSmaller);
+            const TwoSums second = statistics(kSmaller, slots[2]);
+            s = row_grad(mean_of(second.a, a.width, a.eps, kSmaller), second, a.width, kSmaller);
             if constexpr (L > 64) __syncthreads();
         }
 #pragma unroll
@@ -219,8 +221,13 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormGradArgs a)
     };
     RowGrad s;
     const TwoSums first = statistics(1.0f, slots[0]);
-    if (first.a < __uint_as_float(kInfinity)) s = row_grad(first, a.width, a.eps, 1.0f);
-    else s = row_grad(statistics(kSmaller, slots[1]), a.width, a.eps, kSmaller);
+    const float mean = mean_of(first.a, a.width, a.eps);
+    if (in_range(mean)) {
+        s = row_grad(mean, first, a.width, 1.0f);
+    } else {
+        const TwoSums second = statistics(kSmaller, slots[1]);
+        s = row_grad(mean_of(second.a, a.width, a.eps, kSmaller), second, a.width, kSmaller);
+    }
     if (a.dx)
         for (int at = threadIdx.x * 8; at < a.width; at += L * 8) {
             float h[8], g[8];

@@ -322,3 +322,18 @@ def test_norms_of_large_and_small_weights(width, kind):
         r, want = norm(x, weight, EPS)
         y, _ = layers.rms_norm(x, weight, eps=EPS)
         within(y, want, want.abs() * (root_error(width) + 4 * U32) + rounded(want, x.dtype) + 2.0 ** -150, "y")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [24, 600, 3000, 20000])
+def test_an_eps_beside_squares_beyond_32_bits(width, kind):
+    # the sum of the squares, or their mean with eps, leaves the range
+    for size, eps in ((2e19, 3e38), (1e18, 3.4e38), (1e19, 3.4e38), (1e25, 3e38)):
+        h, dy, weight = (values(s, kind, i) for i, s in enumerate(((3, width), (3, width), (width,))))
+        h = h.float().clamp(-2.0, 2.0).mul(size).to(h.dtype)
+        r, want = norm(h, weight, eps)
+        y, _ = layers.rms_norm(h, weight, eps=eps)
+        within(y, want, want.abs() * (root_error(width) + 4 * U32) + rounded(want, h.dtype), "y")
+        codes, scale, _ = layers.rms_norm8(h, weight, eps=eps)
+        check_scale(scale, ((h.double() * weight.double()).abs().amax(1) * r[:, 0] / 127).cpu(), root_error(width) + 4 * U32)
+        check_grad(*layers.rms_norm_grad(dy, h, weight, eps), dy, h, weight, None, eps)
