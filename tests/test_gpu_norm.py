@@ -337,3 +337,16 @@ def test_an_eps_beside_squares_beyond_32_bits(width, kind):
         codes, scale, _ = layers.rms_norm8(h, weight, eps=eps)
         check_scale(scale, ((h.double() * weight.double()).abs().amax(1) * r[:, 0] / 127).cpu(), root_error(width) + 4 * U32)
         check_grad(*layers.rms_norm_grad(dy, h, weight, eps), dy, h, weight, None, eps)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("tokens,width", [(1, 1), (5, 7), (300, 1000), (9, 2100), (3, 9001), (2, 20001)])
+def test_the_norm_and_its_8_bits_in_one_call(tokens, width, kind):
+    x, res, weight = values((tokens, width), kind, 1), values((tokens, width), kind, 2), values((width,), kind, 3)
+    want = layers.rms_norm(x, weight, res, EPS) + layers.rms_norm8(x, weight, res, EPS)[:2]
+    got = [torch.zeros_like(t) for t in want]
+    y, total, codes, scale = (t.data_ptr() for t in got)
+    assert layers.lib().ozimmu_rms_norm(tokens, width, layers._TYPES[x.dtype], x.data_ptr(), width, res.data_ptr(), width, weight.data_ptr(), EPS, total, width,
+                                        y, width, codes, width, scale, torch.cuda.current_stream().cuda_stream) == layers.OK
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
