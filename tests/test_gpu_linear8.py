@@ -246,3 +246,18 @@ def test_scales_bias_and_operands_at_any_alignment(shape, kind):
         y = layers.linear8(moved(x, by), moved(xs, by), moved(w, by), moved(ws, by), moved(bias, by), moved(residual, by), layers.ACT_GELU,
                            out=moved(torch.empty_like(want), by))
         assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,n_in", [(3, 16), (40, 16), (300, 16), (300, 16384)])
+def test_gelu_far_from_zero(tokens, n_in, kind):
+    # z is the bias; the header's bounds: 1e-5 of |z| Phi(-|z|) down to -6, 1e-13 beyond (1 + erf has no digits there)
+    x, w = (torch.zeros(n, n_in, dtype=torch.int8, device="cuda") for n in (tokens, 520))
+    bias = torch.linspace(-12.5, 12.5, 520, device="cuda").to(TYPES[kind])
+    y = layers.linear8(x, torch.ones(tokens, device="cuda"), w, torch.ones(520, device="cuda"), bias, activation=layers.ACT_GELU)
+    z = bias.double()
+    tail = z.abs() * 0.5 * torch.erfc(z.abs() * 0.5 ** 0.5)
+    want = z.clamp_min(0.0) - tail
+    error = torch.where(z.abs() <= 6, 1e-5 * tail, 1e-13) + U32 * want.abs()
+    for row in y:
+        within(row, want, error * (1 + ROUND[TYPES[kind]]) + rounded(want, TYPES[kind]), "y")
