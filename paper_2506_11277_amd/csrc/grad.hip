@@ -3,7 +3,7 @@
 // Bound by memory: dy and pre are read once, dz is written once; the column sums ride along in registers.  A work-group
 // owns 512 columns of grad_rows() tokens, its four wavefronts every fourth token; sums meet in LDS, then, one row per
 // work-group of tokens, with the products of dx and dw or in a kernel of their own, always in the same order.
-// 8192 x 8192 bf16 with gelu, 403 MB: 77 us, 5.2 TB/s (the library's erf: 110); from 8 bits, with 8192 x 4096 of x to bf16 beside it, 435 MB: 85 us.
+// 8192 x 8192 bf16 with gelu, 403 MB: 73 to 77 us between products, 5.2 to 5.5 TB/s (the library's erf: 110); from 8 bits, with 8192 x 4096 of x to bf16 beside it, 435 MB: 85 us.
 #include "pad_dev.h"
 
 namespace oz {
@@ -13,20 +13,36 @@ namespace {
 // decisions, the launch takes 7.9 us instead of 6.0 for 500 x 384 f32, silu, and its copies; two rows at a time 80 us instead of 77 for 8192 x 8192 bf16.)
 // FULL: 8 of them in all lanes (8192 x 4096 bf16 from 8 bits, without dz, 36.2 -> 34.6 us, 16384 x 2048 with dz and dx 60.4 -> 59.1).
 //
+// Whole strips of 16 bits with nothing in 8: as many loads as a compute unit can have on their way at once are more than memory serves well (8192 x 8192,
+// where all work-groups are resident), so that a row's dy and pre are asked for in turn.  Of gelu and its tanh form, whose arithmetic is as long as a
+// load, the next row's dy comes during it.  dz, and dx of 8 columns, of 8192 x 8192 bf16 with relu 109.5 -> 104.4 us, silu 111.3 -> 105.6, gelu
+// 114.0 -> 109.0 (dy in turn, and nothing during the arithmetic: 119.6), gelu_tanh 111.1 -> 107.1; 8192 x 4096 with gelu 60.5 -> 58.2.
+//
 // dz of operands in 16 bits, x or w of which is held in 8 (SPLIT): dz m[t] n[o] with the m and n of their scales (split_scale), which leaves
 // the operands exact and the products' rows to be divided by m[t] (dx) and n[o] (dw).
 template <class T, int ACT, bool EIGHT, bool SPLIT, bool FULL>
 __device__ __forceinline__ void grad_rows_of(const GradInput &a, long long first, long long last, bool writes_inverse, int c, int n, const float (&factor)[8], float (&sum)[8])
 {
     typedef std::conditional_t<EIGHT, int8_t, T> Pre;
+    constexpr bool kTurns = FULL && !EIGHT && !SPLIT && sizeof(T) == 2 && ACT != OZIMMU_ACT_NONE;
+    constexpr bool kAhead = kTurns && (ACT == OZIMMU_ACT_GELU || ACT == OZIMMU_ACT_GELU_TANH);
+    Eight<T> next;
+    if (kAhead && first < last) next.load((const T *)a.dy + (size_t)first * a.lddy + c, 8);
     for (long long r = first; r < last; r += 4) {
         Eight<T> dy;
         Eight<Pre> pre;
         float scale = 1.0f, m = 1.0f, d[8];
-        dy.load((const T *)a.dy + (size_t)r * a.lddy + c, FULL ? 8 : n);
+        if constexpr (kAhead) dy = next;
+        else dy.load((const T *)a.dy + (size_t)r * a.lddy + c, FULL ? 8 : n);
         if constexpr (ACT != OZIMMU_ACT_NONE) {
+            if constexpr (kTurns && !kAhead) asm volatile("" : "+v"(dy.v));             // (a wait for it)
             pre.load((const Pre *)a.pre + (size_t)r * a.ldpre + c, FULL ? 8 : n);
             if constexpr (EIGHT) scale = a.pre_scale[r];
+            if constexpr (kAhead) {
+                asm volatile("" : "+v"(pre.v));
+                next.load((const T *)a.dy + (size_t)(r + 4 < last ? r + 4 : r) * a.lddy + c, 8);
+                asm volatile("" ::: "memory");                                          // (the load stays in front of the arithmetic)
+            }
         }
         if (SPLIT && a.x_scale) m = split_scale<T>(a.x_scale[r]).m;
 #pragma unroll
