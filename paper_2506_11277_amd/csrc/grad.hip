@@ -10,7 +10,7 @@ namespace oz {
 namespace {
 
 // Rows first, first + 4, ... of a lane's 8 columns from c on, `n` of them there.  (With a decision on the activation for each value, and loads behind
-// decisions, the launch takes 7.9 us instead of 6.0 for 500 x 384 f32, silu, and its copies; two rows at a time 80 us instead of 77 for 8192 x 8192 bf16.)
+// decisions, the launch takes 7.9 us instead of 6.0 for 500 x 384 f32, silu, and its copies.)
 // FULL: 8 of them in all lanes (8192 x 4096 bf16 from 8 bits, without dz, 36.2 -> 34.6 us, 16384 x 2048 with dz and dx 60.4 -> 59.1).
 //
 // Whole strips of 16 bits with nothing in 8: as many loads as a compute unit can have on their way at once are more than memory serves well (8192 x 8192,

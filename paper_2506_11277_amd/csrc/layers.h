@@ -106,7 +106,7 @@ struct NormGradArgs {
     float eps;
 };
 // Parts of the rows whose sums of dw are formed apart, and how: rows in registers, dw beside them, or in a pass by columns, `group` rows a part.
-// (512 parts at most: with 1024 8192 x 8192 bf16 takes 111 us instead of 106, 2048 x 8192 42 instead of 35, for their sums alone; with two rows a part
+// (Up to 512 parts, 1024 of rows of 1025 to 1536 values where there are many, and more where a part would have more than 1024 rows.  With 1024 8192 x 8192 bf16 takes 111 us instead of 106, 2048 x 8192 42 instead of 35, for their sums alone; with two rows a part
 // at least 512 x 4096 11.4 instead of 12.7, but 64 x 4096 7.4 instead of 6.7 and 1531 x 1001 f16 12.9 instead of 11.9.)
 struct NormGradPlan {
     bool in_registers;

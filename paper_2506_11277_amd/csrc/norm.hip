@@ -4,8 +4,8 @@
 //
 // Bound by memory: every value is read once, into registers, and written once.  A row is a wavefront's (no barriers) or
 // a work-group's, C groups of 8 values a thread; rows beyond the largest of these are read twice, in a loop.
-// 8192 x 8192 bf16 with a residual to 8 bits: 82 us, 16384 x 4096 80 (5.9 TB/s; a copy of as many bytes takes 96); to 8 bits alone: 30 us, of a copy's 41;
-// one row of 4096: 2.4 us, a launch and one trip to memory.
+// 8192 x 8192 bf16 with a residual to 8 bits: 82 us, 16384 x 4096 80 (5.9 TB/s; a copy of as many bytes takes 96); to 8 bits alone: 36 us, of a copy's 41 (30 to 32 where x is in the last-level cache);
+// one row of 4096: 2.4 us on the device, a launch and one trip to memory (2.7 on operands that no cache holds).
 // h^2 that leaves the range: h 2^-80 and r 2^80 take their places (a product with a power of two is exact).
 #include "norm_dev.h"
 
@@ -210,7 +210,7 @@ hipError_t launch(const NormArgs &a, hipStream_t st)
 {
     if (a.rows == 0) return hipSuccess;
     // (Threads a row, bf16.  Where many rows fill the machine, as few as hold it: 30000 x 1500 to 8 bits 58 us by wavefronts, 65 with 256;
-    // 16384 x 4096 80 and the norm alone 39 with 256, 81 and 42 with 512.  Fewer rows, more threads: 1 x 4096 3.1 us with 512, 3.4 with 256; 64 x 6000
+    // 16384 x 4096 80 and the norm alone 39 with 256, 81 and 42 with 512.  Fewer rows, more threads: with a residual to 8 bits 1 x 4096 2.4 us with 512, 2.6 with 256, and 256 x 4096 from memory 4.4, 4.8; 64 x 6000
     // 4.7 with 512, 5.8 with 256.  9370 values 86 us with 512, 131 with 1024; 16384 values 84, 98; 30000 values 96 from registers, 114 in two
     // passes; 20000 values 102 either way.)
     if (a.width <= 512) return launch_rows<T, 64, 1>(a, st);

@@ -1,5 +1,5 @@
 // What the kernels over whole rows share (norm.hip, norm_grad.hip): sums and maxima over a row, rows in 8 bits.  Both are bound by memory
-// (8192 x 8192 bf16 to 8 bits 30 us, 6.7 TB/s); of a single row's 2.4 us nearly all is the launch and one trip to memory, so one barrier is all they have.
+// (8192 x 8192 bf16 to 8 bits 36 us, 5.6 TB/s); of a single row's 2.4 us nearly all is the launch and one trip to memory, so one barrier is all they have.
 #pragma once
 #include "layers.h"
 

@@ -10,7 +10,7 @@
 // 1024^3 260).  32 bits: the matrix instructions (2048^3 133 TFLOP/s, 4096^3 140).
 //
 // 8 bits, results in 16: a step takes as long as in 16 bits, with twice the k.  8192 x 4096 x 8192 211 us (2.6 POP/s; without an epilogue 195),
-// with gelu and `pre` 240, 16384 of k 2.9 POP/s; on operands of zeros a step takes a quarter less: power.  A tile's epilogue is 5 us of
+// with gelu and `pre` 239 to 252 from card to card, 16384 of k 2.9 POP/s; on operands of zeros a step takes a quarter less: power.  A tile's epilogue is 5 us of
 // vector instructions (10 with gelu), and as long goes by until its first products: four times in 8192 x 8192.
 //
 // k_rows: the entries of an operand's row are contiguous along k (activations and weights of a forward pass).  LDS row r
